@@ -217,6 +217,59 @@ int dcnv4_module_forward_static(const void *x, const void *w_in, const void *b_i
 /* Size in bytes of the built-in workspace of dcnv4_module_forward_static.  Host-only helper. */
 long long dcnv4_module_static_workspace_limit(void);
 
+/* Operators of a training step around the module, on rows: x [P][C], C channels (or features) of P pixels.  As everywhere:
+ * DEVICE pointers, dense, 16-byte aligned, tensors of element type `dtype`, arithmetic and statistics in fp32, one rounding
+ * to nearest at each store, outputs must not alias inputs, nothing is allocated, nothing is kept between calls.  A workspace is the
+ * caller's and needs no initial values; two calls, or two captured graphs, that may run at the same time need one each. */
+
+/* Layer norm over the channels of each row (biased variance, as normalisation layers have it):
+ *     y = (x - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps)
+ * gamma, beta [C] or NULL (ones, zeros).  mean, rstd: fp32 [P] for the backward pass, or NULL.  Any C from 1 to 16384 (else
+ * DCNV4_ERR_UNSUPPORTED), any P; eps >= 0. */
+int dcnv4_layer_norm(const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd,
+                     long long P, int C, float eps, int dtype, void *stream);
+
+/* Its backward pass, from the forward's mean and rstd.  With xhat = (x - mean) * rstd and g = grad_y * gamma:
+ *     grad_x     = rstd * (g - avg(g) - xhat * avg(g * xhat))
+ *     grad_gamma = sum over the rows of grad_y * xhat,   grad_beta = sum of grad_y      (fp32 sums in a fixed order)
+ * grad_gamma, grad_beta [C]: either or both NULL where not wanted (both: no workspace is needed).  `workspace`: at least
+ * dcnv4_layer_norm_workspace_bytes(P, C) bytes. */
+int dcnv4_layer_norm_backward(const void *x, const void *gamma, const float *mean, const float *rstd, const void *grad_y,
+                              void *grad_x, void *grad_gamma, void *grad_beta, void *workspace, long long workspace_bytes,
+                              long long P, int C, int dtype, void *stream);
+
+/* Bytes of workspace the backward passes of the two norms need; -1 for a bad argument.  Host-only helper. */
+long long dcnv4_layer_norm_workspace_bytes(long long P, int C);
+
+/* Dropout of n elements, its mask never stored:  y[i] = residual[i] + (dropped(i) ? 0 : x[i] / (1 - p'))
+ * residual: [n] or NULL (zeros).  0 <= p <= 1; p' is p to the nearest multiple of 2^-16.  Element i is dropped where its 16
+ * random bits are below p' * 65536: number i % 8 (low half of a word first) of the four words that Philox 4x32 with ten
+ * rounds makes of the key `seed` and the counter (i / 8, offset), low words first.  So the same (seed, offset) drops the same
+ * elements, in the backward pass as in the forward one, whatever the type, and every call of a training run takes an offset of
+ * its own.  offset_on_device: NULL, or the device address (8-byte aligned) of one 64-bit number that is added to
+ * `offset` as the kernel runs: for captured graphs, whose arguments stay what they were.  A dropped element gives zero whatever x holds. */
+int dcnv4_dropout(const void *x, const void *residual, void *y, long long n, float p, unsigned long long seed,
+                  unsigned long long offset, const void *offset_on_device, int dtype, void *stream);
+
+/* grad_x of dcnv4_dropout with the same p, seed and offset (that of the residual is grad_y itself). */
+int dcnv4_dropout_backward(const void *grad_y, void *grad_x, long long n, float p, unsigned long long seed,
+                           unsigned long long offset, const void *offset_on_device, int dtype, void *stream);
+
+/* The end of a residual branch and the norm in front of the next one, in one pass:
+ *     z = residual + dropout(x)  (element i = row * C + channel),   y = layer norm of z as stored
+ * x, residual, z, y [P][C]; the rest as in dcnv4_layer_norm and dcnv4_dropout. */
+int dcnv4_dropout_add_layer_norm(const void *x, const void *residual, const void *gamma, const void *beta, void *z, void *y,
+                                 float *mean, float *rstd, long long P, int C, float p, unsigned long long seed,
+                                 unsigned long long offset, const void *offset_on_device, float eps, int dtype, void *stream);
+
+/* Its backward pass.  grad_y: the gradient of y; grad_z: that of z from what else reads it, or NULL.
+ *     grad_residual = grad_z + the norm's grad_x at z,   grad_x = dropout's gradient of that sum (before its rounding) */
+int dcnv4_dropout_add_layer_norm_backward(const void *z, const void *gamma, const float *mean, const float *rstd,
+                                          const void *grad_y, const void *grad_z, void *grad_x, void *grad_residual,
+                                          void *grad_gamma, void *grad_beta, void *workspace, long long workspace_bytes,
+                                          long long P, int C, float p, unsigned long long seed, unsigned long long offset,
+                                          const void *offset_on_device, int dtype, void *stream);
+
 /* Bytes the ideal memory-access model of Sec. 3.2 ("2HWC + 27HWG", every value touched
  * once) assigns to one forward call: x + offset + mask + y.  Host-only helper. */
 long long dcnv4_forward_algorithmic_bytes(int N, int H, int W, int G, int Cg,

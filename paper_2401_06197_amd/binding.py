@@ -19,6 +19,9 @@ EXPORTS = (
     "dcnv4_forward_softmax", "dcnv4_backward_softmax",
     "dcnv4_linear", "dcnv4_depthwise3x3", "dcnv4_module_forward", "dcnv4_module_workspace_bytes",
     "dcnv4_module_forward_static", "dcnv4_module_static_workspace_limit",
+    "dcnv4_layer_norm", "dcnv4_layer_norm_backward", "dcnv4_layer_norm_workspace_bytes",
+    "dcnv4_dropout", "dcnv4_dropout_backward",
+    "dcnv4_dropout_add_layer_norm", "dcnv4_dropout_add_layer_norm_backward",
     "dcnv4_forward_algorithmic_bytes", "dcnv4_backward_algorithmic_bytes",
     "dcnv4_forward_merged_algorithmic_bytes", "dcnv4_backward_merged_algorithmic_bytes",
     "dcnv4_set_option", "dcnv4_last_kernel_name", "dcnv4_status_string",
@@ -76,6 +79,19 @@ def load_library():
     lib.dcnv4_module_static_workspace_limit.restype = ctypes.c_longlong
     lib.dcnv4_module_workspace_bytes.argtypes = [ci] * 8
     lib.dcnv4_module_workspace_bytes.restype = ctypes.c_longlong
+    ll, ull = ctypes.c_longlong, ctypes.c_ulonglong
+    drop = [cf, ull, ull, vp]
+    lib.dcnv4_layer_norm.argtypes = [vp] * 6 + [ll, ci, cf, ci, vp]
+    lib.dcnv4_layer_norm_backward.argtypes = [vp] * 9 + [ll, ll, ci, ci, vp]
+    lib.dcnv4_layer_norm_workspace_bytes.argtypes = [ll, ci]
+    lib.dcnv4_layer_norm_workspace_bytes.restype = ll
+    lib.dcnv4_dropout.argtypes = [vp] * 3 + [ll] + drop + [ci, vp]
+    lib.dcnv4_dropout_backward.argtypes = [vp] * 2 + [ll] + drop + [ci, vp]
+    lib.dcnv4_dropout_add_layer_norm.argtypes = [vp] * 8 + [ll, ci] + drop + [cf, ci, vp]
+    lib.dcnv4_dropout_add_layer_norm_backward.argtypes = [vp] * 11 + [ll, ll, ci] + drop + [ci, vp]
+    for f in (lib.dcnv4_layer_norm, lib.dcnv4_layer_norm_backward, lib.dcnv4_dropout, lib.dcnv4_dropout_backward,
+              lib.dcnv4_dropout_add_layer_norm, lib.dcnv4_dropout_add_layer_norm_backward):
+        f.restype = ci
     lib.dcnv4_set_option.argtypes = [ctypes.c_char_p, ci]
     lib.dcnv4_set_option.restype = ci
     lib.dcnv4_last_kernel_name.argtypes = [ci]
@@ -455,3 +471,173 @@ def dcnv4_module_forward_static(x, w_om, b_om, G, out, w_in=None, b_in=None, w_o
     if rc:
         raise Dcnv4Error(rc, "dcnv4_module_forward_static")
     return out
+
+
+# Operators on rows [..., C].  Optional tensors may be None; statistics and losses are float32.
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _rows(x):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("dcnv4: expected x [..., C]")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def _check_like(x, named):
+    """_check_all, and the shape of each (name, tensor, shape); tensors that are None are left out."""
+    named = [n for n in named if n[1] is not None]
+    _check_all(x, [(name, t) for name, t, _ in named])
+    for name, t, shape in named:
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"dcnv4: {name} must have shape {tuple(shape)}")
+
+
+def _check_plain(name, t, x, shape, dtype):
+    if t.get_device() != x.get_device() or t.dtype is not dtype or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"dcnv4: {name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on x's device")
+
+
+def _outputs(x, out, specs):
+    """The output tensors: those of `out`, checked, or new ones.  specs: (name, shape, dtype), None for one that is not wanted."""
+    import torch
+    if out is None:
+        return [None if s is None else _uninitialised(x, s[1]) if s[2] is x.dtype else torch.empty(s[1], dtype=s[2], device=x.device)
+                for s in specs]
+    out = list(out) if isinstance(out, (tuple, list)) else [out]
+    if len(out) != len(specs):
+        raise ValueError(f"dcnv4: out must hold {len(specs)} tensors")
+    for t, s in zip(out, specs):
+        if (t is None) != (s is None):
+            raise ValueError("dcnv4: out must hold a tensor for every result, and None where there is none")
+        if t is not None:
+            _check_plain(s[0], t, x, s[1], s[2])
+    return out
+
+
+def _workspace(x, workspace, need):
+    import torch
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+    if workspace.get_device() != x.get_device() or not workspace.is_contiguous():
+        raise ValueError("dcnv4: workspace must be a contiguous tensor on x's device")
+    return workspace
+
+
+def _drop_args(x, p, seed, offset, offset_on_device):
+    """(p, seed, offset, address): 64-bit numbers of either sign are taken modulo 2^64."""
+    import torch
+    if offset_on_device is not None and (offset_on_device.get_device() != x.get_device() or offset_on_device.dtype is not torch.int64
+                                         or offset_on_device.numel() != 1):
+        raise ValueError("dcnv4: offset_on_device must be one int64 on x's device")
+    return float(p), int(seed) & (2 ** 64 - 1), int(offset) & (2 ** 64 - 1), _ptr(offset_on_device)
+
+
+def dcnv4_layer_norm_workspace_bytes(P, C):
+    return int(load_library().dcnv4_layer_norm_workspace_bytes(P, C))
+
+
+def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, stream=None, prepare_only=False):
+    """y = (x - mean) * rstd * gamma + beta over the last axis of x [..., C].  With `stats` (y, mean, rstd), mean and
+    rstd float32 [...], which dcnv4_layer_norm_backward takes.  `out`: y, or the three."""
+    import torch
+    P, C = _rows(x)
+    _check_like(x, (("gamma", gamma, (C,)), ("beta", beta, (C,))))
+    stat = x.shape[:-1]
+    specs = [("y", x.shape, x.dtype)] + ([("mean", stat, torch.float32), ("rstd", stat, torch.float32)] if stats else [])
+    got = _outputs(x, out, specs)
+    y, mean, rstd = got if stats else (got[0], None, None)
+    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), P, C, float(eps), _dtype_code(x),
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_layer_norm", args)
+    return (y, mean, rstd) if stats else y
+
+
+def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=None, stream=None, prepare_only=False):
+    """(grad_x, grad_gamma, grad_beta) of dcnv4_layer_norm; the last two are None where gamma is None (a norm without
+    parameters)."""
+    import torch
+    P, C = _rows(x)
+    _check_like(x, (("gamma", gamma, (C,)), ("grad_y", grad_y, x.shape)))
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _check_plain(name, t, x, x.shape[:-1], torch.float32)
+    param = None if gamma is None else ((C,), x.dtype)
+    gx, gg, gb = _outputs(x, out, [("grad_x", x.shape, x.dtype)] + [param and (name, *param) for name in ("grad_gamma", "grad_beta")])
+    if param is not None:
+        workspace = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C))
+    args = (x.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), grad_y.data_ptr(), gx.data_ptr(), _ptr(gg), _ptr(gb),
+            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), P, C, _dtype_code(x),
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_layer_norm_backward", args)
+    return gx, gg, gb
+
+
+def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, out=None, stream=None, prepare_only=False):
+    """[residual +] dropout of x: element i is dropped where its bits of the generator (include/dcnv4.h) at (seed, offset) say so,
+    else scaled by 1 / (1 - p).  offset_on_device: one int64 on the GPU, added to offset as the kernel runs (captured
+    graphs)."""
+    _check_like(x, (("residual", residual, x.shape),))
+    y, = _outputs(x, out, [("out", x.shape, x.dtype)])
+    args = (x.data_ptr(), _ptr(residual), y.data_ptr(), x.numel(), *_drop_args(x, p, seed, offset, offset_on_device), _dtype_code(x),
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_dropout", args)
+    return y
+
+
+def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out=None, stream=None, prepare_only=False):
+    """grad_x of dcnv4_dropout with the same p, seed and offset (that of the residual is grad_y itself)."""
+    _check_all(grad_y, ())
+    gx, = _outputs(grad_y, out, [("out", grad_y.shape, grad_y.dtype)])
+    args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), *_drop_args(grad_y, p, seed, offset, offset_on_device), _dtype_code(grad_y),
+            _stream_ptr(stream, grad_y.device))
+    if prepare_only:
+        return args
+    _call(grad_y.device, "dcnv4_dropout_backward", args)
+    return gx
+
+
+def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, offset_on_device=None, eps=1e-6, out=None, stream=None,
+                                 prepare_only=False):
+    """(z, y, mean, rstd): z = residual + dropout(x), y = layer norm of z over the last axis."""
+    import torch
+    P, C = _rows(x)
+    _check_like(x, (("residual", residual, x.shape), ("gamma", gamma, (C,)), ("beta", beta, (C,))))
+    stat = x.shape[:-1]
+    z, y, mean, rstd = _outputs(x, out, [("z", x.shape, x.dtype), ("y", x.shape, x.dtype), ("mean", stat, torch.float32),
+                                         ("rstd", stat, torch.float32)])
+    args = (x.data_ptr(), residual.data_ptr(), _ptr(gamma), _ptr(beta), z.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), P, C,
+            *_drop_args(x, p, seed, offset, offset_on_device), float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_dropout_add_layer_norm", args)
+    return z, y, mean, rstd
+
+
+def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed, offset=0, offset_on_device=None, grad_z=None,
+                                          workspace=None, out=None, stream=None, prepare_only=False):
+    """(grad_x, grad_residual, grad_gamma, grad_beta) of dcnv4_dropout_add_layer_norm; grad_z: the gradient of z from what else
+    reads it.  The last two are None where gamma is None."""
+    import torch
+    P, C = _rows(z)
+    _check_like(z, (("gamma", gamma, (C,)), ("grad_y", grad_y, z.shape), ("grad_z", grad_z, z.shape)))
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _check_plain(name, t, z, z.shape[:-1], torch.float32)
+    param = None if gamma is None else ((C,), z.dtype)
+    gx, gr, gg, gb = _outputs(z, out, [("grad_x", z.shape, z.dtype), ("grad_residual", z.shape, z.dtype)] +
+                              [param and (name, *param) for name in ("grad_gamma", "grad_beta")])
+    if param is not None:
+        workspace = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C))
+    args = (z.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), grad_y.data_ptr(), _ptr(grad_z), gx.data_ptr(), gr.data_ptr(),
+            _ptr(gg), _ptr(gb), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), P, C,
+            *_drop_args(z, p, seed, offset, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
+    if prepare_only:
+        return args
+    _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
+    return gx, gr, gg, gb

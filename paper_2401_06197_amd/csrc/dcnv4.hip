@@ -15,38 +15,12 @@
 
 #include <type_traits>
 
-#include "dcnv4.h"
+#include "dcnv4_common.h"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTaps = 9;
-constexpr int kXcds = 8;
-// Word 3 of a gfx9-family raw buffer descriptor: 32-bit data format, no swizzle, no stride.
-constexpr int kRsrcWord3 = 0x00020000;
-// A byte offset no descriptor of ours reaches (images are validated below 2^31 bytes):
-// loads through it return zero, atomics through it are dropped.
-constexpr int kOutside = (int)0x80000000u;
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-
-// n / d for 0 <= n < 2^31 as mulhi + add + shift (d >= 1), constants made on the host.
-struct FastDiv {
-    unsigned mul, shift;
-};
-
-__device__ __forceinline__ int fdiv(int n, FastDiv f)
-{
-    return (int)((__umulhi((unsigned)n, f.mul) + (unsigned)n) >> f.shift);
-}
-
 typedef const __attribute__((address_space(4))) FastDiv ArgDiv;        // in the kernel's arguments
 __device__ __forceinline__ int arg_div(int n, ArgDiv &f)
 {
@@ -67,11 +41,6 @@ struct Geo {
     int row_bytes;      // W*C*sizeof(T)
     int pix_bytes;      // C*sizeof(T)
 };
-
-__device__ __forceinline__ rsrc_t make_rsrc(const void *base, unsigned bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, kRsrcWord3);
-}
 
 // blockIdx -> tile.  Hardware deals consecutive workgroups to the 8 XCDs in turn; with the
 // remap XCD i works through tiles [i*tiles_per_xcd, (i+1)*tiles_per_xcd) in order, so the
@@ -547,19 +516,6 @@ struct Options {
 
 char g_last_kernel[2][128];
 
-FastDiv make_div(unsigned d)
-{
-    unsigned s = 0;
-    while ((1ull << s) < d)
-        ++s;
-    FastDiv f;
-    f.shift = s;
-    f.mul = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
-    return f;
-}
-
-int esize(int dtype) { return dtype == DCNV4_F16 ? 2 : 4; }
-
 struct Problem {
     int N, H, W, G, Cg, Ho, Wo;
     int kh, kw;     // window: 3x3 everywhere; 1x1 and 5x5 through the direct kernels only
@@ -722,32 +678,6 @@ constexpr int kDefaultHaloGradX = 4;
 constexpr int kStripMinHalo = 4, kStripMaxHalo = 12;
 constexpr int kDefaultLdsKb = 158;
 constexpr int kMaxLdsBytes = 160 * 1024;
-
-// Per-device caches (compute-unit count, dynamic-LDS grants) are indexed by the HIP device number.
-constexpr int kMaxDevices = 64;
-int current_device()
-{
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices)
-        return -1;
-    return dev;
-}
-
-// Number of compute units of the current device (persistent kernels launch one workgroup each).
-int device_cus()
-{
-    static int cus[kMaxDevices];
-    const int dev = current_device();
-    if (dev < 0)
-        return 0;
-    if (cus[dev] == 0) {
-        int n = 0;
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < kXcds)
-            return 0;
-        cus[dev] = n;
-    }
-    return cus[dev];
-}
 
 // Lets `kern` use `lds` bytes of dynamic LDS on the current device (asked for once per device and size).
 bool grant_lds(const void *kern, int lds, int (&granted)[kMaxDevices])
@@ -2304,8 +2234,6 @@ int launch_depthwise(const void *x, const void *w, const void *b, void *y, int N
                            (const float *)w, (const float *)b, (float *)y, g);
     return hipGetLastError() == hipSuccess ? DCNV4_OK : DCNV4_ERR_LAUNCH;
 }
-
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 }  // namespace
 

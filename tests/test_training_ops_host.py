@@ -1,0 +1,96 @@
+"""Host-side checks of the operators around the module: refusals before any launch, and the plain forms themselves."""
+import numpy as np
+import pytest
+
+import training_ref as ref
+from paper_2401_06197_amd import binding as dcn
+
+A = 4096                                                     # aligned, never dereferenced
+
+
+def test_generator_gives_the_published_numbers():
+    """The known answers that its authors publish for Philox 4x32 with ten rounds."""
+    words = lambda counter, key: [int(w) for w in ref.philox(counter, key)]
+    assert words([0, 0, 0, 0], (0, 0)) == [0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]
+    assert words([0xffffffff] * 4, (0xffffffff, 0xffffffff)) == [0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]
+
+
+def test_gradient_of_the_plain_norm_against_differences():
+    rng = np.random.default_rng(0)
+    x, gamma, gy = rng.standard_normal((2, 5)), rng.standard_normal(5), rng.standard_normal((2, 5))
+    _, mean, rstd = ref.layer_norm(x, gamma, None, 1e-3)
+    (gx, gg, gb), _ = ref.layer_norm_backward(x, gamma, mean, rstd, gy)
+    value = lambda x, g, b: (ref.layer_norm(x, g, b, 1e-3)[0] * gy).sum()
+    h = 1e-6
+    for which, grad in enumerate((gx, gg, gb)):
+        for i in range(grad.size):
+            args = [x.copy(), gamma.copy(), np.zeros(5)]
+            args[which].reshape(-1)[i] += h
+            up = value(*args)
+            args[which].reshape(-1)[i] -= 2 * h
+            assert abs((up - value(*args)) / (2 * h) - grad.reshape(-1)[i]) < 1e-7
+
+
+def norm(x=A, gamma=None, beta=None, y=A, mean=None, rstd=None, P=5, C=16, eps=1e-6, dtype=0):
+    return dcn.load_library().dcnv4_layer_norm(x, gamma, beta, y, mean, rstd, P, C, eps, dtype, None)
+
+
+def norm_back(ptrs=(A,) * 9, size=1 << 30, P=5, C=16, dtype=0):
+    return dcn.load_library().dcnv4_layer_norm_backward(*ptrs, size, P, C, dtype, None)
+
+
+def drop(x=A, r=None, y=A, n=10, p=0.1, more=None, dtype=0):
+    return dcn.load_library().dcnv4_dropout(x, r, y, n, p, 1, 2, more, dtype, None)
+
+
+def branch(ptrs=(A,) * 8, P=5, C=16, p=0.1, eps=1e-6, more=None, dtype=0):
+    return dcn.load_library().dcnv4_dropout_add_layer_norm(*ptrs, P, C, p, 1, 2, more, eps, dtype, None)
+
+
+def branch_back(ptrs=(A,) * 11, size=1 << 30, P=5, C=16, p=0.1, more=None, dtype=0):
+    return dcn.load_library().dcnv4_dropout_add_layer_norm_backward(*ptrs, size, P, C, p, 1, 2, more, dtype, None)
+
+
+def without(count, i, value=None):
+    ptrs = [A] * count
+    ptrs[i] = value
+    return tuple(ptrs)
+
+
+def test_norm_and_dropout_validate_on_the_host():
+    assert norm(x=None) == 1 and norm(y=None) == 1
+    assert norm(P=0) == 2 and norm(C=0) == 2 and norm(P=-1) == 2
+    assert norm(C=16385) == 3 and norm(dtype=2) == 3 and norm(eps=-1.0) == 3 and norm(eps=float("nan")) == 3 and norm(eps=float("inf")) == 3
+    for name in ("x", "gamma", "beta", "y", "mean", "rstd"):
+        assert norm(**{name: A + 8}) == 4
+    for i in (0, 2, 3, 4, 5, 8):
+        assert norm_back(without(9, i)) == 1
+    assert norm_back(size=dcn.dcnv4_layer_norm_workspace_bytes(5, 16) - 1) == 2 and norm_back(P=0) == 2 and norm_back(C=20000) == 3
+    for i in range(9):
+        assert norm_back(without(9, i, A + 4)) == 4
+    assert drop(x=None) == 1 and drop(y=None) == 1 and drop(n=0) == 2 and drop(dtype=5) == 3
+    assert drop(p=-0.1) == 3 and drop(p=1.01) == 3 and drop(p=float("nan")) == 3
+    assert drop(x=A + 2) == 4 and drop(r=A + 8) == 4 and drop(y=A + 4) == 4 and drop(more=A + 4) == 4
+    assert dcn.load_library().dcnv4_dropout_backward(None, A, 10, 0.1, 1, 2, None, 0, None) == 1
+    for i in (0, 1, 4, 5):
+        assert branch(without(8, i)) == 1
+    assert branch(p=2.0) == 3 and branch(P=0) == 2 and branch(eps=-1.0) == 3 and branch(more=A + 1) == 4
+    for i in range(8):
+        assert branch(without(8, i, A + 8)) == 4
+    for i in (0, 2, 3, 4, 6, 7, 10):
+        assert branch_back(without(11, i)) == 1
+    for i in range(11):
+        assert branch_back(without(11, i, A + 8)) == 4
+    assert branch_back(size=0) == 2 and branch_back(p=-1.0) == 3 and branch_back(C=16385) == 3
+    assert dcn.dcnv4_layer_norm_workspace_bytes(0, 16) == -1 and dcn.dcnv4_layer_norm_workspace_bytes(5, 20000) == -1
+    assert dcn.dcnv4_layer_norm_workspace_bytes(10 ** 9, 16384) < 1 << 30
+
+
+def test_host_tensors_are_refused():
+    import torch
+    x, s = torch.zeros((3, 8)), torch.zeros(3)
+    for call in (lambda: dcn.dcnv4_layer_norm(x), lambda: dcn.dcnv4_layer_norm_backward(x, None, s, s, x), lambda: dcn.dcnv4_dropout(x, 0.1, 1),
+                 lambda: dcn.dcnv4_dropout_backward(x, 0.1, 1), lambda: dcn.dcnv4_dropout_add_layer_norm(x, x, None, None, 0.1, 1),
+                 lambda: dcn.dcnv4_dropout_add_layer_norm_backward(x, None, s, s, x, 0.1, 1)):
+        with pytest.raises(ValueError, match="x must be a GPU tensor"):
+            call()
