@@ -270,6 +270,33 @@ int dcnv4_dropout_add_layer_norm_backward(const void *z, const void *gamma, cons
                                           long long P, int C, float p, unsigned long long seed, unsigned long long offset,
                                           const void *offset_on_device, int dtype, void *stream);
 
+/* Softmax cross entropy out of the last linear layer (a classifier's, or each pixel's), without its logits being stored:
+ *     logit[p][v] = sum_k x[p][k] * w[v][k] + b[v],   lse[p] = log sum_v exp(logit[p][v]),   loss[p] = lse[p] - logit[p][target[p]]
+ * x [P][K], w [V][K], b [V] or NULL; target: 64-bit class numbers [P]; loss, lse: fp32 [P].  A row whose target is ignore_index
+ * has loss 0; one whose target is neither that nor a class has loss NaN.  Logits and sums are fp32 (F32: products of operands
+ * held as three bf16 numbers, fp32's accuracy for numbers above 2^-100; x and w must be finite, F16 follows fp16's infinities).  b may
+ * hold -infinity: that class has probability 0.
+ * Needs K * element size a multiple of 32 bytes, K and P up to 2^20, V up to 2^22 (else DCNV4_ERR_UNSUPPORTED); any V and P.
+ * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 0) bytes. */
+int dcnv4_linear_cross_entropy(const void *x, const void *w, const void *b, const long long *target, float *loss, float *lse,
+                               void *workspace, long long workspace_bytes, long long P, int K, int V,
+                               long long ignore_index, int dtype, void *stream);
+
+/* Its backward pass, from the forward's lse and grad_loss fp32 [P].  With d = exp(logit - lse) - (v == target), a piece of the classes
+ * at a time:
+ *     grad_x[p] = grad_loss[p] * sum_v d[p][v] * w[v],   grad_w[v] = sum_p grad_loss[p] * d[p][v] * x[p],   grad_b[v] = sum_p grad_loss[p] * d[p][v]
+ * In F16 d is rounded to fp16 (of 2^15 * d, for grad_w and grad_b times grad_loss / a power of two no less than the largest), sums are fp32.
+ * A row that is ignored, or whose grad_loss is 0, counts for nothing and has grad_x 0, whatever x holds there; one with
+ * loss NaN has grad_x NaN and makes grad_w NaN.  grad_b may be NULL.  Sums are made in a fixed order.
+ * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 1) bytes. */
+int dcnv4_linear_cross_entropy_backward(const void *x, const void *w, const void *b, const long long *target,
+                                        const float *lse, const float *grad_loss, void *grad_x, void *grad_w, void *grad_b,
+                                        void *workspace, long long workspace_bytes, long long P, int K, int V,
+                                        long long ignore_index, int dtype, void *stream);
+
+/* Bytes of workspace the two need; -1 for arguments that they refuse.  Host-only helper. */
+long long dcnv4_linear_cross_entropy_workspace_bytes(long long P, int K, int V, int dtype, int backward);
+
 /* Bytes the ideal memory-access model of Sec. 3.2 ("2HWC + 27HWG", every value touched
  * once) assigns to one forward call: x + offset + mask + y.  Host-only helper. */
 long long dcnv4_forward_algorithmic_bytes(int N, int H, int W, int G, int Cg,
@@ -313,6 +340,9 @@ long long dcnv4_backward_merged_algorithmic_bytes(int N, int H, int W, int G, in
  *   "linear_tile" tile of the linear layers, output channels x pixels: 1 = 128x128, 2 = 64x64, 3 = 256x256,
  *                 4 = 128x256 (fp32), 5 = the kernel that reads x once (fp16, K of up to 256 bytes); 0 = the one
  *                 with the lowest estimated time.  In place of a tile that a type or K does not have: 128x128
+ *   "loss_tile"   tile of the cross entropy's products, classes x pixels: 1 = 64x64, 2 = 128x128, 3 = 256x256 (fp32: 256x128)
+ *   "loss_splits" workgroups that share a sum of its gradients (1..64)
+ *   "loss_piece"  classes of a piece (rounded up to a multiple of 256); these three change the size of its workspace
  *   "gom_coop"    1 = the fp32 grad_offset/grad_mask pass moves its values through per-wave LDS slices
  *                 even for whole groups (default: each lane reads and writes its own pixel's values)
  *   "gx_threads"  workgroup size of the staged grad_x kernel (256, 512 or 768)

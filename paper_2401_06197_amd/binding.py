@@ -22,6 +22,7 @@ EXPORTS = (
     "dcnv4_layer_norm", "dcnv4_layer_norm_backward", "dcnv4_layer_norm_workspace_bytes",
     "dcnv4_dropout", "dcnv4_dropout_backward",
     "dcnv4_dropout_add_layer_norm", "dcnv4_dropout_add_layer_norm_backward",
+    "dcnv4_linear_cross_entropy", "dcnv4_linear_cross_entropy_backward", "dcnv4_linear_cross_entropy_workspace_bytes",
     "dcnv4_forward_algorithmic_bytes", "dcnv4_backward_algorithmic_bytes",
     "dcnv4_forward_merged_algorithmic_bytes", "dcnv4_backward_merged_algorithmic_bytes",
     "dcnv4_set_option", "dcnv4_last_kernel_name", "dcnv4_status_string",
@@ -89,6 +90,11 @@ def load_library():
     lib.dcnv4_dropout_backward.argtypes = [vp] * 2 + [ll] + drop + [ci, vp]
     lib.dcnv4_dropout_add_layer_norm.argtypes = [vp] * 8 + [ll, ci] + drop + [cf, ci, vp]
     lib.dcnv4_dropout_add_layer_norm_backward.argtypes = [vp] * 11 + [ll, ll, ci] + drop + [ci, vp]
+    lib.dcnv4_linear_cross_entropy.argtypes = [vp] * 7 + [ll, ll, ci, ci, ll, ci, vp]
+    lib.dcnv4_linear_cross_entropy_backward.argtypes = [vp] * 10 + [ll, ll, ci, ci, ll, ci, vp]
+    lib.dcnv4_linear_cross_entropy_workspace_bytes.argtypes = [ll, ci, ci, ci, ci]
+    lib.dcnv4_linear_cross_entropy_workspace_bytes.restype = ll
+    lib.dcnv4_linear_cross_entropy.restype = lib.dcnv4_linear_cross_entropy_backward.restype = ci
     for f in (lib.dcnv4_layer_norm, lib.dcnv4_layer_norm_backward, lib.dcnv4_dropout, lib.dcnv4_dropout_backward,
               lib.dcnv4_dropout_add_layer_norm, lib.dcnv4_dropout_add_layer_norm_backward):
         f.restype = ci
@@ -641,3 +647,50 @@ def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed,
         return args
     _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
     return gx, gr, gg, gb
+
+
+def dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dtype, backward):
+    return int(load_library().dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dtype, int(bool(backward))))
+
+
+def _loss_args(x, w, target, b, workspace, backward):
+    import torch
+    P, K = _rows(x)
+    if w.dim() != 2 or w.shape[1] != K:
+        raise ValueError("dcnv4: expected x [..., K], w [V, K]")
+    V = w.shape[0]
+    _check_like(x, (("w", w, (V, K)), ("b", b, (V,))))
+    _check_plain("target", target, x, x.shape[:-1], torch.int64)
+    return P, K, V, _workspace(x, workspace, dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, _dtype_code(x), backward))
+
+
+def dcnv4_linear_cross_entropy(x, w, target, b=None, ignore_index=-100, workspace=None, out=None, stream=None, prepare_only=False):
+    """(loss, lse), float32 [...]: loss = lse - logit[target] with logits x w^T + b that are never stored.  x [..., K], w [V, K],
+    target [...] int64; rows whose target is ignore_index have loss 0."""
+    import torch
+    P, K, V, workspace = _loss_args(x, w, target, b, workspace, False)
+    loss, lse = _outputs(x, out, [("loss", x.shape[:-1], torch.float32), ("lse", x.shape[:-1], torch.float32)])
+    args = (x.data_ptr(), w.data_ptr(), _ptr(b), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_linear_cross_entropy", args)
+    return loss, lse
+
+
+def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ignore_index=-100, workspace=None, out=None, stream=None,
+                                        prepare_only=False):
+    """(grad_x, grad_w, grad_b) of dcnv4_linear_cross_entropy for grad_loss [...] float32, from its lse; grad_b is None where b is."""
+    import torch
+    P, K, V, workspace = _loss_args(x, w, target, b, workspace, True)
+    for name, t in (("lse", lse), ("grad_loss", grad_loss)):
+        _check_plain(name, t, x, x.shape[:-1], torch.float32)
+    gx, gw, gb = _outputs(x, out, [("grad_x", x.shape, x.dtype), ("grad_w", (V, K), x.dtype),
+                                   None if b is None else ("grad_b", (V,), x.dtype)])
+    args = (x.data_ptr(), w.data_ptr(), _ptr(b), target.data_ptr(), lse.data_ptr(), grad_loss.data_ptr(), gx.data_ptr(), gw.data_ptr(),
+            _ptr(gb), workspace.data_ptr(), workspace.numel() * workspace.element_size(), P, K, V, int(ignore_index), _dtype_code(x),
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return args
+    _call(x.device, "dcnv4_linear_cross_entropy_backward", args)
+    return gx, gw, gb

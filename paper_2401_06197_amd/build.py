@@ -8,7 +8,7 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("dcnv4.hip", "dcnv4_norm.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("dcnv4.hip", "dcnv4_norm.hip", "dcnv4_loss.hip")]
 LIB = os.path.join(HERE, "libdcnv4.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

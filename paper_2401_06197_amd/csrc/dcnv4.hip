@@ -2521,7 +2521,7 @@ int dcnv4_set_option(const char *key, int value)
         return DCNV4_ERR_NULL;
     if (!strcmp(key, "reset")) {             // every switch back to the library's own choice
         g_opt = Options();
-        return DCNV4_OK;
+        return loss_set_option(key, value);
     }
     if (!strcmp(key, "fwd_cpt") && (value == 0 || value == 8 || value == 16)) {
         g_opt.fwd_cpt = value;
@@ -2587,7 +2587,7 @@ int dcnv4_set_option(const char *key, int value)
         g_opt.fwd_threads = value;
         return DCNV4_OK;
     }
-    return DCNV4_ERR_UNSUPPORTED;
+    return loss_set_option(key, value);
 }
 
 const char *dcnv4_last_kernel_name(int backward)

@@ -5,6 +5,9 @@
 
 #include "dcnv4.h"
 
+// Switches of the cross entropy (dcnv4_loss.hip); DCNV4_ERR_UNSUPPORTED for a key or value that is not one of them.
+__attribute__((visibility("hidden"))) int loss_set_option(const char *key, int value);
+
 namespace {
 
 constexpr int kXcds = 8;

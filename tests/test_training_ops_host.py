@@ -94,3 +94,40 @@ def test_host_tensors_are_refused():
                  lambda: dcn.dcnv4_dropout_add_layer_norm_backward(x, None, s, s, x, 0.1, 1)):
         with pytest.raises(ValueError, match="x must be a GPU tensor"):
             call()
+
+
+def loss(ptrs=(A,) * 7, size=1 << 40, P=5, K=32, V=7, dtype=0):
+    return dcn.load_library().dcnv4_linear_cross_entropy(*ptrs, size, P, K, V, -100, dtype, None)
+
+
+def loss_back(ptrs=(A,) * 10, size=1 << 40, P=5, K=32, V=7, dtype=0):
+    return dcn.load_library().dcnv4_linear_cross_entropy_backward(*ptrs, size, P, K, V, -100, dtype, None)
+
+
+def test_cross_entropy_validates_on_the_host():
+    for call, count, optional in ((loss, 7, (2,)), (loss_back, 10, (2, 8))):
+        for i in range(count):
+            if i not in optional:
+                assert call(without(count, i)) == 1
+            assert call(without(count, i, A + 8)) == 4
+        assert call(P=0) == 2 and call(K=0) == 2 and call(V=0) == 2 and call(V=-3) == 2
+        assert call(K=12) == 3 and call(K=24, dtype=1) == 3 and call(dtype=2) == 3
+        assert call(P=(1 << 20) + 1) == 3 and call(V=(1 << 22) + 1) == 3 and call(K=1 << 21) == 3
+        for dtype in (0, 1):
+            need = dcn.dcnv4_linear_cross_entropy_workspace_bytes(5, 32, 7, dtype, call is loss_back)
+            assert call(size=need - 1, dtype=dtype) == 2
+    assert dcn.dcnv4_linear_cross_entropy_workspace_bytes(0, 32, 7, 0, False) == -1
+    # in pieces: far less than the logits' 4 bytes * P * V, whatever V
+    P, K, V = 8192, 1024, 1 << 20
+    assert dcn.dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, 1, True) < 4 * P * V / 16
+    for key, bad in (("loss_tile", 4), ("loss_splits", 65), ("loss_piece", -1)):
+        with pytest.raises(dcn.Dcnv4Error):
+            dcn.dcnv4_set_option(key, bad)
+
+
+def test_cross_entropy_refuses_host_tensors():
+    import torch
+    x, w, t, s = torch.zeros((3, 8)), torch.zeros((5, 8)), torch.zeros(3, dtype=torch.int64), torch.zeros(3)
+    for call in (lambda: dcn.dcnv4_linear_cross_entropy(x, w, t), lambda: dcn.dcnv4_linear_cross_entropy_backward(x, w, t, s, s)):
+        with pytest.raises(ValueError, match="x must be a GPU tensor"):
+            call()
