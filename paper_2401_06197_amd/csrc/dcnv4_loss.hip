@@ -164,71 +164,69 @@ template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, b
             sa.load(to, t, t1);
             sb.load(to + BM * STEP, t, t1);
         };
+        // Fragments are read while the products of the group before them run, across steps too: where the last group of a
+        // step is in registers, its stage is free for the loads of step t + STAGES, and the next step's first group is read beside its
+        // products.
+        u32x4 af[2][PL][WM], bf[2][PL][WN];
+        auto fetch = [&](const char *stage, int g) {
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
+            for (int p = 0; p < PL; ++p) {
+#pragma unroll
+                for (int m = 0; m < WM; ++m)
+                    af[g & 1][p][m] = fragment<TA, BM>(stage + p * PLANE, (wr * WM + m) * 32, g, lane);
+#pragma unroll
+                for (int n = 0; n < WN; ++n)
+                    bf[g & 1][p][n] = fragment<TB, BN>(stage + p * PLANE + BM * STEP, (wc * WN + n) * 32, g, lane);
+            }
+        };
+        auto products = [&](int g) {
+            // (three planes: small parts first)
+            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+            for (int q = PL == 1 ? 5 : 0; q < 6; ++q)
+#pragma unroll
+                for (int m = 0; m < WM; ++m)
+#pragma unroll
+                    for (int n = 0; n < WN; ++n) {
+                        const u32x4 x = af[g & 1][pa[q]][m], y = bf[g & 1][pb[q]][n];
+                        if constexpr (PL == 1)
+                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y),
+                                                                               acc[m][n], 0, 0, 0);
+                        else
+                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y),
+                                                                                acc[m][n], 0, 0, 0);
+                    }
+        };
+        constexpr int GROUPS = R / 16;
+        static_assert(GROUPS % 2 == 0 && (STAGES - 1) * LOADS < 64);
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
             load(t0 + s, s);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fetch(smem, 0);
         int at = 0;
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
-            // this step's loads have landed, for every wave, and all are done with the stage of the step before
+            const char *stage = smem + at * STAGE;
+#pragma unroll
+            for (int g = 0; g + 1 < GROUPS; ++g) {
+                fetch(stage, g + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                products(g);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // the next step's loads have landed, for every wave, and all have read this stage
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * LOADS) : "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            load(t + STAGES - 1, at == 0 ? STAGES - 1 : at - 1);
-            const char *stage = smem + at * STAGE;
+            load(t + STAGES, at);
             at = at + 1 == STAGES ? 0 : at + 1;
-            auto fetch_a = [&](int p, int g, int m) { return fragment<TA, BM>(stage + p * PLANE, (wr * WM + m) * 32, g, lane); };
-            auto fetch_b = [&](int p, int g, int n) { return fragment<TB, BN>(stage + p * PLANE + BM * STEP, (wc * WN + n) * 32, g, lane); };
-            if constexpr (PL == 1) {
-                // fragments are read while the products of the group before them run
-                u32x4 af[2][WM], bf[2][WN];
-                auto fetch = [&](int g) {
-#pragma unroll
-                    for (int m = 0; m < WM; ++m)
-                        af[g & 1][m] = fetch_a(0, g, m);
-#pragma unroll
-                    for (int n = 0; n < WN; ++n)
-                        bf[g & 1][n] = fetch_b(0, g, n);
-                };
-                fetch(0);
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if (g + 1 < 4)
-                        fetch(g + 1);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int m = 0; m < WM; ++m)
-#pragma unroll
-                        for (int n = 0; n < WN; ++n)
-                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, af[g & 1][m]),
-                                                                               __builtin_bit_cast(f16x8, bf[g & 1][n]), acc[m][n], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    u32x4 af[3][WM], bf[3][WN];
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) {
-#pragma unroll
-                        for (int m = 0; m < WM; ++m)
-                            af[p][m] = fetch_a(p, g, m);
-#pragma unroll
-                        for (int n = 0; n < WN; ++n)
-                            bf[p][n] = fetch_b(p, g, n);
-                    }
-                    // small parts first
-                    constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};
-#pragma unroll
-                    for (int q = 0; q < 6; ++q)
-#pragma unroll
-                        for (int m = 0; m < WM; ++m)
-#pragma unroll
-                            for (int n = 0; n < WN; ++n)
-                                acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, af[pa[q]][m]),
-                                                                                    __builtin_bit_cast(bf16x8, bf[pb[q]][n]), acc[m][n], 0, 0, 0);
-                }
-            }
+            fetch(smem + at * STAGE, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            products(GROUPS - 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (results go where the last loads write)
         __syncthreads();
