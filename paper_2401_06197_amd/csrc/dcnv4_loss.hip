@@ -40,8 +40,8 @@ struct Operand {
 struct Product {
     Operand a, b;
     int steps, steps_per_split;
-    int a_tiles, tiles, tiles_per_xcd;
-    FastDiv div_a;
+    int a_tiles, b_tiles, tiles, tiles_per_xcd;
+    FastDiv div_band, div_3;           // by the tiles of a band of four, and by three
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -54,11 +54,12 @@ __device__ __forceinline__ s16x4 read_turned(const lds_s16x4 *__restrict p)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_s16x4 *>(p));
 }
 
-// PL planes: 1 (fp16) or 3 (fp32 as three bf16).  A step is 64 numbers r of one plane, or 32 of each of three.  TA, TB: A, B turned.
-template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, bool TB = false> struct Tile {
+// PL planes: 1 (fp16) or 3 (fp32 as three bf16).  A step is R numbers r of each plane, of which STAGES are in LDS or on their way.  TA, TB:
+// A, B turned.
+template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = false, bool TB = false> struct Tile {
     static constexpr int kWaves = WR * WC, kThreads = kWaves * 64;
     static constexpr int BM = WR * 32 * WM, BN = WC * 32 * WN;
-    static constexpr int R = PL == 1 ? 64 : 32, STEP = 2 * R;              // a step in numbers, and in bytes
+    static constexpr int STEP = 2 * R;                                     // a step in bytes
     static constexpr int LOAD = kWaves * 1024;                             // bytes that all waves' load brings
     static constexpr int LA = BM * STEP / LOAD, LB = BN * STEP / LOAD, LOADS = (LA + LB) * PL;
     static_assert(LA * LOAD == BM * STEP && LB * LOAD == BN * STEP);
@@ -67,13 +68,14 @@ template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, b
     static constexpr int LDS = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
     static constexpr int kWavesPerSimd = kWaves / 4 * (LDS > 80 * 1024 ? 1 : 2);     // that registers have to leave room for
 
-    // Where things lie in LDS.  As it is: rows of STEP bytes, their 16-byte units permuted so that a fragment's reads, 16 rows at a
-    // time, fall on all banks.  Turned: rows (r) of 2 * COUNT bytes, their pieces of 32 bytes (what 16 lanes of a turning read take of a
-    // row) permuted so that the eight rows of a read (k to k + 3 and k + 8 to k + 11) fall on all banks.
-    static __device__ __forceinline__ int swizzle(int row) { return PL == 1 ? row & 7 : (row >> 2) & 3; }
-    template <int COUNT> static __device__ __forceinline__ int swizzle_turned(int r)
+    // Where things lie in LDS, so that what is read in one pass falls on all 64 banks.  As it is: rows of STEP bytes; a pass of a 16-byte
+    // read is 16 lanes (of the first 32: 0-3, 12-15, 20-27, and the others), so rows two apart (128-byte rows; four, 64-byte rows) take
+    // other units.  Turned: rows (r) of 2 * COUNT bytes; a pass of a turning read is 32 lanes, 64 bytes of four rows, which take
+    // other 64-byte pieces.  (Units by row % 8: half of all passes met a conflict, 8192 x 1024 x 8192 forward 152 us.)
+    static __device__ __forceinline__ int swizzle(int row) { return R == 64 ? row >> 1 & 7 : row >> 2 & 3; }
+    template <int COUNT> static __device__ __forceinline__ int swizzle_turned(int r)     // in pieces of 32 bytes
     {
-        return COUNT >= 128 ? (r & 3) | (r >> 1 & 4) : (r >> 1 & 1) | (r >> 2 & 2);
+        return COUNT >= 128 ? (r & 3) << 1 : r & 2;
     }
 
     // An operand's loads: what a lane asks for, load after load, of COUNT rows from i0 on.
@@ -106,29 +108,28 @@ template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, b
                     from[i] = (int)(min(i * kWaves * ROWS + first, rows - 1) * o.row_bytes) + at0;
             }
         }
-        // past t1: nothing is read, zeros are written; likewise past the sum's length
-        __device__ __forceinline__ void load(char *to, int t, int t1) const
+        // Step t: past t1 nothing is read and zeros are written, likewise past the sum's length.
+        rsrc_t r;
+        unsigned out;
+        int at;
+        __device__ __forceinline__ void step(int t, int t1)
         {
-            rsrc_t r;
-            unsigned out = 0u;
-            int at = 0;
             if constexpr (TURNED) {
                 // (from row t * R on; what lies past a row's end is the next one's, for rows of the result that are dropped)
                 const int left = t < t1 ? min(R, o.length - t * R) : 0;
-                r = make_rsrc(base + (long long)t * R * o.row_bytes, (unsigned)(left * o.row_bytes - (base - o.base)));
-                if (left <= 0)
-                    r = make_rsrc(base, 0u);
+                r = make_rsrc(base + (long long)t * R * o.row_bytes, left <= 0 ? 0u : (unsigned)(left * o.row_bytes - (base - o.base)));
+                out = 0u;
+                at = 0;
             } else {
                 r = make_rsrc(base, (unsigned)(rows * o.row_bytes));
                 at = t * STEP;
                 out = t < t1 && at + at0 < 2 * o.length ? 0u : (unsigned)kOutside;
             }
-#pragma unroll
-            for (int p = 0; p < PL; ++p)
-#pragma unroll
-                for (int i = 0; i < LOADS_; ++i)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + p * PLANE + i * LOAD), 16,
-                                                             (int)((unsigned)(from[i] + at + p * o.plane_bytes) | out), 0, 0, 0);
+        }
+        __device__ __forceinline__ void load(char *to, int p, int i) const
+        {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + p * PLANE + i * LOAD), 16,
+                                                     (int)((unsigned)(from[i] + at + p * o.plane_bytes) | out), 0, 0, 0);
         }
     };
 
@@ -157,37 +158,38 @@ template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, b
         const int tid = (int)threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wr = wave / WC, wc = wave % WC;
-        const Source<TA, BM, LA> sa(a, a0, wave, lane);
-        const Source<TB, BN, LB> sb(b, b0, wave, lane);
-        auto load = [&](int t, int stage) {
+        Source<TA, BM, LA> sa(a, a0, wave, lane);
+        Source<TB, BN, LB> sb(b, b0, wave, lane);
+        auto load = [&](int j, int stage) {               // load j of the step that sa and sb are at
             char *to = smem + stage * STAGE + wave * 1024;
-            sa.load(to, t, t1);
-            sb.load(to + BM * STEP, t, t1);
+            const int p = j / (LA + LB), i = j % (LA + LB);
+            if (i < LA)
+                sa.load(to, p, i);
+            else
+                sb.load(to + BM * STEP, p, i - LA);
         };
-        // Fragments are read while the products of the group before them run, across steps too: where the last group of a
-        // step is in registers, its stage is free for the loads of step t + STAGES, and the next step's first group is read beside its
-        // products.
         u32x4 af[2][PL][WM], bf[2][PL][WN];
-        auto fetch = [&](const char *stage, int g) {
-#pragma unroll
-            for (int p = 0; p < PL; ++p) {
-#pragma unroll
-                for (int m = 0; m < WM; ++m)
-                    af[g & 1][p][m] = fragment<TA, BM>(stage + p * PLANE, (wr * WM + m) * 32, g, lane);
-#pragma unroll
-                for (int n = 0; n < WN; ++n)
-                    bf[g & 1][p][n] = fragment<TB, BN>(stage + p * PLANE + BM * STEP, (wc * WN + n) * 32, g, lane);
-            }
+        auto fetch = [&](const char *stage, int g, int f) {      // fragment f of group g
+            const int p = f / (WM + WN), i = f % (WM + WN);
+            if (i < WM)
+                af[g & 1][p][i] = fragment<TA, BM>(stage + p * PLANE, (wr * WM + i) * 32, g, lane);
+            else
+                bf[g & 1][p][i - WM] = fragment<TB, BN>(stage + p * PLANE + BM * STEP, (wc * WN + i - WM) * 32, g, lane);
         };
-        auto products = [&](int g) {
+        // The products of group g.  Among them: the fragments of the next group (`next` of `ahead`), as early as two to a product, and loads
+        // j0 to j1 - 1 of a later step into stage `to`.  (Before the products they would hold the wave up: eight waves' loads take
+        // the unit 29 clocks a KiB, and more than 15 LDS reads on their way are waited for.)
+        auto products = [&](int g, const char *ahead, int next, int j0, int j1, int to) {
             // (three planes: small parts first)
-            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0};
+            constexpr int pa[6] = {0, 2, 1, 0, 1, 0}, pb[6] = {2, 0, 1, 1, 0, 0}, Q = PL == 1 ? 1 : 6, ALL = Q * WM * WN, ALL_F = PL * (WM + WN);
+            int j = j0, f = 0;
 #pragma unroll
-            for (int q = PL == 1 ? 5 : 0; q < 6; ++q)
+            for (int q = 6 - Q; q < 6; ++q)
 #pragma unroll
                 for (int m = 0; m < WM; ++m)
 #pragma unroll
                     for (int n = 0; n < WN; ++n) {
+                        const int k = ((q - 6 + Q) * WM + m) * WN + n;
                         const u32x4 x = af[g & 1][pa[q]][m], y = bf[g & 1][pb[q]][n];
                         if constexpr (PL == 1)
                             acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y),
@@ -195,52 +197,72 @@ template <int PL, int WR, int WC, int WM, int WN, int STAGES, bool TA = false, b
                         else
                             acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y),
                                                                                 acc[m][n], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int e = 0; e < (ALL_F + ALL - 1) / ALL + 1; ++e)
+                            if (f < ALL_F)
+                                fetch(ahead, next, f++);
+#pragma unroll
+                        for (int e = 0; e < LOADS; ++e)
+                            if (j < j1 && (k + 1) * (j1 - j0) >= (j - j0 + 1) * ALL)
+                                load(j++, to);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
         };
-        constexpr int GROUPS = R / 16;
-        static_assert(GROUPS % 2 == 0 && (STAGES - 1) * LOADS < 64);
+        // Fragments are read while the products of the group before them run, across steps too: where the last group of a step is in
+        // registers, the next step's loads have to have landed and the step's stage is free.  Three stages and more: a step
+        // issues the loads of the step STAGES - 1 later, a part with each group, into the stage that the step before has freed.  Two stages:
+        // its last group issues those of the step after the next, into its own.
+        constexpr int GROUPS = R / 16, AHEAD = STAGES > 2 ? STAGES - 1 : 2;
+        constexpr int EARLY = STAGES > 2 ? LOADS * (GROUPS - 1) / GROUPS : 0;          // of a step's loads, before its last group
+        constexpr int FLYING = STAGES > 2 ? (STAGES - 3) * LOADS + EARLY : 0;          // that need not have landed there
+        static_assert(GROUPS % 2 == 0 && STAGES > 1 && (AHEAD - 1) * LOADS < 64 && FLYING < 64);
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s)
-            load(t0 + s, s);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * LOADS) : "memory");
+        for (int s = 0; s < AHEAD; ++s) {
+            sa.step(t0 + s, t1);
+            sb.step(t0 + s, t1);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j)
+                load(j, s);
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        fetch(smem, 0);
+#pragma unroll
+        for (int f = 0; f < PL * (WM + WN); ++f)
+            fetch(smem, 0, f);
         int at = 0;
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
+            const int to = STAGES == 2 ? at : at == 0 ? STAGES - 1 : at - 1;
+            sa.step(t + AHEAD, t1);
+            sb.step(t + AHEAD, t1);
             const char *stage = smem + at * STAGE;
 #pragma unroll
-            for (int g = 0; g + 1 < GROUPS; ++g) {
-                fetch(stage, g + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                products(g);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int g = 0; g + 1 < GROUPS; ++g)
+                products(g, stage, g + 1, EARLY * g / (GROUPS - 1), EARLY * (g + 1) / (GROUPS - 1), to);
             // the next step's loads have landed, for every wave, and all have read this stage
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * LOADS) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLYING) : "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            load(t + STAGES, at);
             at = at + 1 == STAGES ? 0 : at + 1;
-            fetch(smem + at * STAGE, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            products(GROUPS - 1);
-            __builtin_amdgcn_sched_barrier(0);
+            products(GROUPS - 1, smem + at * STAGE, 0, EARLY, LOADS, to);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (results go where the last loads write)
         __syncthreads();
     }
 };
 
-// The tile of this workgroup: consecutive ones to one XCD.  False: none.
+// The tile of this workgroup: consecutive ones to one XCD, in the order of bands of four tiles of B and along A within a band, so that the 32
+// tiles that an XCD has at once read eight tiles of A and four of B into its L2, not 32 and one.  False: none.
 __device__ __forceinline__ bool tile_of(const Product &q, int &a_tile, int &b_tile)
 {
     const int tile = ((int)blockIdx.x & (kXcds - 1)) * q.tiles_per_xcd + ((int)blockIdx.x >> 3);
     if (((int)blockIdx.x >> 3) >= q.tiles_per_xcd || tile >= q.tiles)
         return false;
-    b_tile = fdiv(tile, q.div_a);
-    a_tile = tile - b_tile * q.a_tiles;
+    const int band = fdiv(tile, q.div_band), rest = tile - band * 4 * q.a_tiles, wide = min(4, q.b_tiles - band * 4);
+    a_tile = wide == 4 ? rest >> 2 : wide == 2 ? rest >> 1 : wide == 1 ? rest : fdiv(rest, q.div_3);
+    b_tile = band * 4 + rest - a_tile * wide;
     return true;
 }
 
@@ -298,10 +320,10 @@ __device__ __forceinline__ float sum_of_32(float v)        // over the lane's ha
 
 // Forward: per pixel and tile of classes the largest logit and the sum of the others' exponentials beside it: partial[a_tile][P];
 // the target's logit goes to target_logit[P] (one lane of the grid has it).
-template <typename T, int PL, int WR, int WC, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, STAGES>::kWavesPerSimd)) void dcnv4_loss_kernel(Product q, Labels l, float2 *partial, float *target_logit)
+template <typename T, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_loss_kernel(Product q, Labels l, float2 *partial, float *target_logit)
 {
-    typedef Tile<PL, WR, WC, WM, WN, STAGES> G;
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt;
     if (!tile_of(q, at, bt))
@@ -492,10 +514,10 @@ struct Deltas {
 };
 
 // Backward, first part: the logits of a tile again, and d out of them.
-template <typename T, int PL, int WR, int WC, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, STAGES>::kWavesPerSimd)) void dcnv4_loss_delta_kernel(Product q, Labels l, Deltas d)
+template <typename T, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_loss_delta_kernel(Product q, Labels l, Deltas d)
 {
-    typedef Tile<PL, WR, WC, WM, WN, STAGES> G;
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt;
     if (!tile_of(q, at, bt))
@@ -595,10 +617,10 @@ struct Result {
 
 // Backward, second part: out[j][i] = scale * sum_r A[i][r] * B[j][r], whole (T) or a split of the sum (float planes).
 // A turned, B turned in the product over pixels (grad_w).
-template <typename T, bool WHOLE, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, STAGES>::kWavesPerSimd)) void dcnv4_loss_product_kernel(Product q, Result o)
+template <typename T, bool WHOLE, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_loss_product_kernel(Product q, Result o)
 {
-    typedef Tile<PL, WR, WC, WM, WN, STAGES, true, PIXELS> G;
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
     typedef std::conditional_t<WHOLE, T, float> S;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt;
@@ -705,14 +727,14 @@ constexpr long long kMaxPiece = 1 << 20;                   // (256 rows of d, in
 constexpr long long kPieceWeights = 1ll << 27;
 
 struct Shape {
-    int bm, bn;
+    int bm, bn, r;                     // classes (or columns of a result), pixels (or its rows), numbers of a step
     float step, fixed, alone;          // us: a step of all tiles that a unit has at once, a tile's beginning and end, a lone tile's step
     int slots;                         // tiles of a unit side by side
 };
 inline const Shape &shape_of(int pl, int i)
 {
-    static const Shape f16[] = {{64, 64, .17f, 1.2f, .25f, 2}, {128, 128, .55f, 1.9f, .55f, 2}, {256, 256, 1.15f, 8.6f, 1.15f, 1}};
-    static const Shape f32[] = {{64, 64, .45f, 1.2f, .55f, 2}, {128, 128, .85f, 2.5f, .85f, 1}, {256, 128, 1.5f, 5.f, 1.5f, 1}};
+    static const Shape f16[] = {{64, 64, 64, .17f, 1.2f, .25f, 2}, {128, 128, 32, .28f, 1.9f, .28f, 2}, {256, 256, 32, .58f, 8.6f, .58f, 1}};
+    static const Shape f32[] = {{64, 64, 32, .45f, 1.2f, .55f, 2}, {128, 128, 32, .85f, 2.5f, .85f, 1}, {256, 128, 32, 1.5f, 5.f, 1.5f, 1}};
     return (pl == 1 ? f16 : f32)[i];
 }
 
@@ -728,7 +750,7 @@ struct Choice {
 };
 
 // The tile, and over how many workgroups a sum is split, with the lowest estimated time.
-Choice choose_product(int pl, long long m, long long n, int steps, bool may_split)
+Choice choose_product(int pl, long long m, long long n, int length, bool may_split)
 {
     Choice best = {-1, 1};
     float best_us = 0.f;
@@ -736,6 +758,7 @@ Choice choose_product(int pl, long long m, long long n, int steps, bool may_spli
         if (g_loss.tile && g_loss.tile != 1 + i)
             continue;
         const Shape &s = shape_of(pl, i);
+        const int steps = (length + s.r - 1) / s.r;
         const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
         for (int splits = 1; splits == 1 || (may_split && splits <= 64 && steps / splits >= 4); splits *= 2) {
             const float full = ceilf((float)(tiles * splits) / (float)kUnits);
@@ -750,14 +773,13 @@ Choice choose_product(int pl, long long m, long long n, int steps, bool may_spli
         }
     }
     if (may_split && g_loss.splits)
-        best.splits = g_loss.splits < steps ? g_loss.splits : steps;
+        best.splits = g_loss.splits;
     return best;
 }
 
 struct Plan {
     int pl, es, K, P, V;
     int kp, vc, vp, pieces;            // padded K (split operands), classes of a piece and padded, pieces
-    int k_steps, v_steps, p_steps;
     Choice logits, gx, gw;
     bool gx_planes, gw_planes;
     // bytes from the start of the workspace
@@ -793,11 +815,7 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
     p.vc = p.vc < V ? p.vc : V;
     p.pieces = (V + p.vc - 1) / p.vc;
     p.vp = (int)round_up(p.vc, 64);
-    const int step = p.pl == 1 ? 64 : 32;                  // numbers of a step
-    p.k_steps = (p.kp + step - 1) / step;
-    p.v_steps = p.vp / step;
-    p.p_steps = (int)((P + step - 1) / step);
-    p.logits = choose_product(p.pl, p.vc, P, p.k_steps, false);
+    p.logits = choose_product(p.pl, p.vc, P, p.kp, false);
     long long at = 0;
     auto take = [&](long long bytes) {
         const long long here = at;
@@ -814,8 +832,8 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
         p.partial = take(tiles * P * 8);
         p.hit = take(P * 4);
     } else {
-        p.gx = choose_product(p.pl, K, P, p.v_steps, true);
-        p.gw = choose_product(p.pl, K, p.vc, p.p_steps, true);
+        p.gx = choose_product(p.pl, K, P, p.vp, true);
+        p.gw = choose_product(p.pl, K, p.vc, p.P, true);
         p.gx_planes = p.gx.splits > 1 || p.pieces > 1;
         p.gw_planes = p.gw.splits > 1;
         p.scale = take(4);
@@ -841,35 +859,37 @@ Operand rows_of(const void *base, int rows, int cols, int pl, int pad)
 }
 Operand turned(const Operand &o) { return {o.base, o.row_bytes, o.length, o.count, o.plane_bytes}; }
 
-Product product_of(const Operand &a, const Operand &b, int pl, const Choice &c, int steps)
+Product product_of(const Operand &a, const Operand &b, int pl, const Choice &c)
 {
     const Shape &s = shape_of(pl, c.shape);
     Product q;
     q.a = a;
     q.b = b;
-    q.steps = steps;
-    q.steps_per_split = (steps + c.splits - 1) / c.splits;
+    q.steps = (b.length + s.r - 1) / s.r;
+    q.steps_per_split = (q.steps + c.splits - 1) / c.splits;
     q.a_tiles = (a.count + s.bm - 1) / s.bm;
-    q.tiles = q.a_tiles * ((b.count + s.bn - 1) / s.bn);
+    q.b_tiles = (b.count + s.bn - 1) / s.bn;
+    q.tiles = q.a_tiles * q.b_tiles;
     q.tiles_per_xcd = (q.tiles + kXcds - 1) / kXcds;
-    q.div_a = make_div((unsigned)q.a_tiles);
+    q.div_band = make_div(4u * (unsigned)q.a_tiles);
+    q.div_3 = make_div(3);
     return q;
 }
 
 // Calls f with the tile's parameters (waves, blocks of a wave, stages) as constants.
-template <int A, int B, int C, int D, int E> struct TileOf {
-    static constexpr int WR = A, WC = B, WM = C, WN = D, STAGES = E;
+template <int A, int B, int C, int D, int E, int F> struct TileOf {
+    static constexpr int WR = A, WC = B, WM = C, WN = D, R = E, STAGES = F;
 };
 template <int PL, typename F> int with_tile(int shape, F &&f)
 {
     if constexpr (PL == 1) {
-        if (shape == kLarge) return f(TileOf<4, 2, 2, 4, 2>());
-        if (shape == kMiddle) return f(TileOf<2, 2, 2, 2, 2>());
-        return f(TileOf<2, 2, 1, 1, 4>());
+        if (shape == kLarge) return f(TileOf<4, 2, 2, 4, 32, 4>());
+        if (shape == kMiddle) return f(TileOf<2, 2, 2, 2, 32, 4>());
+        return f(TileOf<2, 2, 1, 1, 64, 4>());
     } else {
-        if (shape == kLarge) return f(TileOf<4, 2, 2, 2, 2>());
-        if (shape == kMiddle) return f(TileOf<2, 2, 2, 2, 3>());
-        return f(TileOf<2, 2, 1, 1, 3>());
+        if (shape == kLarge) return f(TileOf<4, 2, 2, 2, 32, 2>());
+        if (shape == kMiddle) return f(TileOf<2, 2, 2, 2, 32, 3>());
+        return f(TileOf<2, 2, 1, 1, 32, 3>());
     }
 }
 
@@ -897,10 +917,10 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
         const char *rows = (const char *)w + (long long)l.v0 * p.K * p.es;
         if (PL == 3)
             split_rows(rows, l.count, p.K, p.kp, ws + p.w_split, s);
-        const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, PL, p.logits, p.k_steps);
+        const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, PL, p.logits);
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
-            hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
+            hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
                                dim3(G::WR * G::WC * 64), 0, s, q, l, (float2 *)(ws + p.partial) + (long long)tiles * p.P, (float *)(ws + p.hit));
             return 0;
         });
@@ -918,9 +938,9 @@ void launch_product(const Product &q, const Choice &c, bool planes, const Result
         typedef decltype(t) G;
         const dim3 grid((unsigned)(q.tiles_per_xcd * kXcds), (unsigned)c.splits), block(G::WR * G::WC * 64);
         if (planes)
-            hipLaunchKernelGGL((dcnv4_loss_product_kernel<T, false, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::STAGES>), grid, block, 0, s, q, o);
+            hipLaunchKernelGGL((dcnv4_loss_product_kernel<T, false, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
         else
-            hipLaunchKernelGGL((dcnv4_loss_product_kernel<T, true, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::STAGES>), grid, block, 0, s, q, o);
+            hipLaunchKernelGGL((dcnv4_loss_product_kernel<T, true, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
         return 0;
     });
 }
@@ -951,18 +971,18 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         l.v0 = piece * p.vc;
         l.count = p.V - l.v0 < p.vc ? p.V - l.v0 : p.vc;
         const char *rows = (const char *)w + (long long)l.v0 * p.K * p.es;
-        const int vp = (int)round_up(l.count, 64), v_steps = vp / (PL == 1 ? 64 : 32);      // (nothing behind them is written or read)
+        const int vp = (int)round_up(l.count, 64);         // (nothing behind them is written or read)
         if (PL == 3)
             split_rows(rows, l.count, p.K, p.kp, ws + p.w_split, s);
         const void *wrows = PL == 3 ? (const void *)(ws + p.w_split) : rows;
         // d
         const Deltas d = {lse, g, (unsigned short *)(ws + p.d), grad_b != nullptr ? (float *)(ws + p.bias_sums) : nullptr, vp};
-        const Product q = product_of(rows_of(wrows, l.count, p.kp, PL, p.kp), xo, PL, p.logits, p.k_steps);
+        const Product q = product_of(rows_of(wrows, l.count, p.kp, PL, p.kp), xo, PL, p.logits);
         int runs = 0;
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
-            runs = q.tiles / q.a_tiles * G::WC;
-            hipLaunchKernelGGL((dcnv4_loss_delta_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
+            runs = q.b_tiles * G::WC;
+            hipLaunchKernelGGL((dcnv4_loss_delta_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
                                dim3(G::WR * G::WC * 64), 0, s, q, l, d);
             return 0;
         });
@@ -971,7 +991,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
                                l.count, (T *)grad_b + l.v0);
         // grad_x, over the pieces
         const Result ox = {grad_x, 0, g, nullptr, down, 0};
-        const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), PL, p.gx, v_steps);
+        const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), PL, p.gx);
         if (p.gx_planes) {
             const Result o = {ws + p.gx_at, (long long)p.P * p.K, nullptr, nullptr, 1.f, piece > 0};
             launch_product<T, PL, false>(qx, p.gx, true, o, s);
@@ -982,7 +1002,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         }
         // grad_w of the piece
         const Result ow = {(char *)grad_w + (long long)l.v0 * p.K * p.es, 0, nullptr, scale, down, 0};
-        const Product qw = product_of(xg, turned(rows_of(d.d, p.P, l.count, PL, vp)), PL, p.gw, p.p_steps);
+        const Product qw = product_of(xg, turned(rows_of(d.d, p.P, l.count, PL, vp)), PL, p.gw);
         if (p.gw_planes) {
             const Result o = {ws + p.gw_at, (long long)l.count * p.K, nullptr, nullptr, 1.f, 0};
             launch_product<T, PL, true>(qw, p.gw, true, o, s);
