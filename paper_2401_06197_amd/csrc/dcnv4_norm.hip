@@ -3,7 +3,9 @@
 //
 // All of it is bound by memory: a kernel reads each input once, keeps a row in registers while its statistics are made, and
 // writes each output once.  A lane holds runs of eight channels (16 bytes in fp16, 32 in fp32).  A row belongs to L lanes: as
-// few of a wave as its runs need, whole waves for wide rows.
+// few of a wave as its runs need, whole waves for wide rows.  A workgroup stays for many rows and asks for the next ones before it
+// deals with the present ones: a wave's loads alone, some KiB, do not cover the memory's latency (50176 x 256 fp16 norm forward
+// 4.3 -> 5.4 TB/s, backward 3.1 -> 4.6).
 #include <math.h>
 
 #include <initializer_list>
@@ -55,95 +57,84 @@ __device__ __forceinline__ Bits8 philox(unsigned long long block, unsigned long 
     return {{c0, c1, c2, c3}};
 }
 
-// The bits of eight elements from element i on.  WHOLE: i is a multiple of eight.
-template <bool WHOLE>
-__device__ __forceinline__ Bits8 drop_bits(unsigned long long i, unsigned long long offset, unsigned long long seed)
+// The decisions of a block's eight elements, a bit each: set where the element goes.
+__device__ __forceinline__ unsigned gone_of(const Bits8 &b, const Drop &d)
 {
-    const Bits8 lo = philox(i >> 3, offset, seed);
-    if constexpr (WHOLE)
-        return lo;
-    const Bits8 hi = philox((i >> 3) + 1, offset, seed);
-    const unsigned words = (unsigned)(i >> 1) & 3u, half = ((unsigned)i & 1u) * 16u;
-    unsigned c[8], s[5];
+    unsigned m = 0u;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        c[k] = lo.w[k];
-        c[4 + k] = hi.w[k];
-    }
-#pragma unroll
-    for (int k = 0; k < 5; ++k) {                          // (word k + words: at most 7)
-        const unsigned even = words & 2u ? c[k + 2] : c[k], odd = words & 2u ? c[k + 3] : c[k + 1];
-        s[k] = words & 1u ? odd : even;
-    }
-    Bits8 out;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        out.w[k] = __builtin_amdgcn_alignbit(s[k + 1], s[k], half);
-    return out;
+    for (int e = 0; e < 8; ++e)
+        m |= ((b.w[e / 2] >> (16 * (e & 1))) & 0xffffu) < d.limit ? 1u << e : 0u;
+    return m;
 }
 
-// Element e of the eight: r + v scaled, or r alone whatever v is.
-__device__ __forceinline__ float drop_apply(const Bits8 &b, int e, const Drop &d, float v, float r)
+// Element e of the eight: r + v scaled, or r alone whatever v is.  WHOLE: by the block's bits; else by decisions (in w[0]).
+template <bool WHOLE> __device__ __forceinline__ float drop_apply(const Bits8 &b, int e, const Drop &d, float v, float r)
 {
-    const unsigned half = (b.w[e / 2] >> (16 * (e & 1))) & 0xffffu;
-    return half < d.limit ? r : __builtin_fmaf(v, d.scale, r);
+    const bool gone = WHOLE ? ((b.w[e / 2] >> (16 * (e & 1))) & 0xffffu) < d.limit : (b.w[0] >> e & 1u) != 0u;
+    float sum = __builtin_fmaf(v, d.scale, r);
+    asm("" : "+v"(sum));                                   // (an fp32 number here: not one instruction with a store's rounding)
+    return gone ? r : sum;
 }
 
 // ------------------------------------------------------------------------------------------
 // Runs of eight channels.  WHOLE: C is a multiple of eight, so that every run is whole and aligned; otherwise rows start at any
 // element (memory instructions of 16 bytes take any address), and the last run of a row may be short.
 // ------------------------------------------------------------------------------------------
-template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Run8 {
-    T e[8];
+template <typename T> struct Run {                         // as they lie in memory, aligned to 16 bytes or to an element
+    typedef T type __attribute__((ext_vector_type(8)));
+    typedef type aligned __attribute__((aligned(16)));
+    typedef type any __attribute__((aligned(sizeof(T))));
 };
+template <typename T> using Raw8 = typename Run<T>::type;
 
-template <typename T, bool WHOLE> __device__ __forceinline__ void load8(const T *p, int n, bool past, float (&v)[8])
+template <typename T, bool WHOLE> __device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool past)
 {
     // n channels of the row; `past`: eight would reach past the end of the tensor
-    if (n <= 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = 0.f;
-    } else if (WHOLE) {
-        const T *q = (const T *)__builtin_assume_aligned(p, 16);
-        T t[8];
-        __builtin_memcpy(t, q, sizeof(t));
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = (float)t[e];
-    } else if (n >= 8 || !past) {
-        const Run8<T> t = *reinterpret_cast<const Run8<T> *>(p);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = e < n ? (float)t.e[e] : 0.f;
+    Raw8<T> r = {};
+    if (WHOLE) {
+        if (n > 0)
+            r = *reinterpret_cast<const typename Run<T>::aligned *>(p);
+    } else if (n >= 8 || (n > 0 && !past)) {
+        r = *reinterpret_cast<const typename Run<T>::any *>(p);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = e < n ? (float)p[e] : 0.f;
+        for (int e = 0; e < 7; ++e)
+            if (e < n)
+                r[e] = p[e];
     }
+    return r;
+}
+// As fp32, zeros behind the n.
+template <typename T, bool WHOLE> __device__ __forceinline__ void unpack(const Raw8<T> &r, int n, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = (WHOLE ? n > 0 : e < n) ? (float)r[e] : 0.f;
 }
 
 template <typename T, bool WHOLE> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
 {
     if (n <= 0)
         return;
-    T t[8];
+    Raw8<T> t;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         t[e] = (T)v[e];                                    // one rounding to nearest even
     if (WHOLE) {
-        __builtin_memcpy(__builtin_assume_aligned(p, 16), t, sizeof(t));
+        *reinterpret_cast<typename Run<T>::aligned *>(p) = t;
     } else if (n >= 8) {
-        Run8<T> r;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            r.e[e] = t[e];
-        *reinterpret_cast<Run8<T> *>(p) = r;
+        *reinterpret_cast<typename Run<T>::any *>(p) = t;
     } else {
-#pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < n)
-                p[e] = t[e];
+        typedef T four __attribute__((ext_vector_type(4)));
+        typedef T two __attribute__((ext_vector_type(2)));
+        typedef four any_four __attribute__((aligned(sizeof(T))));
+        typedef two any_two __attribute__((aligned(sizeof(T))));
+        if (n & 4)
+            *reinterpret_cast<any_four *>(p) = four{t[0], t[1], t[2], t[3]};
+        if (n & 2)
+            *reinterpret_cast<any_two *>(p + (n & 4)) = n & 4 ? two{t[4], t[5]} : two{t[0], t[1]};
+        if (n & 1)
+            p[n - 1] = n == 1 ? t[0] : n == 3 ? t[2] : n == 5 ? t[4] : t[6];
     }
 }
 
@@ -169,10 +160,13 @@ __device__ __forceinline__ float add_halves(float v)       // the other half of 
 }
 template <int L> __device__ __forceinline__ float wave_sum(float v)
 {
-    static_assert(L >= 8 && L <= 64);
-    v += dpp<0xB1>(v);                                     // quad_perm [1,0,3,2]
-    v += dpp<0x4E>(v);                                     // quad_perm [2,3,0,1]
-    v += dpp<0x141>(v);                                    // row_half_mirror
+    static_assert(L >= 1 && L <= 64);
+    if constexpr (L >= 2)
+        v += dpp<0xB1>(v);                                 // quad_perm [1,0,3,2]
+    if constexpr (L >= 4)
+        v += dpp<0x4E>(v);                                 // quad_perm [2,3,0,1]
+    if constexpr (L >= 8)
+        v += dpp<0x141>(v);                                // row_half_mirror
     if constexpr (L >= 16)
         v += dpp<0x140>(v);                                // row_mirror
     if constexpr (L >= 32)
@@ -206,6 +200,43 @@ template <int L, int N> __device__ __forceinline__ void row_sums(float (&v)[N], 
 }
 
 constexpr int norm_threads(int L) { return L > 256 ? L : 256; }
+
+// Where a lane's run j lies in its row, in runs: side by side in a wave, then run after run, then the next wave's.
+template <int L, int NV> __device__ __forceinline__ int run_of(int l, int j)
+{
+    constexpr int G = L < 64 ? L : 64;
+    return (l / G * NV + j) * G + l % G;
+}
+
+// What drop_apply takes for a lane's runs, `first` being the first element of the row.  Rows that start inside a block share each block
+// between two neighbouring runs: a lane makes one block's decisions and takes those of the second from the next lane (the
+// last lane of a wave makes its last ones itself).  Both blocks made by each lane: fp16 branch ends of 52265 x 321 72 us, 41 so.
+template <int L, int NV, bool WHOLE>
+__device__ __forceinline__ void row_bits(Bits8 (&b)[NV], unsigned long long first, int C, int l, unsigned long long offset, const Drop &d)
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        b[j] = philox((first >> 3) + (unsigned)run_of<L, NV>(l, j), offset, d.seed);
+    if constexpr (!WHOLE) {
+        constexpr int G = L < 64 ? L : 64;
+        const unsigned skip = (unsigned)first & 7u;
+        const bool last = l % G == G - 1;
+        unsigned end = 0u, mine[NV], beside[NV];
+        if (last && run_of<L, NV>(l, NV - 1) * 8 < C)
+            end = gone_of(philox((first >> 3) + (unsigned)run_of<L, NV>(l, NV - 1) + 1u, offset, d.seed), d);
+        const int next = ((int)(threadIdx.x & 63) / G * G + (l + 1) % G) * 4;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            mine[j] = gone_of(b[j], d);
+            beside[j] = (unsigned)__builtin_amdgcn_ds_bpermute(next, (int)mine[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const unsigned second = last ? (j + 1 < NV ? beside[j + 1 < NV ? j + 1 : j] : end) : beside[j];
+            b[j].w[0] = (mine[j] | second << 8) >> skip;
+        }
+    }
+}
 
 struct NormArgs {
     const void *x, *residual, *gamma, *beta;   // gamma, beta: null for ones and zeros
@@ -241,40 +272,73 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_kernel(NormArgs a)
     const int l = (int)threadIdx.x % L;
     const T *gamma = (const T *)a.gamma, *beta = (const T *)a.beta;
     const unsigned long long offset = BRANCH ? drop_offset(a.drop) : 0ull;
-    const long long all = a.P * a.C;
-    for (long long row = (long long)blockIdx.x * R + (int)threadIdx.x / L; row < a.P; row += (long long)gridDim.x * R) {
-        const long long at = row * a.C;
-        float v[NV][8], s[1] = {0.f};
+    const long long all = a.P * a.C, stride = (long long)gridDim.x * R;
+    Raw8<T> x[NV], res[BRANCH ? NV : 1], gm[NV], bt[NV];
+    auto load = [&](long long row) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * L + l) * 8, n = a.C - c;
-            load8<T, WHOLE>((const T *)a.x + at + c, n, all - at - c < 8, v[j]);
-            if constexpr (BRANCH) {
-                float r[8];
-                load8<T, WHOLE>((const T *)a.residual + at + c, n, all - at - c < 8, r);
-                if (n > 0) {
-                    const Bits8 b = drop_bits<WHOLE>((unsigned long long)(at + c), offset, a.drop.seed);
+            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            const long long at = row * a.C + c;
+            x[j] = load8<T, WHOLE>((const T *)a.x + at, n, all - at < 8);
+            if constexpr (BRANCH)
+                res[j] = load8<T, WHOLE>((const T *)a.residual + at, n, all - at < 8);
+        }
+    };
+    constexpr bool AHEAD = NV <= 2;                        // (four runs a lane: no registers for two rows)
+    long long row = (long long)blockIdx.x * R + (int)threadIdx.x / L;
+    if (AHEAD && row < a.P)
+        load(row);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[j][e] = WHOLE || e < n ? (float)(T)drop_apply(b, e, a.drop, v[j][e], r[e]) : 0.f;
-                    store8<T, WHOLE>((T *)a.z + at + c, n, v[j]);
-                }
+    for (int j = 0; j < NV; ++j) {
+        const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+        if (gamma != nullptr)
+            gm[j] = load8<T, WHOLE>(gamma + c, n, n < 8);
+        if (beta != nullptr)
+            bt[j] = load8<T, WHOLE>(beta + c, n, n < 8);
+    }
+    for (; row < a.P; row += stride) {
+        const long long at = row * a.C;
+        if (!AHEAD)
+            load(row);
+        float v[NV][8], s[1] = {0.f};
+        Bits8 bits[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            unpack<T, WHOLE>(x[j], a.C - run_of<L, NV>(l, j) * 8, v[j]);
+        float r[BRANCH ? NV : 1][8];
+        if constexpr (BRANCH)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                unpack<T, WHOLE>(res[j], a.C - run_of<L, NV>(l, j) * 8, r[j]);
+        if (AHEAD && row + stride < a.P)
+            load(row + stride);
+        if constexpr (BRANCH) {
+            row_bits<L, NV, WHOLE>(bits, (unsigned long long)at, a.C, l, offset, a.drop);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[j][e] = (WHOLE ? n > 0 : e < n) ? (float)(T)drop_apply<WHOLE>(bits[j], e, a.drop, v[j][e], r[j][e]) : 0.f;
+                store8<T, WHOLE>((T *)a.z + at + c, n, v[j]);
             }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 s[0] += v[j][e];
-        }
         row_sums<L, 1>(s, lds);
         const float mean = s[0] / (float)a.C;              // (divided: the mean of equal numbers that add up exactly is that number)
         s[0] = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int n = a.C - (j * L + l) * 8;
+            const int n = a.C - run_of<L, NV>(l, j) * 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = v[j][e] - mean;
+                v[j][e] -= mean;
                 if (WHOLE ? n > 0 : e < n)
-                    s[0] = __builtin_fmaf(d, d, s[0]);
+                    s[0] = __builtin_fmaf(v[j][e], v[j][e], s[0]);
             }
         }
         row_sums<L, 1>(s, lds);
@@ -287,21 +351,17 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_kernel(NormArgs a)
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * L + l) * 8, n = a.C - c;
-            float g[8], b[8], y[8];
-            if (gamma != nullptr)
-                load8<T, WHOLE>(gamma + c, n, true, g);
-            if (beta != nullptr)
-                load8<T, WHOLE>(beta + c, n, true, b);
+            const int c = run_of<L, NV>(l, j) * 8;
+            float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                y[e] = (v[j][e] - mean) * rstd;
+                y[e] = v[j][e] * rstd;
                 if (gamma != nullptr)
-                    y[e] = beta != nullptr ? __builtin_fmaf(y[e], g[e], b[e]) : y[e] * g[e];
+                    y[e] = beta != nullptr ? __builtin_fmaf(y[e], (float)gm[j][e], (float)bt[j][e]) : y[e] * (float)gm[j][e];
                 else if (beta != nullptr)
-                    y[e] += b[e];
+                    y[e] += (float)bt[j][e];
             }
-            store8<T, WHOLE>((T *)a.y + at + c, n, y);
+            store8<T, WHOLE>((T *)a.y + at + c, a.C - c, y);
         }
     }
 }
@@ -327,56 +387,103 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             dg[j][e] = db[j][e] = 0.f;
-    const long long all = a.P * a.C;
-    for (long long row = (long long)blockIdx.x * R + first; row < a.P; row += (long long)gridDim.x * R) {
-        const long long at = row * a.C;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float xh[NV][8], g[NV][8], s[2] = {0.f, 0.f};
+    const long long all = a.P * a.C, stride = (long long)gridDim.x * R;
+    constexpr bool AHEAD = NV <= 2;                        // (four runs a lane: no registers for two rows, gamma and grad_z)
+    Raw8<T> x[NV], gy[NV], gz[BRANCH && AHEAD ? NV : 1], gm[AHEAD ? NV : 1];
+    float mean = 0.f, rstd = 0.f;
+    auto load = [&](long long row) {
+        mean = a.mean[row];
+        rstd = a.rstd[row];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * L + l) * 8, n = a.C - c;
-            load8<T, WHOLE>((const T *)a.x + at + c, n, all - at - c < 8, xh[j]);
-            load8<T, WHOLE>((const T *)a.grad_y + at + c, n, all - at - c < 8, g[j]);
-            float gm[8];
-            if (gamma != nullptr)
-                load8<T, WHOLE>(gamma + c, n, true, gm);
+            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            const long long at = row * a.C + c;
+            x[j] = load8<T, WHOLE>((const T *)a.x + at, n, all - at < 8);
+            gy[j] = load8<T, WHOLE>((const T *)a.grad_y + at, n, all - at < 8);
+            if constexpr (BRANCH && AHEAD)
+                if (a.grad_z != nullptr)
+                    gz[j] = load8<T, WHOLE>((const T *)a.grad_z + at, n, all - at < 8);
+        }
+    };
+    long long row = (long long)blockIdx.x * R + first;
+    if (AHEAD && row < a.P)
+        load(row);
+    if (AHEAD && gamma != nullptr)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            gm[AHEAD ? j : 0] = load8<T, WHOLE>(gamma + c, n, n < 8);
+        }
+    for (; row < a.P; row += stride) {
+        const long long at = row * a.C;
+        if constexpr (!AHEAD) {
+            load(row);
+            asm volatile("" : "+s"(a.C));                  // (what follows from C is worked out again: kept, it would fill the registers)
+        }
+        const float scale = rstd;
+        float xh[NV][8], g[NV][8], r[BRANCH && AHEAD ? NV : 1][8], s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            unpack<T, WHOLE>(x[j], n, xh[j]);
+            unpack<T, WHOLE>(gy[j], n, g[j]);
+            if constexpr (BRANCH && AHEAD) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    r[j][e] = 0.f;
+                if (a.grad_z != nullptr)
+                    unpack<T, WHOLE>(gz[j], n, r[j]);
+            }
+            if (!AHEAD && gamma != nullptr)
+                gm[0] = load8<T, WHOLE>(gamma + c, n, n < 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 xh[j][e] = (WHOLE ? n > 0 : e < n) ? (xh[j][e] - mean) * rstd : 0.f;
                 dg[j][e] = __builtin_fmaf(g[j][e], xh[j][e], dg[j][e]);
                 db[j][e] += g[j][e];
                 if (gamma != nullptr)
-                    g[j][e] *= gm[e];
+                    g[j][e] = (WHOLE ? n > 0 : e < n) ? g[j][e] * (float)gm[AHEAD ? j : 0][e] : 0.f;
                 s[0] += g[j][e];
                 s[1] = __builtin_fmaf(g[j][e], xh[j][e], s[1]);
             }
         }
+        if (AHEAD && row + stride < a.P)
+            load(row + stride);
         row_sums<L, 2>(s, lds);
         const float m0 = s[0] * a.inv_c, m1 = s[1] * a.inv_c;
+        Bits8 bits[BRANCH && AHEAD ? NV : 1];
+        if constexpr (BRANCH && AHEAD)
+            row_bits<L, NV, WHOLE>(bits, (unsigned long long)at, a.C, l, offset, a.drop);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * L + l) * 8, n = a.C - c;
+            if constexpr (!AHEAD)
+                __builtin_amdgcn_sched_barrier(0);         // (one run after the other)
+            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
             float out[8];
+            if constexpr (BRANCH && !AHEAD) {
+                const unsigned long long i = (unsigned long long)(at + c);
+                bits[0] = philox(i >> 3, offset, a.drop.seed);
+                if constexpr (!WHOLE)
+                    bits[0].w[0] = (gone_of(bits[0], a.drop) | gone_of(philox((i >> 3) + 1, offset, a.drop.seed), a.drop) << 8) >> ((unsigned)i & 7u);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    r[0][e] = 0.f;
+                if (a.grad_z != nullptr)
+                    unpack<T, WHOLE>(load8<T, WHOLE>((const T *)a.grad_z + at + c, n, all - at - c < 8), n, r[0]);
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                out[e] = rstd * __builtin_fmaf(-xh[j][e], m1, g[j][e] - m0);
-                asm("" : "+v"(out[e]));                    // (an fp32 number here: not one instruction with the store's rounding)
+                out[e] = scale * __builtin_fmaf(-xh[j][e], m1, g[j][e] - m0);
+                asm("" : "+v"(out[e]));                    // (as in drop_apply)
             }
             if constexpr (BRANCH) {
-                if (a.grad_z != nullptr) {
-                    float r[8];
-                    load8<T, WHOLE>((const T *)a.grad_z + at + c, n, all - at - c < 8, r);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        out[e] += r[e];
-                }
+                for (int e = 0; e < 8; ++e)
+                    out[e] += r[AHEAD ? j : 0][e];
                 store8<T, WHOLE>((T *)a.grad_residual + at + c, n, out);
-                if (n > 0) {
-                    const Bits8 b = drop_bits<WHOLE>((unsigned long long)(at + c), offset, a.drop.seed);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        out[e] = drop_apply(b, e, a.drop, out[e], 0.f);
-                }
+                for (int e = 0; e < 8; ++e)
+                    out[e] = drop_apply<WHOLE>(bits[AHEAD ? j : 0], e, a.drop, out[e], 0.f);
             }
             store8<T, WHOLE>((T *)a.grad_x + at + c, n, out);
         }
@@ -388,23 +495,35 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * L + l) * 8;
+            const int c = run_of<L, NV>(l, j) * 8;
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 v[e] = k == 0 ? dg[j][e] : db[j][e];
             if constexpr (R > 1) {
-                __syncthreads();                           // all have read what was there before
+                // rows side by side in a wave first: lanes 8, 4, 2, 1 further round (of 16), then rows of 16 and halves
+                constexpr int G = L < 64 ? L : 64, W = norm_threads(L) / 64;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sums[(first * 8 + e) * L + l] = v[e];
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (G < 16) v[e] += dpp<0x128>(v[e]);
+                    if constexpr (G < 8) v[e] += dpp<0x124>(v[e]);
+                    if constexpr (G < 4) v[e] += dpp<0x122>(v[e]);
+                    if constexpr (G < 2) v[e] += dpp<0x121>(v[e]);
+                    if constexpr (G < 32) v[e] = add_rows(v[e]);
+                    if constexpr (G < 64) v[e] = add_halves(v[e]);
+                }
+                __syncthreads();                           // all have read what was there before
+                if ((int)(threadIdx.x & 63) < G)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sums[((int)(threadIdx.x >> 6) * 8 + e) * G + l] = v[e];
                 __syncthreads();
                 if (first == 0)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-#pragma unroll 4
-                        for (int r = 1; r < R; ++r)
-                            v[e] += sums[(r * 8 + e) * L + l];
+#pragma unroll
+                        for (int w = 1; w < W; ++w)
+                            v[e] += sums[(w * 8 + e) * G + l];
             }
             if (first == 0)
 #pragma unroll
@@ -415,23 +534,25 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
     }
 }
 
-// Adds up partial sums [count][2 * C]: 16 columns to a workgroup, 64 of the rows side by side, joined through LDS.
+// Adds up partial sums [count][2 * C]: 16 columns to a workgroup, 64 of the rows side by side.
 template <typename T>
 __global__ __launch_bounds__(1024) void dcnv4_norm_join_kernel(const float *__restrict__ partial, int count, int C, T *grad_gamma, T *grad_beta)
 {
-    __shared__ float sums[64][17];
+    __shared__ float sums[16][16];
     const int col = (int)blockIdx.x * 16 + ((int)threadIdx.x & 15), slice = (int)threadIdx.x >> 4;
     float s = 0.f;
     if (col < 2 * C)
 #pragma unroll 8
         for (int r = slice; r < count; r += 64)
             s += partial[(long long)r * 2 * C + col];
-    sums[slice][threadIdx.x & 15] = s;
+    s = add_halves(add_rows(s));
+    if ((threadIdx.x & 63) < 16)
+        sums[threadIdx.x >> 6][threadIdx.x & 15] = s;
     __syncthreads();
     if (threadIdx.x < 16 && col < 2 * C) {
         s = 0.f;
-#pragma unroll 8
-        for (int r = 0; r < 64; ++r)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
             s += sums[r][threadIdx.x];
         T *to = col < C ? grad_gamma : grad_beta;
         if (to != nullptr)
@@ -439,32 +560,43 @@ __global__ __launch_bounds__(1024) void dcnv4_norm_join_kernel(const float *__re
     }
 }
 
-// out = [residual +] dropout(x), eight elements a lane.
+// out = [residual +] dropout(x): eight elements of each of two stretches a lane, whose loads go out together.
 template <typename T, bool ADD>
 __global__ __launch_bounds__(256) void dcnv4_dropout_kernel(const T *__restrict__ x, const T *__restrict__ residual, T *__restrict__ y, long long n,
                                                             Drop d)
 {
     const unsigned long long offset = drop_offset(d);
-    for (long long i = ((long long)blockIdx.x * 256 + (int)threadIdx.x) * 8; i < n; i += (long long)gridDim.x * 2048) {
-        float v[8], r[8];
-        const int left = (int)(n - i < 8 ? n - i : 8);
-        if (left == 8) {
-            load8<T, true>(x + i, 8, false, v);
-            if (ADD)
-                load8<T, true>(residual + i, 8, false, r);
-        } else {
-            load8<T, false>(x + i, left, true, v);
-            if (ADD)
-                load8<T, false>(residual + i, left, true, r);
-        }
-        const Bits8 b = drop_bits<true>((unsigned long long)i, offset, d.seed);
+    const long long half = (long long)gridDim.x * 2048;
+    for (long long i0 = ((long long)blockIdx.x * 256 + (int)threadIdx.x) * 8; i0 < n; i0 += 2 * half) {
+        Raw8<T> v[2], r[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = drop_apply(b, e, d, v[e], ADD ? r[e] : 0.f);
-        if (left == 8)
-            store8<T, true>(y + i, 8, v);
-        else
-            store8<T, false>(y + i, left, v);
+        for (int k = 0; k < 2; ++k) {
+            const long long i = i0 + k * half, left = n - i;
+            if (left >= 8) {
+                v[k] = load8<T, true>(x + i, 8, false);
+                if (ADD)
+                    r[k] = load8<T, true>(residual + i, 8, false);
+            } else if (left > 0) {
+                v[k] = load8<T, false>(x + i, (int)left, true);
+                if (ADD)
+                    r[k] = load8<T, false>(residual + i, (int)left, true);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const long long i = i0 + k * half, left = n - i;
+            if (left <= 0)
+                continue;
+            const Bits8 b = philox((unsigned long long)i >> 3, offset, d.seed);
+            float out[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                out[e] = drop_apply<true>(b, e, d, (float)v[k][e], ADD ? (float)r[k][e] : 0.f);
+            if (left >= 8)
+                store8<T, true>(y + i, 8, out);
+            else
+                store8<T, false>(y + i, (int)left, out);
+        }
     }
 }
 
@@ -472,8 +604,9 @@ namespace {
 
 // Rows wider than this are refused: 512 lanes with four runs of eight each.
 constexpr int kNormMaxChannels = 16384;
-// Workgroups of the backward pass, each of which leaves partial sums of 2 * C.
-constexpr int kNormBackGroups = 1024;
+// Workgroups of the backward pass, each of which leaves partial sums of 2 * C: as many as memory needs for its rate, fewer for
+// wide rows, where the partial sums would be a good part of what is moved (8192 fp16 channels, 2048 rows: 94 us with 1024 workgroups).
+int norm_back_most(int C) { return C <= 512 ? 1024 : C <= 2048 ? 512 : 256; }
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
@@ -500,18 +633,22 @@ int check_rows(long long P, int C, int dtype)
     return DCNV4_OK;
 }
 
-// Calls f with the lanes of a row and a lane's runs of eight channels, as constants.
+// Calls f with the lanes of a row and a lane's runs of eight channels, as constants: the fewest lanes that hold the row with one run each,
+// up to a wave; with two up to 1024 channels, then whole workgroups.
 template <typename F> int by_width(int C, F &&f)
 {
     const int runs = (C + 7) / 8;
+    if (runs <= 1) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    if (runs <= 2) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+    if (runs <= 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
     if (runs <= 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
     if (runs <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
     if (runs <= 32) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
     if (runs <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     if (runs <= 128) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
     if (runs <= 256) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    if (runs <= 512) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    if (runs <= 1024) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    if (runs <= 512) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+    if (runs <= 1024) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
 }
 
@@ -520,7 +657,9 @@ int norm_back_groups(long long P, int C)
     int groups = 0;
     by_width(C, [&](auto L, auto) {
         const long long rows = norm_threads(L()) / L(), n = (P + rows - 1) / rows;
-        groups = (int)(n < kNormBackGroups ? n : kNormBackGroups);
+        // (eight rows a lane at least where that leaves every unit a workgroup)
+        const long long enough = n / 8 > 256 ? n / 8 : 256, most = norm_back_most(C);
+        groups = (int)(n < enough ? n : enough < most ? enough : most);
         return 0;
     });
     return groups;
@@ -533,7 +672,7 @@ template <typename T, bool BRANCH> int launch_norm(const NormArgs &a, hipStream_
         return DCNV4_ERR_LAUNCH;
     return by_width(a.C, [&](auto L, auto NV) {
         constexpr int threads = norm_threads(L());
-        const long long rows = threads / L(), groups = (a.P + rows - 1) / rows, most = 64LL * cus;
+        const long long rows = threads / L(), groups = (a.P + rows - 1) / rows, most = (long long)(2048 / threads) * cus;
         const dim3 grid((unsigned)(groups < most ? groups : most));
         if (a.C % 8 == 0)
             hipLaunchKernelGGL((dcnv4_norm_kernel<T, L(), NV(), BRANCH, true>), grid, dim3(threads), 0, s, a);
@@ -612,7 +751,7 @@ int launch_dropout(const void *x, const void *residual, void *y, long long n, co
     const int cus = device_cus();
     if (cus <= 0)
         return DCNV4_ERR_LAUNCH;
-    const long long groups = (n + 2047) / 2048, most = 64LL * cus;
+    const long long groups = (n + 4095) / 4096, most = 64LL * cus;
     const dim3 grid((unsigned)(groups < most ? groups : most));
     if (residual != nullptr)
         hipLaunchKernelGGL((dcnv4_dropout_kernel<T, true>), grid, dim3(256), 0, s, (const T *)x, (const T *)residual, (T *)y, n, d);
