@@ -479,38 +479,41 @@ def dcnv4_module_forward_static(x, w_om, b_om, G, out, w_in=None, b_in=None, w_o
     return out
 
 
-# Operators on rows [..., C].  Optional tensors may be None; statistics and losses are float32.
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
-
+# Operators on rows [..., C].  Optional tensors may be None; statistics and losses are float32.  (Small calls are bound by this module:
+# a layer norm of 49 x 1024 takes the GPU 3 us.  So checks make nothing that a call without fault does not need.)
 
 def _rows(x):
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if len(shape) < 1 or shape[-1] < 1:
         raise ValueError("dcnv4: expected x [..., C]")
-    return x.numel() // x.shape[-1], x.shape[-1]
+    C = shape[-1]
+    return x.numel() // C, C
 
 
 def _check_like(x, named):
     """_check_all, and the shape of each (name, tensor, shape); tensors that are None are left out."""
-    named = [n for n in named if n[1] is not None]
-    _check_all(x, [(name, t) for name, t, _ in named])
+    at, dt = x.get_device(), x.dtype
+    if at < 0 or not x.is_cuda or not x.is_contiguous():
+        _check("x", x, x)
     for name, t, shape in named:
-        if tuple(t.shape) != tuple(shape):
+        if t is None:
+            continue
+        if t.get_device() != at or t.dtype is not dt or not t.is_contiguous():
+            _check(name, t, x)
+        if t.shape != shape:
             raise ValueError(f"dcnv4: {name} must have shape {tuple(shape)}")
 
 
-def _check_plain(name, t, x, shape, dtype):
-    if t.get_device() != x.get_device() or t.dtype is not dtype or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+def _check_plain(name, t, at, shape, dtype):
+    if t.get_device() != at or t.dtype is not dtype or not t.is_contiguous() or t.shape != shape:
         raise ValueError(f"dcnv4: {name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on x's device")
 
 
 def _outputs(x, out, specs):
     """The output tensors: those of `out`, checked, or new ones.  specs: (name, shape, dtype), None for one that is not wanted."""
-    import torch
     if out is None:
-        return [None if s is None else _uninitialised(x, s[1]) if s[2] is x.dtype else torch.empty(s[1], dtype=s[2], device=x.device)
-                for s in specs]
+        dt = x.dtype
+        return [None if s is None else _uninitialised(x, s[1]) if s[2] is dt else x.new_empty(s[1], dtype=s[2]) for s in specs]
     out = list(out) if isinstance(out, (tuple, list)) else [out]
     if len(out) != len(specs):
         raise ValueError(f"dcnv4: out must hold {len(specs)} tensors")
@@ -518,26 +521,31 @@ def _outputs(x, out, specs):
         if (t is None) != (s is None):
             raise ValueError("dcnv4: out must hold a tensor for every result, and None where there is none")
         if t is not None:
-            _check_plain(s[0], t, x, s[1], s[2])
+            _check_plain(s[0], t, x.get_device(), s[1], s[2])
     return out
 
 
 def _workspace(x, workspace, need):
+    """(workspace, bytes): the caller's, or a new one."""
     import torch
     if workspace is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+        need = max(need, 16)
+        return torch.empty(need, dtype=torch.uint8, device=x.device), need
     if workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         raise ValueError("dcnv4: workspace must be a contiguous tensor on x's device")
-    return workspace
+    return workspace, workspace.nbytes
 
 
-def _drop_args(x, p, seed, offset, offset_on_device):
-    """(p, seed, offset, address): 64-bit numbers of either sign are taken modulo 2^64."""
+_MASK64 = 2 ** 64 - 1
+
+
+def _offset_ptr(x, offset_on_device):
     import torch
-    if offset_on_device is not None and (offset_on_device.get_device() != x.get_device() or offset_on_device.dtype is not torch.int64
-                                         or offset_on_device.numel() != 1):
+    if offset_on_device is None:
+        return None
+    if offset_on_device.get_device() != x.get_device() or offset_on_device.dtype is not torch.int64 or offset_on_device.numel() != 1:
         raise ValueError("dcnv4: offset_on_device must be one int64 on x's device")
-    return float(p), int(seed) & (2 ** 64 - 1), int(offset) & (2 ** 64 - 1), _ptr(offset_on_device)
+    return offset_on_device.data_ptr()
 
 
 def dcnv4_layer_norm_workspace_bytes(P, C):
@@ -550,11 +558,14 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
     import torch
     P, C = _rows(x)
     _check_like(x, (("gamma", gamma, (C,)), ("beta", beta, (C,))))
-    stat = x.shape[:-1]
-    specs = [("y", x.shape, x.dtype)] + ([("mean", stat, torch.float32), ("rstd", stat, torch.float32)] if stats else [])
-    got = _outputs(x, out, specs)
-    y, mean, rstd = got if stats else (got[0], None, None)
-    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), P, C, float(eps), _dtype_code(x),
+    mean = rstd = None
+    if stats:
+        stat, f32 = x.shape[:-1], torch.float32
+        y, mean, rstd = _outputs(x, out, (("y", x.shape, x.dtype), ("mean", stat, f32), ("rstd", stat, f32)))
+    else:
+        y = _uninitialised(x, x.shape) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),))[0]
+    args = (x.data_ptr(), None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(), y.data_ptr(),
+            None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, eps, _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -567,15 +578,19 @@ def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=
     parameters)."""
     import torch
     P, C = _rows(x)
-    _check_like(x, (("gamma", gamma, (C,)), ("grad_y", grad_y, x.shape)))
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _check_plain(name, t, x, x.shape[:-1], torch.float32)
-    param = None if gamma is None else ((C,), x.dtype)
-    gx, gg, gb = _outputs(x, out, [("grad_x", x.shape, x.dtype)] + [param and (name, *param) for name in ("grad_gamma", "grad_beta")])
-    if param is not None:
-        workspace = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C))
-    args = (x.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), grad_y.data_ptr(), gx.data_ptr(), _ptr(gg), _ptr(gb),
-            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), P, C, _dtype_code(x),
+    shape, dt, at = x.shape, x.dtype, x.get_device()
+    _check_like(x, (("gamma", gamma, (C,)), ("grad_y", grad_y, shape)))
+    _check_plain("mean", mean, at, shape[:-1], torch.float32)
+    _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
+    if gamma is None:
+        (gx, gg, gb), size = _outputs(x, out, (("grad_x", shape, dt), None, None)), 0
+        workspace = None
+    else:
+        gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
+        workspace, size = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0)
+    ptr = torch.Tensor.data_ptr
+    args = (ptr(x), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), ptr(gx), None if gg is None else ptr(gg),
+            None if gb is None else ptr(gb), None if workspace is None else ptr(workspace), size, P, C, _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -585,12 +600,13 @@ def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=
 
 def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, out=None, stream=None, prepare_only=False):
     """[residual +] dropout of x: element i is dropped where its bits of the generator (include/dcnv4.h) at (seed, offset) say so,
-    else scaled by 1 / (1 - p).  offset_on_device: one int64 on the GPU, added to offset as the kernel runs (captured
-    graphs)."""
-    _check_like(x, (("residual", residual, x.shape),))
-    y, = _outputs(x, out, [("out", x.shape, x.dtype)])
-    args = (x.data_ptr(), _ptr(residual), y.data_ptr(), x.numel(), *_drop_args(x, p, seed, offset, offset_on_device), _dtype_code(x),
-            _stream_ptr(stream, x.device))
+    else scaled by 1 / (1 - p).  seed and offset: 64 bits, of either sign.  offset_on_device: one int64 on the GPU, added to
+    offset as the kernel runs (captured graphs)."""
+    shape = x.shape
+    _check_like(x, (("residual", residual, shape),))
+    y = _uninitialised(x, shape) if out is None else _outputs(x, out, (("out", shape, x.dtype),))[0]
+    args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), p, seed & _MASK64, offset & _MASK64,
+            _offset_ptr(x, offset_on_device), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
     _call(x.device, "dcnv4_dropout", args)
@@ -599,10 +615,11 @@ def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, ou
 
 def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out=None, stream=None, prepare_only=False):
     """grad_x of dcnv4_dropout with the same p, seed and offset (that of the residual is grad_y itself)."""
+    shape = grad_y.shape
     _check_all(grad_y, ())
-    gx, = _outputs(grad_y, out, [("out", grad_y.shape, grad_y.dtype)])
-    args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), *_drop_args(grad_y, p, seed, offset, offset_on_device), _dtype_code(grad_y),
-            _stream_ptr(stream, grad_y.device))
+    gx = _uninitialised(grad_y, shape) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),))[0]
+    args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), p, seed & _MASK64, offset & _MASK64, _offset_ptr(grad_y, offset_on_device),
+            _dtype_code(grad_y), _stream_ptr(stream, grad_y.device))
     if prepare_only:
         return args
     _call(grad_y.device, "dcnv4_dropout_backward", args)
@@ -614,12 +631,14 @@ def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, of
     """(z, y, mean, rstd): z = residual + dropout(x), y = layer norm of z over the last axis."""
     import torch
     P, C = _rows(x)
-    _check_like(x, (("residual", residual, x.shape), ("gamma", gamma, (C,)), ("beta", beta, (C,))))
-    stat = x.shape[:-1]
-    z, y, mean, rstd = _outputs(x, out, [("z", x.shape, x.dtype), ("y", x.shape, x.dtype), ("mean", stat, torch.float32),
-                                         ("rstd", stat, torch.float32)])
-    args = (x.data_ptr(), residual.data_ptr(), _ptr(gamma), _ptr(beta), z.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), P, C,
-            *_drop_args(x, p, seed, offset, offset_on_device), float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
+    shape, dt, f32 = x.shape, x.dtype, torch.float32
+    _check_like(x, (("residual", residual, shape), ("gamma", gamma, (C,)), ("beta", beta, (C,))))
+    stat = shape[:-1]
+    z, y, mean, rstd = _outputs(x, out, (("z", shape, dt), ("y", shape, dt), ("mean", stat, f32), ("rstd", stat, f32)))
+    ptr = torch.Tensor.data_ptr
+    args = (ptr(x), ptr(residual), None if gamma is None else ptr(gamma), None if beta is None else ptr(beta), ptr(z), ptr(y), ptr(mean),
+            ptr(rstd), P, C, p, seed & _MASK64, offset & _MASK64, _offset_ptr(x, offset_on_device), eps, _dtype_code(x),
+            _stream_ptr(stream, x.device))
     if prepare_only:
         return args
     _call(x.device, "dcnv4_dropout_add_layer_norm", args)
@@ -632,17 +651,21 @@ def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed,
     reads it.  The last two are None where gamma is None."""
     import torch
     P, C = _rows(z)
-    _check_like(z, (("gamma", gamma, (C,)), ("grad_y", grad_y, z.shape), ("grad_z", grad_z, z.shape)))
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _check_plain(name, t, z, z.shape[:-1], torch.float32)
-    param = None if gamma is None else ((C,), z.dtype)
-    gx, gr, gg, gb = _outputs(z, out, [("grad_x", z.shape, z.dtype), ("grad_residual", z.shape, z.dtype)] +
-                              [param and (name, *param) for name in ("grad_gamma", "grad_beta")])
-    if param is not None:
-        workspace = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C))
-    args = (z.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), grad_y.data_ptr(), _ptr(grad_z), gx.data_ptr(), gr.data_ptr(),
-            _ptr(gg), _ptr(gb), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), P, C,
-            *_drop_args(z, p, seed, offset, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
+    shape, dt, at = z.shape, z.dtype, z.get_device()
+    _check_like(z, (("gamma", gamma, (C,)), ("grad_y", grad_y, shape), ("grad_z", grad_z, shape)))
+    _check_plain("mean", mean, at, shape[:-1], torch.float32)
+    _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
+    specs = (("grad_x", shape, dt), ("grad_residual", shape, dt))
+    if gamma is None:
+        (gx, gr, gg, gb), size = _outputs(z, out, specs + (None, None)), 0
+        workspace = None
+    else:
+        gx, gr, gg, gb = _outputs(z, out, specs + (("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
+        workspace, size = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0)
+    ptr = torch.Tensor.data_ptr
+    args = (ptr(z), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), None if grad_z is None else ptr(grad_z), ptr(gx),
+            ptr(gr), None if gg is None else ptr(gg), None if gb is None else ptr(gb), None if workspace is None else ptr(workspace), size,
+            P, C, p, seed & _MASK64, offset & _MASK64, _offset_ptr(z, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
     if prepare_only:
         return args
     _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
@@ -659,19 +682,22 @@ def _loss_args(x, w, target, b, workspace, backward):
     if w.dim() != 2 or w.shape[1] != K:
         raise ValueError("dcnv4: expected x [..., K], w [V, K]")
     V = w.shape[0]
-    _check_like(x, (("w", w, (V, K)), ("b", b, (V,))))
-    _check_plain("target", target, x, x.shape[:-1], torch.int64)
-    return P, K, V, _workspace(x, workspace, dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, _dtype_code(x), backward))
+    _check_like(x, (("w", w, w.shape), ("b", b, (V,))))
+    _check_plain("target", target, x.get_device(), x.shape[:-1], torch.int64)
+    need = dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, _dtype_code(x), backward) if workspace is None else 0
+    return P, K, V, *_workspace(x, workspace, need)
 
 
 def dcnv4_linear_cross_entropy(x, w, target, b=None, ignore_index=-100, workspace=None, out=None, stream=None, prepare_only=False):
     """(loss, lse), float32 [...]: loss = lse - logit[target] with logits x w^T + b that are never stored.  x [..., K], w [V, K],
     target [...] int64; rows whose target is ignore_index have loss 0."""
     import torch
-    P, K, V, workspace = _loss_args(x, w, target, b, workspace, False)
-    loss, lse = _outputs(x, out, [("loss", x.shape[:-1], torch.float32), ("lse", x.shape[:-1], torch.float32)])
-    args = (x.data_ptr(), w.data_ptr(), _ptr(b), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
+    P, K, V, workspace, size = _loss_args(x, w, target, b, workspace, False)
+    stat, f32 = x.shape[:-1], torch.float32
+    loss, lse = _outputs(x, out, (("loss", stat, f32), ("lse", stat, f32)))
+    ptr = torch.Tensor.data_ptr
+    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(workspace), size, P, K, V, ignore_index,
+            _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
     _call(x.device, "dcnv4_linear_cross_entropy", args)
@@ -682,14 +708,14 @@ def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ig
                                         prepare_only=False):
     """(grad_x, grad_w, grad_b) of dcnv4_linear_cross_entropy for grad_loss [...] float32, from its lse; grad_b is None where b is."""
     import torch
-    P, K, V, workspace = _loss_args(x, w, target, b, workspace, True)
-    for name, t in (("lse", lse), ("grad_loss", grad_loss)):
-        _check_plain(name, t, x, x.shape[:-1], torch.float32)
-    gx, gw, gb = _outputs(x, out, [("grad_x", x.shape, x.dtype), ("grad_w", (V, K), x.dtype),
-                                   None if b is None else ("grad_b", (V,), x.dtype)])
-    args = (x.data_ptr(), w.data_ptr(), _ptr(b), target.data_ptr(), lse.data_ptr(), grad_loss.data_ptr(), gx.data_ptr(), gw.data_ptr(),
-            _ptr(gb), workspace.data_ptr(), workspace.numel() * workspace.element_size(), P, K, V, int(ignore_index), _dtype_code(x),
-            _stream_ptr(stream, x.device))
+    P, K, V, workspace, size = _loss_args(x, w, target, b, workspace, True)
+    shape, dt, at = x.shape, x.dtype, x.get_device()
+    _check_plain("lse", lse, at, shape[:-1], torch.float32)
+    _check_plain("grad_loss", grad_loss, at, shape[:-1], torch.float32)
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_w", w.shape, dt), None if b is None else ("grad_b", (V,), dt)))
+    ptr = torch.Tensor.data_ptr
+    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(lse), ptr(grad_loss), ptr(gx), ptr(gw), None if gb is None else ptr(gb),
+            ptr(workspace), size, P, K, V, ignore_index, _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
     _call(x.device, "dcnv4_linear_cross_entropy_backward", args)
