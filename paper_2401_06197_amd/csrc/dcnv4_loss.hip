@@ -419,17 +419,21 @@ __global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *part
 
 // What the backward pass knows of its rows beforehand: g per row (zero where the row is ignored, NaN where its target is no class), and
 // the largest |g| (of finite ones) of each 1024 rows.
+__device__ __forceinline__ float row_weight(const float *grad_loss, const Labels &l, long long px)
+{
+    const long long t = l.target[px];
+    return t == l.ignore ? 0.f : t >= 0 && t < l.V ? grad_loss[px] : __builtin_nanf("");
+}
+__device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
+
 __global__ __launch_bounds__(1024) void dcnv4_loss_rows_kernel(const float *grad_loss, Labels l, float *most, float *g)
 {
     __shared__ float part[16];
     const int px = (int)blockIdx.x * 1024 + (int)threadIdx.x;
     float top = 0.f;
     if (px < l.P) {
-        const long long t = l.target[px];
-        const float v = t == l.ignore ? 0.f : t >= 0 && t < l.V ? grad_loss[px] : __builtin_nanf("");
-        g[px] = v;
-        if (fabsf(v) < __builtin_inff())
-            top = fabsf(v);
+        g[px] = row_weight(grad_loss, l, px);
+        top = finite_size(g[px]);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)
@@ -447,17 +451,21 @@ __global__ __launch_bounds__(1024) void dcnv4_loss_rows_kernel(const float *grad
 
 // Rows as the products take them: in [rows][cols] -> out [rows][PL planes][pad], zeros behind the columns, fp32 numbers split into three.
 // With g: a row times g / scale, scale the largest |g| (1 if there is none), which goes to scale[0]; rows whose g is zero are
-// zeros, whatever they hold.  Eight numbers a lane.
+// zeros, whatever they hold.  Few rows (parts = 0): g and the largest are made here too, a launch less.  Eight numbers a lane.
 template <typename T, int PL, bool SCALED>
 __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, long long rows, int cols, int pad, unsigned short *out,
-                                                                 const float *g, const float *most, int parts, float *scale)
+                                                                 float *g, const float *most, int parts, float *scale, const float *grad_loss, Labels l)
 {
     float inv = 1.f;
     if constexpr (SCALED) {
         __shared__ float part[4];
         float top = 0.f;
-        for (int i = (int)threadIdx.x; i < parts; i += 256)
-            top = fmaxf(top, most[i]);
+        if (parts > 0)
+            for (int i = (int)threadIdx.x; i < parts; i += 256)
+                top = fmaxf(top, most[i]);
+        else
+            for (int i = (int)threadIdx.x; i < l.P; i += 256)
+                top = fmaxf(top, finite_size(row_weight(grad_loss, l, i)));
 #pragma unroll
         for (int d = 1; d < 64; d *= 2)
             top = fmaxf(top, __shfl_xor(top, d));
@@ -473,8 +481,16 @@ __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, lo
     const int units = pad / 8, unit = (int)threadIdx.x & 31;
     for (long long row = (long long)blockIdx.x * 8 + ((int)threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * 8) {
         float by = 1.f;
-        if constexpr (SCALED)
-            by = g[row] / inv;
+        if constexpr (SCALED) {
+            if (parts > 0) {
+                by = g[row];
+            } else {
+                by = row_weight(grad_loss, l, row);
+                if (unit == 0)
+                    g[row] = by;
+            }
+            by /= inv;
+        }
         for (int u = unit; u < units; u += 32) {
             float v[8];
 #pragma unroll
@@ -680,6 +696,7 @@ __global__ __launch_bounds__(256) void dcnv4_loss_sum_kernel(const float *planes
     const int units = cols / 4;
     for (long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x; i < n / 4; i += (long long)gridDim.x * 256) {
         f32x4 v = *reinterpret_cast<const f32x4 *>(planes + i * 4);
+#pragma unroll 8
         for (int s = 1; s < splits; ++s)
             v += *reinterpret_cast<const f32x4 *>(planes + s * plane + i * 4);
         const float by = o.row_scale != nullptr ? scale * o.row_scale[i / units] : scale;
@@ -714,11 +731,12 @@ __global__ __launch_bounds__(1024) void dcnv4_loss_bias_kernel(const float *sums
 
 namespace {
 
-// Tiles by number: classes (or columns of a result) x pixels (or its rows).
-enum { kSmall, kMiddle, kLarge };                          // fp16: 64x64, 128x128, 256x256; fp32: 64x64, 128x128, 256x128
+// Tiles by number: classes (or columns of a result) x pixels (or its rows).  fp16: 64x64, 128x128, 256x256; fp32: 64x64, 128x128, 256x128.
+enum { kSmall, kMiddle, kLarge };
 
 // The work is planned for this many compute units (the plan gives the size of the workspace, without a device).
 constexpr int kUnits = 256;
+constexpr int kFewRows = 2048;       // that every workgroup looks through by itself
 constexpr int kLossMaxRows = 1 << 20, kLossMaxClasses = 1 << 22;
 // Classes of a piece: d takes P * classes numbers in each layout, this many at most.
 constexpr long long kPieceNumbers = 1ll << 27;
@@ -728,13 +746,18 @@ constexpr long long kPieceWeights = 1ll << 27;
 
 struct Shape {
     int bm, bn, r;                     // classes (or columns of a result), pixels (or its rows), numbers of a step
-    float step, fixed, alone;          // us: a step of all tiles that a unit has at once, a tile's beginning and end, a lone tile's step
-    int slots;                         // tiles of a unit side by side
+    int slots;                         // tiles of a compute unit side by side
+    float step, fixed, alone, gen;
 };
+// Estimated times (us): a unit works through its share of the tiles, `slots` of them side by side, where half the difference between the
+// fullest unit and the mean is felt, and a part (`gen`) of the idle slots of the last round.  A tile takes `step` for a step, a lone
+// one `alone` at least, and `fixed` for its first loads and its results.  Fitted to 14 products of each type (16 to 51200 rows, 30 to 40000 classes,
+// K 128 to 1024, every tile, 1 to 16 splits; rms 15 %): the choice costs 3 % (fp16) and 0.4 % (fp32) on average.  16384 rows, 512 -> 1000,
+// forward: 53 (64x64), 30, 26 us, fp32 of 8192: 64, 50, 43; 1000, 256 -> 1000: 6.4, 9.0, 15, fp32: 9.7, 14, 21.
 inline const Shape &shape_of(int pl, int i)
 {
-    static const Shape f16[] = {{64, 64, 64, .17f, 1.2f, .25f, 2}, {128, 128, 32, .28f, 1.9f, .28f, 2}, {256, 256, 32, .58f, 8.6f, .58f, 1}};
-    static const Shape f32[] = {{64, 64, 32, .45f, 1.2f, .55f, 2}, {128, 128, 32, .85f, 2.5f, .85f, 1}, {256, 128, 32, 1.5f, 5.f, 1.5f, 1}};
+    static const Shape f16[] = {{64, 64, 64, 2, .21f, .72f, .26f, 1.f}, {128, 128, 32, 2, .268f, 2.f, .257f, .33f}, {256, 256, 32, 1, .562f, 7.6f, 0.f, 0.f}};
+    static const Shape f32[] = {{64, 64, 64, 1, .714f, 1.75f, 0.f, 0.f}, {128, 128, 32, 1, 1.017f, 3.6f, 0.f, 0.f}, {256, 128, 32, 1, 1.7f, 5.84f, 0.f, 0.f}};
     return (pl == 1 ? f16 : f32)[i];
 }
 
@@ -760,12 +783,14 @@ Choice choose_product(int pl, long long m, long long n, int length, bool may_spl
         const Shape &s = shape_of(pl, i);
         const int steps = (length + s.r - 1) / s.r;
         const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
-        for (int splits = 1; splits == 1 || (may_split && splits <= 64 && steps / splits >= 4); splits *= 2) {
-            const float full = ceilf((float)(tiles * splits) / (float)kUnits);
-            const int each = (steps + splits - 1) / splits;
-            float us = (float)each * (s.step * full > s.alone ? s.step * full : s.alone) + s.fixed * full;
+        for (int splits = 1; splits == 1 || (may_split && splits <= 64 && length / splits >= 256); splits *= 2) {
+            const float x = (float)(tiles * splits) / (float)kUnits, full = ceilf(x), slots = (float)s.slots;
+            const float rounds = x > slots ? slots * ceilf(x / slots) : full, even = s.slots > 1 && x > 1.f ? .5f * (x + full) : full;
+            const float share = even + s.gen * (rounds - even);
+            const float step = s.step * share > s.alone ? s.step * share : s.alone;
+            float us = (float)((steps + splits - 1) / splits) * step + s.fixed * share;
             if (splits > 1)                                // planes written and read once more, by a launch of its own
-                us += 3.f + (float)(m * n) * 8e-6f * (float)splits / 4.f;
+                us += 3.5f + .2f * (float)splits + (float)(m * n) * (float)splits * .9e-6f;
             if (best.shape < 0 || us < best_us) {
                 best = {i, splits};
                 best_us = us;
@@ -889,7 +914,7 @@ template <int PL, typename F> int with_tile(int shape, F &&f)
     } else {
         if (shape == kLarge) return f(TileOf<4, 2, 2, 2, 32, 2>());
         if (shape == kMiddle) return f(TileOf<2, 2, 2, 2, 32, 3>());
-        return f(TileOf<2, 2, 1, 1, 32, 3>());
+        return f(TileOf<2, 2, 1, 1, 64, 3>());
     }
 }
 
@@ -900,7 +925,7 @@ unsigned row_groups(long long rows) { return (unsigned)((rows + 7) / 8 < 8192 ? 
 void split_rows(const void *in, long long rows, int cols, int pad, void *out, hipStream_t s)
 {
     hipLaunchKernelGGL((dcnv4_loss_rows_in_kernel<float, 3, false>), dim3(row_groups(rows)), dim3(256), 0, s, (const float *)in, rows, cols, pad,
-                       (unsigned short *)out, (const float *)nullptr, (const float *)nullptr, 0, (float *)nullptr);
+                       (unsigned short *)out, (float *)nullptr, (const float *)nullptr, 0, (float *)nullptr, (const float *)nullptr, Labels{});
 }
 
 template <typename T, int PL> int loss_forward(const Plan &p, const void *x, const void *w, const Labels &labels, float *loss, float *lse, char *ws,
@@ -957,10 +982,11 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
                   void *grad_w, void *grad_b, char *ws, hipStream_t s)
 {
     float *scale = (float *)(ws + p.scale), *most = (float *)(ws + p.most), *g = (float *)(ws + p.g);
-    const int parts = (p.P + 1023) / 1024;
-    hipLaunchKernelGGL(dcnv4_loss_rows_kernel, dim3((unsigned)parts), dim3(1024), 0, s, grad_loss, labels, most, g);
+    const int parts = p.P <= kFewRows ? 0 : (p.P + 1023) / 1024;
+    if (parts > 0)
+        hipLaunchKernelGGL(dcnv4_loss_rows_kernel, dim3((unsigned)parts), dim3(1024), 0, s, grad_loss, labels, most, g);
     hipLaunchKernelGGL((dcnv4_loss_rows_in_kernel<T, PL, true>), dim3(row_groups(p.P)), dim3(256), 0, s, (const T *)x, (long long)p.P, p.K, p.kp,
-                       (unsigned short *)(ws + p.x_scaled), (const float *)g, (const float *)most, parts, scale);
+                       (unsigned short *)(ws + p.x_scaled), g, (const float *)most, parts, scale, grad_loss, labels);
     if (PL == 3)
         split_rows(x, p.P, p.K, p.kp, ws + p.x_split, s);
     const Operand xo = rows_of(PL == 3 ? (const void *)(ws + p.x_split) : x, p.P, p.kp, PL, p.kp);
