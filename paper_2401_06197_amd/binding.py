@@ -509,11 +509,25 @@ def _check_plain(name, t, at, shape, dtype):
         raise ValueError(f"dcnv4: {name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on x's device")
 
 
+def _new_like(x):
+    """_uninitialised(x, x.shape), faster (1.2 us, 1.8 with the shape)."""
+    import torch
+    return torch.empty_like(x) if type(x) is torch.Tensor else _uninitialised(x, x.shape)
+
+
+def _new(x, shape, dtype):
+    import torch
+    if type(x) is not torch.Tensor:
+        return torch.empty(shape, dtype=dtype, device=x.device)
+    if dtype is not x.dtype:
+        return x.new_empty(shape, dtype=dtype)
+    return torch.empty_like(x) if shape == x.shape else x.new_empty(shape)
+
+
 def _outputs(x, out, specs):
     """The output tensors: those of `out`, checked, or new ones.  specs: (name, shape, dtype), None for one that is not wanted."""
     if out is None:
-        dt = x.dtype
-        return [None if s is None else _uninitialised(x, s[1]) if s[2] is dt else x.new_empty(s[1], dtype=s[2]) for s in specs]
+        return [None if s is None else _new(x, s[1], s[2]) for s in specs]
     out = list(out) if isinstance(out, (tuple, list)) else [out]
     if len(out) != len(specs):
         raise ValueError(f"dcnv4: out must hold {len(specs)} tensors")
@@ -563,7 +577,7 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
         stat, f32 = x.shape[:-1], torch.float32
         y, mean, rstd = _outputs(x, out, (("y", x.shape, x.dtype), ("mean", stat, f32), ("rstd", stat, f32)))
     else:
-        y = _uninitialised(x, x.shape) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),))[0]
+        y = _new_like(x) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),))[0]
     args = (x.data_ptr(), None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(), y.data_ptr(),
             None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, eps, _dtype_code(x),
             _stream_ptr(stream, x.device))
@@ -604,7 +618,7 @@ def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, ou
     offset as the kernel runs (captured graphs)."""
     shape = x.shape
     _check_like(x, (("residual", residual, shape),))
-    y = _uninitialised(x, shape) if out is None else _outputs(x, out, (("out", shape, x.dtype),))[0]
+    y = _new_like(x) if out is None else _outputs(x, out, (("out", shape, x.dtype),))[0]
     args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), p, seed & _MASK64, offset & _MASK64,
             _offset_ptr(x, offset_on_device), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
@@ -617,7 +631,7 @@ def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out
     """grad_x of dcnv4_dropout with the same p, seed and offset (that of the residual is grad_y itself)."""
     shape = grad_y.shape
     _check_all(grad_y, ())
-    gx = _uninitialised(grad_y, shape) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),))[0]
+    gx = _new_like(grad_y) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),))[0]
     args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), p, seed & _MASK64, offset & _MASK64, _offset_ptr(grad_y, offset_on_device),
             _dtype_code(grad_y), _stream_ptr(stream, grad_y.device))
     if prepare_only:
