@@ -274,24 +274,47 @@ struct Labels {
     int v0, count;                    // of this launch: first class, how many
 };
 
-template <typename T> __device__ __forceinline__ float bias_of(const Labels &l, int v)
-{
-    return l.bias != nullptr ? (float)((const T *)l.bias)[min(v, l.V - 1)] : 0.f;
-}
-
 // The logits of a wave's classes and pixels: acc[m][n][4 * a + c] is class first + 32 * m + 8 * a + 4 * kb + c, pixel n * 32 + lane % 32.
 template <typename T, int WM, int WN>
 __device__ __forceinline__ void start_with_bias(const Labels &l, int first, int kb, f32x16 (&acc)[WM][WN])
 {
+    typedef T four __attribute__((ext_vector_type(4)));
+    const T *bias = (const T *)l.bias;
+    const bool inside = first + 32 * WM <= l.V;
 #pragma unroll
     for (int m = 0; m < WM; ++m)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float b = bias_of<T>(l, first + 32 * m + 8 * (r / 4) + 4 * kb + r % 4);
+        for (int a = 0; a < 4; ++a) {
+            const int c = first + 32 * m + 8 * a + 4 * kb;
+            four b = {};
+            if (bias != nullptr) {
+                if (inside)
+                    b = *reinterpret_cast<const four *>(bias + c);
+                else
+                    b = four{bias[min(c, l.V - 1)], bias[min(c + 1, l.V - 1)], bias[min(c + 2, l.V - 1)], bias[min(c + 3, l.V - 1)]};
+            }
 #pragma unroll
             for (int n = 0; n < WN; ++n)
-                acc[m][n][r] = b;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[m][n][4 * a + e] = (float)b[e];
         }
+}
+
+// Class of a wave's acc[m][n][r], from its first.
+__device__ __forceinline__ int class_of(int m, int r, int kb) { return 32 * m + 8 * (r / 4) + 4 * kb + r % 4; }
+
+// Calls f with the (m, r) of the lane's class `want`, in lanes that have it (-1: none).  Most waves have none: a few of thousands of classes.
+template <int WM, typename F> __device__ __forceinline__ void at_class(int want, int kb, F &&f)
+{
+    if (__builtin_amdgcn_ballot_w64(want >= 0) == 0)
+        return;
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (class_of(m, r, kb) == want)
+                f(m, r);
 }
 
 __device__ __forceinline__ float other_half(float v)       // of the lane 32 away
@@ -340,23 +363,19 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
         const int col = (wc * WN + n) * 32 + (lane & 31), px = bt * G::BN + col;
         const long long t = px < l.P ? l.target[px] : -1;
         const int want = t >= l.v0 + first && t < l.v0 + l.count && t < l.v0 + first + 32 * WM ? (int)(t - l.v0 - first) : -1;
-        float top = -__builtin_inff(), hit = 0.f;
-        bool have = false;
+        if (first + 32 * WM > l.count)                     // (the same for the whole wave)
+#pragma unroll
+            for (int m = 0; m < WM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    acc[m][n][r] = first + class_of(m, r, kb) < l.count ? acc[m][n][r] : -__builtin_inff();
+        at_class<WM>(want, kb, [&](int m, int r) { target_logit[px] = acc[m][n][r]; });
+        float top = -__builtin_inff();
 #pragma unroll
         for (int m = 0; m < WM; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int c = 32 * m + 8 * (r / 4) + 4 * kb + r % 4;
-                if (first + c >= l.count)
-                    acc[m][n][r] = -__builtin_inff();
-                if (c == want) {
-                    hit = acc[m][n][r];
-                    have = true;
-                }
+            for (int r = 0; r < 16; ++r)
                 top = fmaxf(top, acc[m][n][r]);
-            }
-        if (have)
-            target_logit[px] = hit;
         top = fmaxf(top, other_half(top));
         // (no class left: a sum of zeros.  The difference comes first: the product of a type's lowest value overflows)
         const float base = top == -__builtin_inff() ? 0.f : top;
@@ -556,13 +575,21 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
         for (int m = 0; m < WM; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int c = 32 * m + 8 * (r / 4) + 4 * kb + r % 4;
-                float v = __builtin_amdgcn_exp2f((acc[m][n][r] - lse) * kLog2e);
-                if (c == want)
-                    v -= 1.f;
-                acc[m][n][r] = g[n] != 0.f && first + c < l.count ? v : 0.f;
-            }
+            for (int r = 0; r < 16; ++r)
+                acc[m][n][r] = __builtin_amdgcn_exp2f((acc[m][n][r] - lse) * kLog2e);
+        at_class<WM>(want, kb, [&](int m, int r) { acc[m][n][r] -= 1.f; });
+        if (first + 32 * WM > l.count)
+#pragma unroll
+            for (int m = 0; m < WM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    acc[m][n][r] = first + class_of(m, r, kb) < l.count ? acc[m][n][r] : 0.f;
+        if (__builtin_amdgcn_ballot_w64(g[n] == 0.f) != 0)
+#pragma unroll
+            for (int m = 0; m < WM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    acc[m][n][r] = g[n] != 0.f ? acc[m][n][r] : 0.f;
     }
     if (d.bias_sums != nullptr) {
         // over the pixels of a lane, then of 32 lanes; lane i of them stores class i
@@ -574,11 +601,11 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
                 float s = 0.f;
 #pragma unroll
                 for (int n = 0; n < WN; ++n)
-                    s += acc[m][n][r] == 0.f ? 0.f : acc[m][n][r] * g[n];      // (a zero counts for nothing beside any g)
+                    s = __builtin_fmaf(acc[m][n][r], g[n], s);
                 s = sum_of_32(s);
                 mine = (row & 15) == r ? s : mine;
             }
-            const int c = first + 32 * m + 8 * ((row & 15) / 4) + 4 * kb + (row & 3);
+            const int c = first + class_of(m, row & 15, kb);
             if (row < 16 && c < l.count)
                 d.bias_sums[(long long)(bt * WC + wc) * l.count + c] = mine;
         }
