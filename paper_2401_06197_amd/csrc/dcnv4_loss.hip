@@ -40,8 +40,8 @@ struct Operand {
 struct Product {
     Operand a, b;
     int steps, steps_per_split;
-    int a_tiles, b_tiles, tiles, tiles_per_xcd;
-    FastDiv div_band, div_3;           // by the tiles of a band of four, and by three
+    int a_tiles, b_tiles, all, per_xcd;   // all: tiles times splits
+    FastDiv div_tiles, div_band, div_3;   // by the tiles, those of a band of four, and three
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -253,13 +253,16 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
     }
 };
 
-// The tile of this workgroup: consecutive ones to one XCD, in the order of bands of four tiles of B and along A within a band, so that the 32
-// tiles that an XCD has at once read eight tiles of A and four of B into its L2, not 32 and one.  False: none.
-__device__ __forceinline__ bool tile_of(const Product &q, int &a_tile, int &b_tile)
+// The tile and split of this workgroup: consecutive ones to one XCD, split after split (the tiles of a split read the same part of both
+// operands), in the order of bands of four tiles of B and along A within a band, so that the 32 tiles that an XCD has at once
+// read eight tiles of A and four of B into its L2, not 32 and one.  False: none.
+__device__ __forceinline__ bool tile_of(const Product &q, int &a_tile, int &b_tile, int &split)
 {
-    const int tile = ((int)blockIdx.x & (kXcds - 1)) * q.tiles_per_xcd + ((int)blockIdx.x >> 3);
-    if (((int)blockIdx.x >> 3) >= q.tiles_per_xcd || tile >= q.tiles)
+    const int at = ((int)blockIdx.x & (kXcds - 1)) * q.per_xcd + ((int)blockIdx.x >> 3);
+    if (((int)blockIdx.x >> 3) >= q.per_xcd || at >= q.all)
         return false;
+    split = fdiv(at, q.div_tiles);
+    const int tile = at - split * q.a_tiles * q.b_tiles;
     const int band = fdiv(tile, q.div_band), rest = tile - band * 4 * q.a_tiles, wide = min(4, q.b_tiles - band * 4);
     a_tile = wide == 4 ? rest >> 2 : wide == 2 ? rest >> 1 : wide == 1 ? rest : fdiv(rest, q.div_3);
     b_tile = band * 4 + rest - a_tile * wide;
@@ -348,8 +351,8 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 {
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
-    int at, bt;
-    if (!tile_of(q, at, bt))
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, kb = lane >> 5;
@@ -554,8 +557,8 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 {
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
-    int at, bt;
-    if (!tile_of(q, at, bt))
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
@@ -666,8 +669,8 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
     typedef std::conditional_t<WHOLE, T, float> S;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
-    int at, bt;
-    if (!tile_of(q, at, bt))
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
@@ -679,12 +682,12 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 acc[m][n][r] = 0.f;
-    const int t0 = (int)blockIdx.y * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
+    const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
     G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
     char *out = smem + wave * (G::OUT / G::kWaves);
     const int i0 = at * G::BM + wr * 32 * WM, j0 = bt * G::BN + wc * 32 * WN;
     constexpr int ES = (int)sizeof(S), ROW = 32 * WM * ES + 16, UNITS = 32 * WM * ES / 16;
-    S *to = (S *)o.out + (WHOLE ? 0 : (long long)blockIdx.y * o.plane);
+    S *to = (S *)o.out + (WHOLE ? 0 : (long long)split * o.plane);
     const float scale = WHOLE ? o.factor * (o.scale != nullptr ? o.scale[0] : 1.f) : 1.f;
 #pragma unroll
     for (int n = 0; n < WN; ++n) {
@@ -810,7 +813,11 @@ Choice choose_product(int pl, long long m, long long n, int length, bool may_spl
         const Shape &s = shape_of(pl, i);
         const int steps = (length + s.r - 1) / s.r;
         const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
-        for (int splits = 1; splits == 1 || (may_split && splits <= 64 && length / splits >= 256); splits *= 2) {
+        // powers of two, and what fills the units once and twice
+        const int fill = tiles < kUnits ? (int)(kUnits / tiles) : 1, tries[] = {1, 2, 4, 8, 16, 32, 64, fill, 2 * fill};
+        for (const int splits : tries) {
+            if (splits > 1 && (!may_split || splits > 64 || length / splits < 256))
+                continue;
             const float x = (float)(tiles * splits) / (float)kUnits, full = ceilf(x), slots = (float)s.slots;
             const float rounds = x > slots ? slots * ceilf(x / slots) : full, even = s.slots > 1 && x > 1.f ? .5f * (x + full) : full;
             const float share = even + s.gen * (rounds - even);
@@ -921,8 +928,9 @@ Product product_of(const Operand &a, const Operand &b, int pl, const Choice &c)
     q.steps_per_split = (q.steps + c.splits - 1) / c.splits;
     q.a_tiles = (a.count + s.bm - 1) / s.bm;
     q.b_tiles = (b.count + s.bn - 1) / s.bn;
-    q.tiles = q.a_tiles * q.b_tiles;
-    q.tiles_per_xcd = (q.tiles + kXcds - 1) / kXcds;
+    q.all = q.a_tiles * q.b_tiles * c.splits;
+    q.per_xcd = (q.all + kXcds - 1) / kXcds;
+    q.div_tiles = make_div((unsigned)(q.a_tiles * q.b_tiles));
     q.div_band = make_div(4u * (unsigned)q.a_tiles);
     q.div_3 = make_div(3);
     return q;
@@ -972,7 +980,7 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
         const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, PL, p.logits);
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
-            hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
+            hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
                                dim3(G::WR * G::WC * 64), 0, s, q, l, (float2 *)(ws + p.partial) + (long long)tiles * p.P, (float *)(ws + p.hit));
             return 0;
         });
@@ -988,7 +996,7 @@ void launch_product(const Product &q, const Choice &c, bool planes, const Result
 {
     with_tile<PL>(c.shape, [&](auto t) {
         typedef decltype(t) G;
-        const dim3 grid((unsigned)(q.tiles_per_xcd * kXcds), (unsigned)c.splits), block(G::WR * G::WC * 64);
+        const dim3 grid((unsigned)(q.per_xcd * kXcds)), block(G::WR * G::WC * 64);
         if (planes)
             hipLaunchKernelGGL((dcnv4_loss_product_kernel<T, false, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
         else
@@ -1035,7 +1043,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
             runs = q.b_tiles * G::WC;
-            hipLaunchKernelGGL((dcnv4_loss_delta_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.tiles_per_xcd * kXcds)),
+            hipLaunchKernelGGL((dcnv4_loss_delta_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
                                dim3(G::WR * G::WC * 64), 0, s, q, l, d);
             return 0;
         });
