@@ -274,7 +274,7 @@ int dcnv4_dropout_add_layer_norm_backward(const void *z, const void *gamma, cons
  *     logit[p][v] = sum_k x[p][k] * w[v][k] + b[v],   lse[p] = log sum_v exp(logit[p][v]),   loss[p] = lse[p] - logit[p][target[p]]
  * x [P][K], w [V][K], b [V] or NULL; target: 64-bit class numbers [P]; loss, lse: fp32 [P].  A row whose target is ignore_index
  * has loss 0; one whose target is neither that nor a class has loss NaN.  Logits and sums are fp32 (F32: products of operands
- * held as three bf16 numbers, fp32's accuracy for numbers above 2^-100; x and w must be finite, F16 follows fp16's infinities).  b may
+ * held as three bf16 numbers, fp32's accuracy for numbers above 2^-100; x and w must be finite and below 3.3e38; F16 follows fp16's infinities).  b may
  * hold -infinity: that class has probability 0.
  * Needs K * element size a multiple of 32 bytes, K and P up to 2^20, V up to 2^22 (else DCNV4_ERR_UNSUPPORTED); any V and P.
  * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 0) bytes. */

@@ -579,7 +579,7 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
     else:
         y = _new_like(x) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),))[0]
     args = (x.data_ptr(), None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(), y.data_ptr(),
-            None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, eps, _dtype_code(x),
+            None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, float(eps), _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -619,7 +619,7 @@ def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, ou
     shape = x.shape
     _check_like(x, (("residual", residual, shape),))
     y = _new_like(x) if out is None else _outputs(x, out, (("out", shape, x.dtype),))[0]
-    args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), p, seed & _MASK64, offset & _MASK64,
+    args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64,
             _offset_ptr(x, offset_on_device), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -632,7 +632,7 @@ def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out
     shape = grad_y.shape
     _check_all(grad_y, ())
     gx = _new_like(grad_y) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),))[0]
-    args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), p, seed & _MASK64, offset & _MASK64, _offset_ptr(grad_y, offset_on_device),
+    args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(grad_y, offset_on_device),
             _dtype_code(grad_y), _stream_ptr(stream, grad_y.device))
     if prepare_only:
         return args
@@ -651,7 +651,7 @@ def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, of
     z, y, mean, rstd = _outputs(x, out, (("z", shape, dt), ("y", shape, dt), ("mean", stat, f32), ("rstd", stat, f32)))
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(residual), None if gamma is None else ptr(gamma), None if beta is None else ptr(beta), ptr(z), ptr(y), ptr(mean),
-            ptr(rstd), P, C, p, seed & _MASK64, offset & _MASK64, _offset_ptr(x, offset_on_device), eps, _dtype_code(x),
+            ptr(rstd), P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(x, offset_on_device), float(eps), _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -679,7 +679,7 @@ def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed,
     ptr = torch.Tensor.data_ptr
     args = (ptr(z), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), None if grad_z is None else ptr(grad_z), ptr(gx),
             ptr(gr), None if gg is None else ptr(gg), None if gb is None else ptr(gb), None if workspace is None else ptr(workspace), size,
-            P, C, p, seed & _MASK64, offset & _MASK64, _offset_ptr(z, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
+            P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(z, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
     if prepare_only:
         return args
     _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
@@ -710,7 +710,7 @@ def dcnv4_linear_cross_entropy(x, w, target, b=None, ignore_index=-100, workspac
     stat, f32 = x.shape[:-1], torch.float32
     loss, lse = _outputs(x, out, (("loss", stat, f32), ("lse", stat, f32)))
     ptr = torch.Tensor.data_ptr
-    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(workspace), size, P, K, V, ignore_index,
+    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(workspace), size, P, K, V, int(ignore_index),
             _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
@@ -729,7 +729,7 @@ def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ig
     gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_w", w.shape, dt), None if b is None else ("grad_b", (V,), dt)))
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(lse), ptr(grad_loss), ptr(gx), ptr(gw), None if gb is None else ptr(gb),
-            ptr(workspace), size, P, K, V, ignore_index, _dtype_code(x), _stream_ptr(stream, x.device))
+            ptr(workspace), size, P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return args
     _call(x.device, "dcnv4_linear_cross_entropy_backward", args)

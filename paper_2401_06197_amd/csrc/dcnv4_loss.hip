@@ -781,13 +781,13 @@ struct Shape {
 };
 // Estimated times (us): a unit works through its share of the tiles, `slots` of them side by side, where half the difference between the
 // fullest unit and the mean is felt, and a part (`gen`) of the idle slots of the last round.  A tile takes `step` for a step, a lone
-// one `alone` at least, and `fixed` for its first loads and its results.  Fitted to 14 products of each type (16 to 51200 rows, 30 to 40000 classes,
-// K 128 to 1024, every tile, 1 to 16 splits; rms 15 %): the choice costs 3 % (fp16) and 0.4 % (fp32) on average.  16384 rows, 512 -> 1000,
-// forward: 53 (64x64), 30, 26 us, fp32 of 8192: 64, 50, 43; 1000, 256 -> 1000: 6.4, 9.0, 15, fp32: 9.7, 14, 21.
+// one `alone` at least, and `fixed` for its first loads and its results.  Fitted to products of 17 sizes (16 to 51200 rows, 30 to 40000 classes,
+// K 128 to 1024, every tile, 1 to 64 splits; rms 12 %): the choice costs 2.5 % (fp16) and 0.9 % (fp32) on average.  16384 rows, 512 -> 1000,
+// forward: 45 (64x64), 29, 25 us, fp32 of 8192: 65, 52, 44; 1000, 256 -> 1000: 5.6, 9.0, 14, fp32: 8.2, 16, 20.
 inline const Shape &shape_of(int pl, int i)
 {
-    static const Shape f16[] = {{64, 64, 64, 2, .21f, .72f, .26f, 1.f}, {128, 128, 32, 2, .268f, 2.f, .257f, .33f}, {256, 256, 32, 1, .562f, 7.6f, 0.f, 0.f}};
-    static const Shape f32[] = {{64, 64, 64, 1, .714f, 1.75f, 0.f, 0.f}, {128, 128, 32, 1, 1.017f, 3.6f, 0.f, 0.f}, {256, 128, 32, 1, 1.7f, 5.84f, 0.f, 0.f}};
+    static const Shape f16[] = {{64, 64, 64, 2, .204f, .75f, .263f, .5f}, {128, 128, 32, 2, .273f, 1.44f, .273f, 0.f}, {256, 256, 32, 1, .562f, 5.9f, 0.f, 0.f}};
+    static const Shape f32[] = {{64, 64, 64, 1, .719f, 1.44f, 0.f, 0.f}, {128, 128, 32, 1, 1.01f, 2.6f, 0.f, 0.f}, {256, 128, 32, 1, 1.73f, 3.7f, 0.f, 0.f}};
     return (pl == 1 ? f16 : f32)[i];
 }
 
@@ -824,7 +824,7 @@ Choice choose_product(int pl, long long m, long long n, int length, bool may_spl
             const float step = s.step * share > s.alone ? s.step * share : s.alone;
             float us = (float)((steps + splits - 1) / splits) * step + s.fixed * share;
             if (splits > 1)                                // planes written and read once more, by a launch of its own
-                us += 3.5f + .2f * (float)splits + (float)(m * n) * (float)splits * .9e-6f;
+                us += 2.5f + .09f * (float)splits + (float)(m * n) * (float)splits * 1.2e-6f;
             if (best.shape < 0 || us < best_us) {
                 best = {i, splits};
                 best_us = us;

@@ -302,3 +302,46 @@ def test_refusals():
     assert e.value.status == 3
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+def test_more_than_32_bits_of_bytes():
+    """x of more than 4 GiB: the last rows are what a call on them alone gives, and gradients of zero weight stay out."""
+    P, K, V = 2 ** 20 - 1, 2064, 40
+    few, w, b, t0, _ = inputs(128, K, V, "f16", 4)
+    x, t = few.repeat(P // 128 + 1, 1)[:P].contiguous(), t0.repeat(P // 128 + 1)[:P].contiguous()
+    loss, lse = dcn.dcnv4_linear_cross_entropy(x, w, t, b)
+    g = torch.zeros(P, device="cuda")
+    g[-100:] = 3.0
+    got = dcn.dcnv4_linear_cross_entropy_backward(x, w, t, lse, g, b)
+    tail = slice(P - 100, P)
+    want = expected(x[tail], w, b, t[tail], g[tail])
+    close("loss", loss[tail], want["loss"], "f32")
+    close("grad_x", got[0][tail], want["grad_x"], "f16")
+    assert not got[0][:P - 100].any()
+    close("grad_w", got[1], want["grad_w"], "f16")
+    close("grad_b", got[2], want["grad_b"], "f16")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_a_class_as_the_ignored_one(dtype):
+    """ignore_index may be a class: its rows count for nothing, and it is a class for the others."""
+    P, K, V = 200, 48, 6
+    x, w, b, t, g = inputs(P, K, V, dtype, 6, ignored=0.0)
+    other = torch.where(t == 3, torch.full_like(t, IGNORE), t)
+    first = dcn.dcnv4_linear_cross_entropy(x, w, other, b)
+    second = dcn.dcnv4_linear_cross_entropy(x, w, t, b, ignore_index=3)
+    assert all(torch.equal(a, c) for a, c in zip(first, second))
+    back = [dcn.dcnv4_linear_cross_entropy_backward(x, w, u, first[1], g, b, ignore_index=i) for u, i in ((other, IGNORE), (t, 3))]
+    assert all(torch.equal(a, c) for a, c in zip(*back))
+
+
+def test_one_vector_and_maps():
+    """x of one vector, and of a map of pixels: targets, losses and gradients have its shape."""
+    x, w, b, t, g = inputs(30, 32, 11, "f32", 7, ignored=0.0)
+    loss, lse = dcn.dcnv4_linear_cross_entropy(x, w, t, b)
+    m = dcn.dcnv4_linear_cross_entropy(x.view(2, 3, 5, 32), w, t.view(2, 3, 5), b)
+    assert m[0].shape == (2, 3, 5) and torch.equal(m[0].view(-1), loss)
+    gx = dcn.dcnv4_linear_cross_entropy_backward(x.view(2, 3, 5, 32), w, t.view(2, 3, 5), m[1], g.view(2, 3, 5), b)[0]
+    assert gx.shape == (2, 3, 5, 32) and torch.equal(gx.view(30, 32), dcn.dcnv4_linear_cross_entropy_backward(x, w, t, lse, g, b)[0])
+    one = dcn.dcnv4_linear_cross_entropy(x[0].clone(), w, t[0].clone(), b)
+    assert one[0].shape == () and abs(one[0].item() - loss[0].item()) <= 1e-5

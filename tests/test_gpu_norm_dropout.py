@@ -319,3 +319,62 @@ def test_refusals():
         assert e.value.status == status
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+def test_more_than_32_bits_of_elements():
+    """2^32 elements and more: what lies behind them is what the definition says, and what a call on the end alone gives."""
+    n, p, seed, offset = 2 ** 32 + 13, 0.5, 21, 4
+    x = torch.ones(n, device="cuda", dtype=torch.float16)
+    y = dcn.dcnv4_dropout(x, p, seed, offset)
+    for first in (0, 2 ** 31 - 5, 2 ** 32 - 100):
+        count = min(500, n - first)
+        gone = ref.dropped(count, p, seed, offset, first=first)
+        assert np.array_equal(y[first:first + count].cpu().numpy() == 0, gone)
+    del x, y
+    P, C = 2 ** 20 + 3, 2056
+    x = torch.randn((64, C), device="cuda", dtype=torch.float16).repeat(P // 64 + 1, 1)[:P].contiguous()
+    gamma = torch.randn(C, device="cuda", dtype=torch.float16)
+    y, mean, rstd = dcn.dcnv4_layer_norm(x, gamma, stats=True)
+    last = x[-70:].clone()
+    alone = dcn.dcnv4_layer_norm(last, gamma, stats=True)
+    assert all(torch.equal(a[-70:], b) for a, b in zip((y, mean, rstd), alone))
+    gx, _, _ = dcn.dcnv4_layer_norm_backward(x, gamma, mean, rstd, y)
+    only, _, _ = dcn.dcnv4_layer_norm_backward(last, gamma, alone[1], alone[2], alone[0])
+    assert torch.equal(gx[-70:], only)
+
+
+def test_explicit_streams():
+    """A call on a stream that is handed over runs there, whatever stream is current."""
+    x = torch.randn((64, 100), device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y = dcn.dcnv4_layer_norm(x, stream=s)
+    d = dcn.dcnv4_dropout(x, 0.5, 1, residual=y, stream=s)
+    s.synchronize()
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y, dcn.dcnv4_layer_norm(x)) and torch.equal(d, dcn.dcnv4_dropout(x, 0.5, 1, residual=y))
+
+
+def test_one_parameter_gradient_alone():
+    """grad_gamma or grad_beta may be left out, also where there is no gamma; numbers of numpy's types are numbers."""
+    P, C = 40, 72
+    x, gy = torch.randn((P, C), device="cuda"), torch.randn((P, C), device="cuda")
+    gamma = torch.randn(C, device="cuda")
+    _, mean, rstd = dcn.dcnv4_layer_norm(x, gamma, eps=np.float32(1e-5), stats=True)
+    both = dcn.dcnv4_layer_norm_backward(x, gamma, mean, rstd, gy)
+    work = torch.empty(dcn.dcnv4_layer_norm_workspace_bytes(P, C), dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for keep in (1, 2):
+        out = [torch.empty_like(x), torch.empty_like(gamma) if keep == 1 else None, torch.empty_like(gamma) if keep == 2 else None]
+        ptr = [None if t is None else t.data_ptr() for t in (x, gamma, mean, rstd, gy, *out)]
+        assert dcn.load_library().dcnv4_layer_norm_backward(*ptr, work.data_ptr(), work.numel(), P, C, 0, stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], both[0]) and torch.equal(out[keep], both[keep])
+    # a norm with beta alone
+    gx, gb = torch.empty_like(x), torch.empty_like(gamma)
+    assert dcn.load_library().dcnv4_layer_norm_backward(x.data_ptr(), None, mean.data_ptr(), rstd.data_ptr(), gy.data_ptr(), gx.data_ptr(), None,
+                                                        gb.data_ptr(), work.data_ptr(), work.numel(), P, C, 0, stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(gb, both[2]) and torch.equal(gx, dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy)[0])
+    a = dcn.dcnv4_dropout(x, np.float64(0.5), np.int64(-7), np.int32(3))
+    assert torch.equal(a, dcn.dcnv4_dropout(x, 0.5, 2 ** 64 - 7, 3))
