@@ -344,10 +344,20 @@ __device__ __forceinline__ float sum_of_32(float v)        // over the lane's ha
 
 }  // namespace
 
+// The loss of a row, from its largest logit, the sum of exponentials beside it, and its target's logit.
+__device__ __forceinline__ void finish_row(const Labels &l, int px, float top, float sum, float hit, float *loss, float *lse)
+{
+    const float all = top + logf(sum);
+    const long long t = l.target[px];
+    lse[px] = all;
+    loss[px] = t == l.ignore ? 0.f : t >= 0 && t < l.V ? all - hit : __builtin_nanf("");
+}
+
 // Forward: per pixel and tile of classes the largest logit and the sum of the others' exponentials beside it: partial[a_tile][P];
-// the target's logit goes to target_logit[P] (one lane of the grid has it).
+// the target's logit goes to target_logit[P] (one lane of the grid has it).  One tile of classes (partial null): the loss at once.
 template <typename T, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_loss_kernel(Product q, Labels l, float2 *partial, float *target_logit)
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_loss_kernel(Product q, Labels l, float2 *partial, float *target_logit,
+                                                                                                                                             float *loss, float *lse)
 {
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
@@ -361,6 +371,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     start_with_bias<T, WM, WN>(l, l.v0 + first, kb, acc);
     G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, 0, q.steps, acc);
     float2 *mine = reinterpret_cast<float2 *>(smem);       // [WR][BN]
+    float *hits = reinterpret_cast<float *>(mine + WR * G::BN);
 #pragma unroll
     for (int n = 0; n < WN; ++n) {
         const int col = (wc * WN + n) * 32 + (lane & 31), px = bt * G::BN + col;
@@ -372,7 +383,12 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     acc[m][n][r] = first + class_of(m, r, kb) < l.count ? acc[m][n][r] : -__builtin_inff();
-        at_class<WM>(want, kb, [&](int m, int r) { target_logit[px] = acc[m][n][r]; });
+        at_class<WM>(want, kb, [&](int m, int r) {
+            if (partial != nullptr)
+                target_logit[px] = acc[m][n][r];
+            else
+                hits[col] = acc[m][n][r];
+        });
         float top = -__builtin_inff();
 #pragma unroll
         for (int m = 0; m < WM; ++m)
@@ -406,7 +422,10 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
         for (int w = 0; w < WR; ++w)
             sum += mine[w * G::BN + col].y * __builtin_amdgcn_exp2f((mine[w * G::BN + col].x - base) * kLog2e);
-        partial[(long long)at * l.P + px] = make_float2(top, sum);
+        if (partial != nullptr)
+            partial[(long long)at * l.P + px] = make_float2(top, sum);
+        else
+            finish_row(l, px, top, sum, hits[col], loss, lse);
     }
 }
 
@@ -433,10 +452,7 @@ __global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *part
 #pragma unroll
     for (int s = 1; s < 16; ++s)
         join(part[s][i]);
-    const float all = top + logf(sum);
-    const long long t = l.target[px];
-    lse[px] = all;
-    loss[px] = t == l.ignore ? 0.f : t >= 0 && t < l.V ? all - target_logit[px] : __builtin_nanf("");
+    finish_row(l, px, top, sum, target_logit[px], loss, lse);
 }
 
 // What the backward pass knows of its rows beforehand: g per row (zero where the row is ignored, NaN where its target is no class), and
@@ -978,15 +994,18 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
         if (PL == 3)
             split_rows(rows, l.count, p.K, p.kp, ws + p.w_split, s);
         const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, PL, p.logits);
+        const bool one = p.pieces == 1 && q.a_tiles == 1;
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
             hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
-                               dim3(G::WR * G::WC * 64), 0, s, q, l, (float2 *)(ws + p.partial) + (long long)tiles * p.P, (float *)(ws + p.hit));
+                               dim3(G::WR * G::WC * 64), 0, s, q, l, one ? nullptr : (float2 *)(ws + p.partial) + (long long)tiles * p.P,
+                               (float *)(ws + p.hit), loss, lse);
             return 0;
         });
         tiles += q.a_tiles;
     }
-    hipLaunchKernelGGL(dcnv4_loss_join_kernel, dim3((unsigned)((p.P + 15) / 16)), dim3(256), 0, s, (const float2 *)(ws + p.partial), tiles,
+    if (tiles > 1)
+        hipLaunchKernelGGL(dcnv4_loss_join_kernel, dim3((unsigned)((p.P + 15) / 16)), dim3(256), 0, s, (const float2 *)(ws + p.partial), tiles,
                        (const float *)(ws + p.hit), labels, loss, lse);
     return launched();
 }
