@@ -4,8 +4,12 @@
 // All of it is bound by memory: a kernel reads each input once, keeps a row in registers while its statistics are made, and
 // writes each output once.  A lane holds runs of eight channels (16 bytes in fp16, 32 in fp32).  A row belongs to L lanes: as
 // few of a wave as its runs need, whole waves for wide rows.  A workgroup stays for many rows and asks for the next ones before it
-// deals with the present ones: a wave's loads alone, some KiB, do not cover the memory's latency (50176 x 256 fp16 norm forward
-// 4.3 -> 5.4 TB/s, backward 3.1 -> 4.6).
+// deals with the present ones: a wave's loads alone, some KiB, do not cover the memory's latency (65536 x 256 fp16 norm: forward 15.8
+// -> 15.0 us, backward 32.5 -> 23.8).
+//
+// Rates (16.8 million elements, 128 to 4096 channels; a copy of as much: 6.5 TB/s in fp16, which the caches hold in part, 5.2 in fp32):
+// norm 4.2 to 4.8 TB/s forward and 3.5 to 4.3 backward in fp16, 4.5 to 4.8 and 4.1 to 4.7 in fp32; branch ends 4.5 to 4.9 and 4.0 to 4.3, 4.8
+// to 5.2 and 4.4 to 4.9; rows of odd lengths 55 to 75 % of that in fp16, 75 to 95 % in fp32.
 #include <math.h>
 
 #include <initializer_list>
@@ -87,14 +91,15 @@ template <typename T> struct Run {                         // as they lie in mem
 };
 template <typename T> using Raw8 = typename Run<T>::type;
 
-template <typename T, bool WHOLE> __device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool past)
+// n channels of a row (none for n <= 0), and what follows them where n < 8.  `safe`: eight from the row's last channel on are memory of
+// the tensor; otherwise no more than the n are read.
+template <typename T, bool WHOLE> __device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool safe)
 {
-    // n channels of the row; `past`: eight would reach past the end of the tensor
     Raw8<T> r = {};
     if (WHOLE) {
         if (n > 0)
             r = *reinterpret_cast<const typename Run<T>::aligned *>(p);
-    } else if (n >= 8 || (n > 0 && !past)) {
+    } else if (n >= 8 || (n > 0 && safe)) {
         r = *reinterpret_cast<const typename Run<T>::any *>(p);
     } else {
 #pragma unroll
@@ -104,12 +109,35 @@ template <typename T, bool WHOLE> __device__ __forceinline__ Raw8<T> load8(const
     }
     return r;
 }
-// As fp32, zeros behind the n.
-template <typename T, bool WHOLE> __device__ __forceinline__ void unpack(const Raw8<T> &r, int n, float (&v)[8])
+// The bits of the first n of eight (which a lane's runs keep from row to row).
+template <typename T> struct Mask8 {
+    unsigned w[2 * sizeof(T)];
+    __device__ __forceinline__ explicit Mask8(int n)
+    {
+#pragma unroll
+        for (int k = 0; k < (int)(2 * sizeof(T)); ++k) {
+            if constexpr (sizeof(T) == 2)
+                w[k] = n >= 2 * k + 2 ? ~0u : n == 2 * k + 1 ? 0xffffu : 0u;
+            else
+                w[k] = n >= k + 1 ? ~0u : 0u;
+        }
+    }
+    __device__ __forceinline__ Mask8() {}
+};
+// As fp32, zeros behind the first n whatever lies there.
+template <typename T, bool WHOLE> __device__ __forceinline__ void unpack(Raw8<T> r, const Mask8<T> &m, float (&v)[8])
 {
+    if constexpr (!WHOLE) {
+        typedef unsigned words __attribute__((ext_vector_type(2 * sizeof(T))));
+        words u = __builtin_bit_cast(words, r);
+#pragma unroll
+        for (int k = 0; k < (int)(2 * sizeof(T)); ++k)
+            u[k] &= m.w[k];
+        r = __builtin_bit_cast(Raw8<T>, u);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        v[e] = (WHOLE ? n > 0 : e < n) ? (float)r[e] : 0.f;
+        v[e] = (float)r[e];
 }
 
 template <typename T, bool WHOLE> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
@@ -182,7 +210,7 @@ template <int L, int N> __device__ __forceinline__ void row_sums(float (&v)[N], 
         v[k] = wave_sum<(L < 64 ? L : 64)>(v[k]);
     if constexpr (L > 64) {
         constexpr int W = L / 64;
-        const int wave = (int)threadIdx.x >> 6;
+        const int wave = (int)threadIdx.x >> 6, first = wave / W * W;
         __syncthreads();                                   // all have read the sums before these
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -191,15 +219,15 @@ template <int L, int N> __device__ __forceinline__ void row_sums(float (&v)[N], 
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            v[k] = lds[0][k];
+            v[k] = lds[first][k];
 #pragma unroll
             for (int w = 1; w < W; ++w)
-                v[k] += lds[w][k];
+                v[k] += lds[first + w][k];
         }
     }
 }
 
-constexpr int norm_threads(int L) { return L > 256 ? L : 256; }
+constexpr int norm_threads(int L) { return L >= 256 ? 512 : 256; }
 
 // Where a lane's run j lies in its row, in runs: side by side in a wave, then run after run, then the next wave's.
 template <int L, int NV> __device__ __forceinline__ int run_of(int l, int j)
@@ -210,7 +238,7 @@ template <int L, int NV> __device__ __forceinline__ int run_of(int l, int j)
 
 // What drop_apply takes for a lane's runs, `first` being the first element of the row.  Rows that start inside a block share each block
 // between two neighbouring runs: a lane makes one block's decisions and takes those of the second from the next lane (the
-// last lane of a wave makes its last ones itself).  Both blocks made by each lane: fp16 branch ends of 52265 x 321 72 us, 41 so.
+// last lane of a wave makes its last ones itself).  Both blocks made by each lane: fp16 branch ends of 52265 x 321 72 us, 49 so.
 template <int L, int NV, bool WHOLE>
 __device__ __forceinline__ void row_bits(Bits8 (&b)[NV], unsigned long long first, int C, int l, unsigned long long offset, const Drop &d)
 {
@@ -268,59 +296,61 @@ template <typename T, int L, int NV, bool BRANCH, bool WHOLE>
 __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_kernel(NormArgs a)
 {
     constexpr int R = norm_threads(L) / L;                 // rows of a workgroup
-    __shared__ float lds[L > 64 ? L / 64 : 1][1];
-    const int l = (int)threadIdx.x % L;
+    __shared__ float lds[norm_threads(L) / 64][1];
+    const int l = (int)threadIdx.x % L, first = (int)threadIdx.x / L;
     const T *gamma = (const T *)a.gamma, *beta = (const T *)a.beta;
     const unsigned long long offset = BRANCH ? drop_offset(a.drop) : 0ull;
     const long long all = a.P * a.C, stride = (long long)gridDim.x * R;
+    constexpr bool AHEAD = NV <= 2;                        // (else no registers for two rows)
     Raw8<T> x[NV], res[BRANCH ? NV : 1], gm[NV], bt[NV];
-    auto load = [&](long long row) {
+    Mask8<T> mask[NV];
+    auto load = [&](long long row) {                       // (a row past the last: nothing)
+        const bool safe = (row + 1) * a.C + 7 <= all;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
-            const long long at = row * a.C + c;
-            x[j] = load8<T, WHOLE>((const T *)a.x + at, n, all - at < 8);
+            const int c = run_of<L, NV>(l, j) * 8, n = row < a.P ? a.C - c : 0;
+            x[j] = load8<T, WHOLE>((const T *)a.x + row * a.C + c, n, safe);
             if constexpr (BRANCH)
-                res[j] = load8<T, WHOLE>((const T *)a.residual + at, n, all - at < 8);
+                res[j] = load8<T, WHOLE>((const T *)a.residual + row * a.C + c, n, safe);
         }
     };
-    constexpr bool AHEAD = NV <= 2;                        // (four runs a lane: no registers for two rows)
-    long long row = (long long)blockIdx.x * R + (int)threadIdx.x / L;
-    if (AHEAD && row < a.P)
-        load(row);
+    long long base = (long long)blockIdx.x * R;
+    if (AHEAD)
+        load(base + first);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+        mask[j] = Mask8<T>(n);
         if (gamma != nullptr)
-            gm[j] = load8<T, WHOLE>(gamma + c, n, n < 8);
+            gm[j] = load8<T, WHOLE>(gamma + c, n, false);
         if (beta != nullptr)
-            bt[j] = load8<T, WHOLE>(beta + c, n, n < 8);
+            bt[j] = load8<T, WHOLE>(beta + c, n, false);
     }
-    for (; row < a.P; row += stride) {
-        const long long at = row * a.C;
+    for (; base < a.P; base += stride) {                   // (the whole workgroup, for the barriers of wide rows)
+        const long long row = base + first, at = row * a.C;
+        const bool live = row < a.P;
         if (!AHEAD)
             load(row);
         float v[NV][8], s[1] = {0.f};
-        Bits8 bits[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            unpack<T, WHOLE>(x[j], a.C - run_of<L, NV>(l, j) * 8, v[j]);
         float r[BRANCH ? NV : 1][8];
-        if constexpr (BRANCH)
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                unpack<T, WHOLE>(res[j], a.C - run_of<L, NV>(l, j) * 8, r[j]);
-        if (AHEAD && row + stride < a.P)
+        for (int j = 0; j < NV; ++j) {
+            unpack<T, WHOLE>(x[j], mask[j], v[j]);
+            if constexpr (BRANCH)
+                unpack<T, WHOLE>(res[j], mask[j], r[j]);
+        }
+        if (AHEAD)
             load(row + stride);
         if constexpr (BRANCH) {
+            Bits8 bits[NV];
             row_bits<L, NV, WHOLE>(bits, (unsigned long long)at, a.C, l, offset, a.drop);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+                const int c = run_of<L, NV>(l, j) * 8;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[j][e] = (WHOLE ? n > 0 : e < n) ? (float)(T)drop_apply<WHOLE>(bits[j], e, a.drop, v[j][e], r[j][e]) : 0.f;
-                store8<T, WHOLE>((T *)a.z + at + c, n, v[j]);
+                for (int e = 0; e < 8; ++e)                // (zeros behind the row: of the sum of two of them)
+                    v[j][e] = (float)(T)drop_apply<WHOLE>(bits[j], e, a.drop, v[j][e], r[j][e]);
+                store8<T, WHOLE>((T *)a.z + at + c, live ? a.C - c : 0, v[j]);
             }
         }
 #pragma unroll
@@ -343,7 +373,7 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_kernel(NormArgs a)
         }
         row_sums<L, 1>(s, lds);
         const float rstd = 1.f / __builtin_sqrtf(__builtin_fmaf(s[0], a.inv_c, a.eps));
-        if (l == 0) {
+        if (l == 0 && live) {
             if (a.mean != nullptr)
                 a.mean[row] = mean;
             if (a.rstd != nullptr)
@@ -361,7 +391,7 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_kernel(NormArgs a)
                 else if (beta != nullptr)
                     y[e] += (float)bt[j][e];
             }
-            store8<T, WHOLE>((T *)a.y + at + c, a.C - c, y);
+            store8<T, WHOLE>((T *)a.y + at + c, live ? a.C - c : 0, y);
         }
     }
 }
@@ -376,7 +406,7 @@ template <typename T, int L, int NV, bool BRANCH, bool WHOLE>
 __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(NormBackArgs a)
 {
     constexpr int R = norm_threads(L) / L;
-    __shared__ float lds[L > 64 ? L / 64 : 1][2];
+    __shared__ float lds[norm_threads(L) / 64][2];
     __shared__ float sums[R > 1 ? norm_threads(L) * 8 : 1];
     const int l = (int)threadIdx.x % L, first = (int)threadIdx.x / L;
     const T *gamma = (const T *)a.gamma;
@@ -388,34 +418,38 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
         for (int e = 0; e < 8; ++e)
             dg[j][e] = db[j][e] = 0.f;
     const long long all = a.P * a.C, stride = (long long)gridDim.x * R;
-    constexpr bool AHEAD = NV <= 2;                        // (four runs a lane: no registers for two rows, gamma and grad_z)
+    constexpr bool AHEAD = NV <= 2;                        // (else no registers for two rows, gamma and grad_z)
     Raw8<T> x[NV], gy[NV], gz[BRANCH && AHEAD ? NV : 1], gm[AHEAD ? NV : 1];
+    Mask8<T> mask[NV];
     float mean = 0.f, rstd = 0.f;
-    auto load = [&](long long row) {
-        mean = a.mean[row];
-        rstd = a.rstd[row];
+    auto load = [&](long long row) {                       // (a row past the last: nothing)
+        const bool safe = (row + 1) * a.C + 7 <= all;
+        mean = row < a.P ? a.mean[row] : 0.f;
+        rstd = row < a.P ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            const int c = run_of<L, NV>(l, j) * 8, n = row < a.P ? a.C - c : 0;
             const long long at = row * a.C + c;
-            x[j] = load8<T, WHOLE>((const T *)a.x + at, n, all - at < 8);
-            gy[j] = load8<T, WHOLE>((const T *)a.grad_y + at, n, all - at < 8);
+            x[j] = load8<T, WHOLE>((const T *)a.x + at, n, safe);
+            gy[j] = load8<T, WHOLE>((const T *)a.grad_y + at, n, safe);
             if constexpr (BRANCH && AHEAD)
                 if (a.grad_z != nullptr)
-                    gz[j] = load8<T, WHOLE>((const T *)a.grad_z + at, n, all - at < 8);
+                    gz[j] = load8<T, WHOLE>((const T *)a.grad_z + at, n, safe);
         }
     };
-    long long row = (long long)blockIdx.x * R + first;
-    if (AHEAD && row < a.P)
-        load(row);
-    if (AHEAD && gamma != nullptr)
+    long long base = (long long)blockIdx.x * R;
+    if (AHEAD)
+        load(base + first);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
-            gm[AHEAD ? j : 0] = load8<T, WHOLE>(gamma + c, n, n < 8);
-        }
-    for (; row < a.P; row += stride) {
-        const long long at = row * a.C;
+    for (int j = 0; j < NV; ++j) {
+        const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+        mask[j] = Mask8<T>(n);
+        if (AHEAD && gamma != nullptr)
+            gm[AHEAD ? j : 0] = load8<T, WHOLE>(gamma + c, n, false);
+    }
+    for (; base < a.P; base += stride) {                   // (the whole workgroup, for the barriers of wide rows)
+        const long long row = base + first, at = row * a.C;
+        const bool live = row < a.P;
         if constexpr (!AHEAD) {
             load(row);
             asm volatile("" : "+s"(a.C));                  // (what follows from C is worked out again: kept, it would fill the registers)
@@ -425,29 +459,30 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
-            unpack<T, WHOLE>(x[j], n, xh[j]);
-            unpack<T, WHOLE>(gy[j], n, g[j]);
+            unpack<T, WHOLE>(x[j], mask[j], xh[j]);
+            unpack<T, WHOLE>(gy[j], mask[j], g[j]);
             if constexpr (BRANCH && AHEAD) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     r[j][e] = 0.f;
                 if (a.grad_z != nullptr)
-                    unpack<T, WHOLE>(gz[j], n, r[j]);
+                    unpack<T, WHOLE>(gz[j], mask[j], r[j]);
             }
             if (!AHEAD && gamma != nullptr)
-                gm[0] = load8<T, WHOLE>(gamma + c, n, n < 8);
+                gm[0] = load8<T, WHOLE>(gamma + c, n, false);
+            // (behind the row grad_y is zero, and so is every sum's term)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[j][e] = (WHOLE ? n > 0 : e < n) ? (xh[j][e] - mean) * rstd : 0.f;
+                xh[j][e] = (xh[j][e] - mean) * rstd;
                 dg[j][e] = __builtin_fmaf(g[j][e], xh[j][e], dg[j][e]);
                 db[j][e] += g[j][e];
                 if (gamma != nullptr)
-                    g[j][e] = (WHOLE ? n > 0 : e < n) ? g[j][e] * (float)gm[AHEAD ? j : 0][e] : 0.f;
+                    g[j][e] *= (float)gm[AHEAD ? j : 0][e];
                 s[0] += g[j][e];
                 s[1] = __builtin_fmaf(g[j][e], xh[j][e], s[1]);
             }
         }
-        if (AHEAD && row + stride < a.P)
+        if (AHEAD)
             load(row + stride);
         row_sums<L, 2>(s, lds);
         const float m0 = s[0] * a.inv_c, m1 = s[1] * a.inv_c;
@@ -458,7 +493,7 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
         for (int j = 0; j < NV; ++j) {
             if constexpr (!AHEAD)
                 __builtin_amdgcn_sched_barrier(0);         // (one run after the other)
-            const int c = run_of<L, NV>(l, j) * 8, n = a.C - c;
+            const int c = run_of<L, NV>(l, j) * 8, n = live ? a.C - c : 0;
             float out[8];
             if constexpr (BRANCH && !AHEAD) {
                 const unsigned long long i = (unsigned long long)(at + c);
@@ -469,7 +504,7 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
                 for (int e = 0; e < 8; ++e)
                     r[0][e] = 0.f;
                 if (a.grad_z != nullptr)
-                    unpack<T, WHOLE>(load8<T, WHOLE>((const T *)a.grad_z + at + c, n, all - at - c < 8), n, r[0]);
+                    unpack<T, WHOLE>(load8<T, WHOLE>((const T *)a.grad_z + at + c, n, (row + 1) * a.C + 7 <= all), mask[j], r[0]);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -512,18 +547,21 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
                     if constexpr (G < 32) v[e] = add_rows(v[e]);
                     if constexpr (G < 64) v[e] = add_halves(v[e]);
                 }
+                // then the waves: all of them (rows of a wave and less), or those with the same part of a row
+                constexpr int PARTS = L < 64 ? 1 : L / 64;
+                const int wave = (int)threadIdx.x >> 6, in = l % G;
                 __syncthreads();                           // all have read what was there before
                 if ((int)(threadIdx.x & 63) < G)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        sums[((int)(threadIdx.x >> 6) * 8 + e) * G + l] = v[e];
+                        sums[(wave * 8 + e) * G + in] = v[e];
                 __syncthreads();
                 if (first == 0)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
 #pragma unroll
-                        for (int w = 1; w < W; ++w)
-                            v[e] += sums[(w * 8 + e) * G + l];
+                        for (int w = PARTS; w < W; w += PARTS)
+                            v[e] += sums[((w + wave) * 8 + e) * G + in];
             }
             if (first == 0)
 #pragma unroll
@@ -577,9 +615,9 @@ __global__ __launch_bounds__(256) void dcnv4_dropout_kernel(const T *__restrict_
                 if (ADD)
                     r[k] = load8<T, true>(residual + i, 8, false);
             } else if (left > 0) {
-                v[k] = load8<T, false>(x + i, (int)left, true);
+                v[k] = load8<T, false>(x + i, (int)left, false);
                 if (ADD)
-                    r[k] = load8<T, false>(residual + i, (int)left, true);
+                    r[k] = load8<T, false>(residual + i, (int)left, false);
             }
         }
 #pragma unroll
@@ -605,7 +643,7 @@ namespace {
 // Rows wider than this are refused: 512 lanes with four runs of eight each.
 constexpr int kNormMaxChannels = 16384;
 // Workgroups of the backward pass, each of which leaves partial sums of 2 * C: as many as memory needs for its rate, fewer for
-// wide rows, where the partial sums would be a good part of what is moved (8192 fp16 channels, 2048 rows: 94 us with 1024 workgroups).
+// wide rows, where the partial sums would be a good part of what is moved (8192 fp16 channels, 2048 rows: 94 us with 1024 workgroups, 38 so).
 int norm_back_most(int C) { return C <= 512 ? 1024 : C <= 2048 ? 512 : 256; }
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -634,8 +672,10 @@ int check_rows(long long P, int C, int dtype)
 }
 
 // Calls f with the lanes of a row and a lane's runs of eight channels, as constants: the fewest lanes that hold the row with one run each,
-// up to a wave; with two up to 1024 channels, then whole workgroups.
-template <typename F> int by_width(int C, F &&f)
+// up to a wave; with two up to 1024 channels, then two, four and eight waves.  (Two rows side by side in a workgroup of four
+// waves each rather than eight waves with one run: twice the loads on their way.)  Forward, up to 1536 channels: three runs and no
+// barriers (16368 x 1025 fp16: 20 us, by two waves 28; backward, whose sums leave it no registers to load ahead, 41 and 44, 11184 x 1500 42 and 35).
+template <bool BACK, typename F> int by_width(int C, F &&f)
 {
     const int runs = (C + 7) / 8;
     if (runs <= 1) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
@@ -646,8 +686,10 @@ template <typename F> int by_width(int C, F &&f)
     if (runs <= 32) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
     if (runs <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     if (runs <= 128) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    if (runs <= 256) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    if (runs <= 512) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+    if constexpr (!BACK)
+        if (runs <= 192) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 3>());
+    if (runs <= 256) return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>());
+    if (runs <= 512) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
     if (runs <= 1024) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
 }
@@ -655,7 +697,7 @@ template <typename F> int by_width(int C, F &&f)
 int norm_back_groups(long long P, int C)
 {
     int groups = 0;
-    by_width(C, [&](auto L, auto) {
+    by_width<true>(C, [&](auto L, auto) {
         const long long rows = norm_threads(L()) / L(), n = (P + rows - 1) / rows;
         // (eight rows a lane at least where that leaves every unit a workgroup)
         const long long enough = n / 8 > 256 ? n / 8 : 256, most = norm_back_most(C);
@@ -670,7 +712,7 @@ template <typename T, bool BRANCH> int launch_norm(const NormArgs &a, hipStream_
     const int cus = device_cus();
     if (cus <= 0)
         return DCNV4_ERR_LAUNCH;
-    return by_width(a.C, [&](auto L, auto NV) {
+    return by_width<false>(a.C, [&](auto L, auto NV) {
         constexpr int threads = norm_threads(L());
         const long long rows = threads / L(), groups = (a.P + rows - 1) / rows, most = (long long)(2048 / threads) * cus;
         const dim3 grid((unsigned)(groups < most ? groups : most));
@@ -685,7 +727,7 @@ template <typename T, bool BRANCH> int launch_norm(const NormArgs &a, hipStream_
 template <typename T, bool BRANCH> int launch_norm_backward(const NormBackArgs &a, void *grad_gamma, void *grad_beta, hipStream_t s)
 {
     const int groups = norm_back_groups(a.P, a.C);
-    const int rc = by_width(a.C, [&](auto L, auto NV) {
+    const int rc = by_width<true>(a.C, [&](auto L, auto NV) {
         constexpr int threads = norm_threads(L());
         if (a.C % 8 == 0)
             hipLaunchKernelGGL((dcnv4_norm_backward_kernel<T, L(), NV(), BRANCH, true>), dim3((unsigned)groups), dim3(threads), 0, s, a);
