@@ -782,7 +782,7 @@ enum { kSmall, kMiddle, kLarge };
 
 // The work is planned for this many compute units (the plan gives the size of the workspace, without a device).
 constexpr int kUnits = 256;
-constexpr int kFewRows = 2048;       // that every workgroup looks through by itself
+constexpr int kFewRows = 512;        // that every workgroup looks through by itself (2000: as long as the launch it saves)
 constexpr int kLossMaxRows = 1 << 20, kLossMaxClasses = 1 << 22;
 // Classes of a piece: d takes P * classes numbers in each layout, this many at most.
 constexpr long long kPieceNumbers = 1ll << 27;

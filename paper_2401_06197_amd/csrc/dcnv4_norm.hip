@@ -675,7 +675,9 @@ int check_rows(long long P, int C, int dtype)
 // up to a wave; with two up to 1024 channels, then two, four and eight waves.  (Two rows side by side in a workgroup of four
 // waves each rather than eight waves with one run: twice the loads on their way.)  Forward, up to 1536 channels: three runs and no
 // barriers (16368 x 1025 fp16: 20 us, by two waves 28; backward, whose sums leave it no registers to load ahead, 41 and 44, 11184 x 1500 42 and 35).
-template <bool BACK, typename F> int by_width(int C, F &&f)
+// Up to 4096 channels in fp32 eight waves with one run after all (4096 x 4096: branch end 50.6 and 71 us, with two 56 and 76; fp16 31.7 and 41,
+// with two 29.7 and 42, norm backward 30.3 and 28.9).
+template <typename T, bool BACK, typename F> int by_width(int C, F &&f)
 {
     const int runs = (C + 7) / 8;
     if (runs <= 1) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
@@ -689,18 +691,18 @@ template <bool BACK, typename F> int by_width(int C, F &&f)
     if constexpr (!BACK)
         if (runs <= 192) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 3>());
     if (runs <= 256) return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>());
-    if (runs <= 512) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    if (runs <= 512) return f(std::integral_constant<int, sizeof(T) == 2 ? 256 : 512>(), std::integral_constant<int, sizeof(T) == 2 ? 2 : 1>());
     if (runs <= 1024) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
 }
 
-int norm_back_groups(long long P, int C)
+template <typename T> int norm_back_groups(long long P, int C)
 {
     int groups = 0;
-    by_width<true>(C, [&](auto L, auto) {
+    by_width<T, true>(C, [&](auto L, auto) {
         const long long rows = norm_threads(L()) / L(), n = (P + rows - 1) / rows;
-        // (eight rows a lane at least where that leaves every unit a workgroup)
-        const long long enough = n / 8 > 256 ? n / 8 : 256, most = norm_back_most(C);
+        // (four rows a lane at least, where that leaves every unit two workgroups)
+        const long long enough = n / 4 > 512 ? n / 4 : 512, most = norm_back_most(C);
         groups = (int)(n < enough ? n : enough < most ? enough : most);
         return 0;
     });
@@ -712,7 +714,7 @@ template <typename T, bool BRANCH> int launch_norm(const NormArgs &a, hipStream_
     const int cus = device_cus();
     if (cus <= 0)
         return DCNV4_ERR_LAUNCH;
-    return by_width<false>(a.C, [&](auto L, auto NV) {
+    return by_width<T, false>(a.C, [&](auto L, auto NV) {
         constexpr int threads = norm_threads(L());
         const long long rows = threads / L(), groups = (a.P + rows - 1) / rows, most = (long long)(2048 / threads) * cus;
         const dim3 grid((unsigned)(groups < most ? groups : most));
@@ -726,8 +728,8 @@ template <typename T, bool BRANCH> int launch_norm(const NormArgs &a, hipStream_
 
 template <typename T, bool BRANCH> int launch_norm_backward(const NormBackArgs &a, void *grad_gamma, void *grad_beta, hipStream_t s)
 {
-    const int groups = norm_back_groups(a.P, a.C);
-    const int rc = by_width<true>(a.C, [&](auto L, auto NV) {
+    const int groups = norm_back_groups<T>(a.P, a.C);
+    const int rc = by_width<T, true>(a.C, [&](auto L, auto NV) {
         constexpr int threads = norm_threads(L());
         if (a.C % 8 == 0)
             hipLaunchKernelGGL((dcnv4_norm_backward_kernel<T, L(), NV(), BRANCH, true>), dim3((unsigned)groups), dim3(threads), 0, s, a);
@@ -841,7 +843,9 @@ long long dcnv4_layer_norm_workspace_bytes(long long P, int C)
 {
     if (P < 1 || C < 1 || C > kNormMaxChannels)
         return -1;
-    return (long long)align256((size_t)norm_back_groups(P, C) * 2 * (size_t)C * 4);
+    // (either type's)
+    const int f32 = norm_back_groups<float>(P, C), f16 = norm_back_groups<_Float16>(P, C);
+    return (long long)align256((size_t)(f32 > f16 ? f32 : f16) * 2 * (size_t)C * 4);
 }
 
 int dcnv4_dropout(const void *x, const void *residual, void *y, long long n, float p, unsigned long long seed,
