@@ -539,15 +539,26 @@ def _outputs(x, out, specs):
     return out
 
 
-def _workspace(x, workspace, need):
-    """(workspace, bytes): the caller's, or a new one."""
+def _workspace(x, workspace, need, stream):
+    """(workspace, bytes): the caller's, or a new one.  A new one is of the stream that the call runs on: it is given back when the call
+    returns, and only what comes later on that stream may have it."""
     import torch
     if workspace is None:
         need = max(need, 16)
-        return torch.empty(need, dtype=torch.uint8, device=x.device), need
+        if stream is None:
+            return torch.empty(need, dtype=torch.uint8, device=x.device), need
+        with torch.cuda.stream(stream):
+            return torch.empty(need, dtype=torch.uint8, device=x.device), need
     if workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         raise ValueError("dcnv4: workspace must be a contiguous tensor on x's device")
     return workspace, workspace.nbytes
+
+
+def _prepared(args, *held):
+    """The arguments alone (prepare_only), whose tensors the caller has to hold."""
+    if any(t is None for t in held):
+        raise ValueError("dcnv4: prepare_only needs out, and a workspace where there is one")
+    return args
 
 
 _MASK64 = 2 ** 64 - 1
@@ -582,7 +593,7 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
             None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, float(eps), _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out)
     _call(x.device, "dcnv4_layer_norm", args)
     return (y, mean, rstd) if stats else y
 
@@ -598,16 +609,16 @@ def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=
     _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
     if gamma is None:
         (gx, gg, gb), size = _outputs(x, out, (("grad_x", shape, dt), None, None)), 0
-        workspace = None
+        space = None
     else:
         gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
-        workspace, size = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0)
+        space, size = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), ptr(gx), None if gg is None else ptr(gg),
-            None if gb is None else ptr(gb), None if workspace is None else ptr(workspace), size, P, C, _dtype_code(x),
+            None if gb is None else ptr(gb), None if space is None else ptr(space), size, P, C, _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out, *(() if gamma is None else (workspace,)))
     _call(x.device, "dcnv4_layer_norm_backward", args)
     return gx, gg, gb
 
@@ -622,7 +633,7 @@ def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, ou
     args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64,
             _offset_ptr(x, offset_on_device), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out)
     _call(x.device, "dcnv4_dropout", args)
     return y
 
@@ -635,7 +646,7 @@ def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out
     args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(grad_y, offset_on_device),
             _dtype_code(grad_y), _stream_ptr(stream, grad_y.device))
     if prepare_only:
-        return args
+        return _prepared(args, out)
     _call(grad_y.device, "dcnv4_dropout_backward", args)
     return gx
 
@@ -654,7 +665,7 @@ def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, of
             ptr(rstd), P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(x, offset_on_device), float(eps), _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out)
     _call(x.device, "dcnv4_dropout_add_layer_norm", args)
     return z, y, mean, rstd
 
@@ -672,16 +683,16 @@ def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed,
     specs = (("grad_x", shape, dt), ("grad_residual", shape, dt))
     if gamma is None:
         (gx, gr, gg, gb), size = _outputs(z, out, specs + (None, None)), 0
-        workspace = None
+        space = None
     else:
         gx, gr, gg, gb = _outputs(z, out, specs + (("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
-        workspace, size = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0)
+        space, size = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(z), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), None if grad_z is None else ptr(grad_z), ptr(gx),
-            ptr(gr), None if gg is None else ptr(gg), None if gb is None else ptr(gb), None if workspace is None else ptr(workspace), size,
+            ptr(gr), None if gg is None else ptr(gg), None if gb is None else ptr(gb), None if space is None else ptr(space), size,
             P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(z, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
     if prepare_only:
-        return args
+        return _prepared(args, out, *(() if gamma is None else (workspace,)))
     _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
     return gx, gr, gg, gb
 
@@ -690,7 +701,7 @@ def dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dtype, backward):
     return int(load_library().dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dtype, int(bool(backward))))
 
 
-def _loss_args(x, w, target, b, workspace, backward):
+def _loss_args(x, w, target, b, workspace, backward, stream):
     import torch
     P, K = _rows(x)
     if w.dim() != 2 or w.shape[1] != K:
@@ -699,21 +710,21 @@ def _loss_args(x, w, target, b, workspace, backward):
     _check_like(x, (("w", w, w.shape), ("b", b, (V,))))
     _check_plain("target", target, x.get_device(), x.shape[:-1], torch.int64)
     need = dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, _dtype_code(x), backward) if workspace is None else 0
-    return P, K, V, *_workspace(x, workspace, need)
+    return P, K, V, *_workspace(x, workspace, need, stream)
 
 
 def dcnv4_linear_cross_entropy(x, w, target, b=None, ignore_index=-100, workspace=None, out=None, stream=None, prepare_only=False):
     """(loss, lse), float32 [...]: loss = lse - logit[target] with logits x w^T + b that are never stored.  x [..., K], w [V, K],
     target [...] int64; rows whose target is ignore_index have loss 0."""
     import torch
-    P, K, V, workspace, size = _loss_args(x, w, target, b, workspace, False)
+    P, K, V, space, size = _loss_args(x, w, target, b, workspace, False, stream)
     stat, f32 = x.shape[:-1], torch.float32
     loss, lse = _outputs(x, out, (("loss", stat, f32), ("lse", stat, f32)))
     ptr = torch.Tensor.data_ptr
-    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(workspace), size, P, K, V, int(ignore_index),
+    args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(space), size, P, K, V, int(ignore_index),
             _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out, workspace)
     _call(x.device, "dcnv4_linear_cross_entropy", args)
     return loss, lse
 
@@ -722,15 +733,15 @@ def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ig
                                         prepare_only=False):
     """(grad_x, grad_w, grad_b) of dcnv4_linear_cross_entropy for grad_loss [...] float32, from its lse; grad_b is None where b is."""
     import torch
-    P, K, V, workspace, size = _loss_args(x, w, target, b, workspace, True)
+    P, K, V, space, size = _loss_args(x, w, target, b, workspace, True, stream)
     shape, dt, at = x.shape, x.dtype, x.get_device()
     _check_plain("lse", lse, at, shape[:-1], torch.float32)
     _check_plain("grad_loss", grad_loss, at, shape[:-1], torch.float32)
     gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_w", w.shape, dt), None if b is None else ("grad_b", (V,), dt)))
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(lse), ptr(grad_loss), ptr(gx), ptr(gw), None if gb is None else ptr(gb),
-            ptr(workspace), size, P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
+            ptr(space), size, P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
-        return args
+        return _prepared(args, out, workspace)
     _call(x.device, "dcnv4_linear_cross_entropy_backward", args)
     return gx, gw, gb

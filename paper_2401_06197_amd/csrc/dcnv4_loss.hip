@@ -795,6 +795,8 @@ constexpr long long kPieceNumbers = 1ll << 27;
 constexpr long long kMaxPiece = 1 << 20;                   // (256 rows of d, in three planes, stay below 2 GiB)
 // ... and fp32 weights, split, this many
 constexpr long long kPieceWeights = 1ll << 27;
+// Logits of a launch: a grid has fewer than 2^32 lanes, and the smallest tile's make 16 logits each.
+constexpr long long kLaunchLogits = 1ll << 35;
 
 struct Shape {
     int bm, bn, r;                     // classes (or columns of a result), pixels (or its rows), numbers of a step
@@ -891,6 +893,7 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
     most = most < 256 ? 256 : most > kMaxPiece ? kMaxPiece : most;
     if (p.pl == 1 && !backward)
         most = V;                                          // (nothing of a piece is kept)
+    most = most < kLaunchLogits / P ? most : kLaunchLogits / P;
     p.pieces = (int)((V + most - 1) / most);
     p.vc = (int)round_up((V + p.pieces - 1) / p.pieces, 256);
     p.vc = p.vc < V ? p.vc : V;

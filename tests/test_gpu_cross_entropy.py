@@ -345,3 +345,57 @@ def test_one_vector_and_maps():
     assert gx.shape == (2, 3, 5, 32) and torch.equal(gx.view(30, 32), dcn.dcnv4_linear_cross_entropy_backward(x, w, t, lse, g, b)[0])
     one = dcn.dcnv4_linear_cross_entropy(x[0].clone(), w, t[0].clone(), b)
     assert one[0].shape == () and abs(one[0].item() - loss[0].item()) <= 1e-5
+
+
+def test_more_logits_than_a_grid_has_lanes_for():
+    """2^20 rows and 700001 classes: more than 2^39 logits, in several launches.  A row's sum has 2735 tiles, 171 of them one after the other and
+    16 more joins, each within 3 * 2^-22 (two exponentials, a product, a sum): 2^-12.8 in all."""
+    P, K, V = 2 ** 20, 16, 700001
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(8)
+    x = torch.randn((P, K), generator=gen, device="cuda").half()
+    w = torch.randn((V, K), generator=gen, device="cuda").half()
+    t = torch.randint(0, V, (P,), generator=gen, device="cuda")
+    t[-1] = V - 1
+    loss, lse = dcn.dcnv4_linear_cross_entropy(x, w, t)
+    rows = [0, 1, 255, 256, P // 2 - 1, P // 2, P - 257, P - 1]
+    want = expected(x[rows], w, None, t[rows], torch.ones(len(rows), device="cuda"))
+    for name, got in (("loss", loss), ("lse", lse)):
+        ref, slack = want[name]
+        close(name, got[rows], (ref, slack + 2.0 ** -12.8), "f32")
+
+
+def test_workspaces_are_of_the_stream_of_the_call():
+    """A call on a stream that is handed over, which has other work to do first: what the current stream allocates and writes after the
+    call's return stays as it is."""
+    x, w, b, t, g = inputs(700, 64, 500, "f16", 9)
+    P, K, V = 700, 64, 500
+    s = torch.cuda.Stream()
+    want = dcn.dcnv4_linear_cross_entropy(x, w, t, b)
+    back = dcn.dcnv4_linear_cross_entropy_backward(x, w, t, want[1], g, b)
+    m = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(4):
+            m @ m
+    got = dcn.dcnv4_linear_cross_entropy(x, w, t, b, stream=s)
+    after = [torch.full((dcn.dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dcn.DCNV4_F16, False),), 7, dtype=torch.uint8, device="cuda")]
+    got_back = dcn.dcnv4_linear_cross_entropy_backward(x, w, t, want[1], g, b, stream=s)
+    after.append(torch.full((dcn.dcnv4_linear_cross_entropy_workspace_bytes(P, K, V, dcn.DCNV4_F16, True),), 7, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    assert all(bool((a == 7).all()) for a in after)
+    assert all(torch.equal(a, c) for a, c in zip((*got, *got_back), (*want, *back)))
+
+
+def test_prepared_arguments_need_their_tensors():
+    x, w, b, t, g = inputs(40, 32, 50, "f16", 10)
+    loss, lse = out = dcn.dcnv4_linear_cross_entropy(x, w, t, b)
+    work = torch.empty(dcn.dcnv4_linear_cross_entropy_workspace_bytes(40, 32, 50, dcn.DCNV4_F16, True), dtype=torch.uint8, device="cuda")
+    for kw in ({}, {"out": out}, {"workspace": work}):
+        with pytest.raises(ValueError):
+            dcn.dcnv4_linear_cross_entropy(x, w, t, b, prepare_only=True, **kw)
+    new = tuple(torch.zeros_like(o) for o in out)
+    args = dcn.dcnv4_linear_cross_entropy(x, w, t, b, out=new, workspace=work, prepare_only=True)
+    assert dcn.load_library().dcnv4_linear_cross_entropy(*args) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(new[0], loss) and torch.equal(new[1], lse)

@@ -378,3 +378,45 @@ def test_one_parameter_gradient_alone():
     assert torch.equal(gb, both[2]) and torch.equal(gx, dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy)[0])
     a = dcn.dcnv4_dropout(x, np.float64(0.5), np.int64(-7), np.int32(3))
     assert torch.equal(a, dcn.dcnv4_dropout(x, 0.5, 2 ** 64 - 7, 3))
+
+
+def test_workspaces_are_of_the_stream_of_the_call():
+    """A call on a stream that is handed over, which has other work to do first: what the current stream allocates and writes after the
+    call's return stays as it is."""
+    P, C = 3000, 130
+    x, gy = torch.randn((P, C), device="cuda"), torch.randn((P, C), device="cuda")
+    gamma = torch.randn(C, device="cuda")
+    _, mean, rstd = dcn.dcnv4_layer_norm(x, gamma, stats=True)
+    norm = lambda **kw: dcn.dcnv4_layer_norm_backward(x, gamma, mean, rstd, gy, **kw)
+    branch = lambda **kw: dcn.dcnv4_dropout_add_layer_norm_backward(x, gamma, mean, rstd, gy, 0.3, 5, **kw)
+    m = torch.randn((4096, 4096), device="cuda")
+    s = torch.cuda.Stream()
+    for call in (norm, branch):
+        want = call()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(4):
+                m @ m
+        got = call(stream=s)
+        after = torch.full((dcn.dcnv4_layer_norm_workspace_bytes(P, C),), 7, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert bool((after == 7).all()) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_prepared_arguments_need_their_tensors():
+    x = torch.randn((8, 40), device="cuda")
+    gamma, stat = torch.ones(40, device="cuda"), torch.ones(8, device="cuda")
+    y = torch.empty_like(x)
+    for call in (lambda **kw: dcn.dcnv4_layer_norm(x, **kw), lambda **kw: dcn.dcnv4_dropout(x, 0.5, 1, **kw),
+                 lambda **kw: dcn.dcnv4_dropout_backward(x, 0.5, 1, **kw)):
+        with pytest.raises(ValueError):
+            call(prepare_only=True)
+        assert call(prepare_only=True, out=y)
+    with pytest.raises(ValueError):
+        dcn.dcnv4_layer_norm_backward(x, gamma, stat, stat, x, out=(y, gamma.clone(), gamma.clone()), prepare_only=True)
+    with pytest.raises(ValueError):
+        dcn.dcnv4_dropout_add_layer_norm(x, x, None, None, 0.1, 1, prepare_only=True)
+    args = dcn.dcnv4_layer_norm_backward(x, None, stat, stat, x, out=(y, None, None), prepare_only=True)
+    assert dcn.load_library().dcnv4_layer_norm_backward(*args) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(y, dcn.dcnv4_layer_norm_backward(x, None, stat, stat, x)[0])
