@@ -16,7 +16,7 @@
 //
 // What bounds it: many rows and classes, the matrix units and the power they draw: 8192 rows, 1024 features, 40009 classes, fp16, forward 630
 // to 740 us, backward 1990 to 2170 (0.93 to 1.1 PFLOP/s; with zeros for numbers, 4096 features, up to 1.73); 2000, 768, 10007, fp32, backward
-// 505 (1.1 PFLOP/s of bf16).  Few classes, the eight launches' beginnings and ends: 51200, 256, 150, fp16, 16 and 71.  Few rows, latency:
+// 505 (1.1 PFLOP/s of bf16).  Few classes, the seven launches' beginnings and ends: 51200, 256, 150, fp16, 16 and 68.  Few rows, latency:
 // 64, 1024, 1000, fp16, 10 and 24.
 #include <math.h>
 #include <string.h>
@@ -739,14 +739,47 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     }
 }
 
-// Adds up the splits' planes [splits][rows][cols] and rounds: four numbers a lane.
+// grad_b: the pixel runs' sums, added up.
+struct Bias {
+    const float *sums;                // [runs][count]
+    int runs, count, blocks;          // blocks: workgroups, none for no grad_b
+    void *grad_b;
+};
+
+// 16 classes to a workgroup of 256, 16 runs side by side.
+template <typename T> __device__ __forceinline__ void bias_of(const Bias &b, int block)
+{
+    __shared__ float part[16][17];
+    const int i = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4, c = block * 16 + i;
+    float s = 0.f;
+    if (c < b.count)
+#pragma unroll 8
+        for (int r = slice; r < b.runs; r += 16)
+            s += b.sums[(long long)r * b.count + c];
+    part[slice][i] = s;
+    __syncthreads();
+    if (slice != 0 || c >= b.count)
+        return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k)
+        s += part[k][i];
+    ((T *)b.grad_b)[c] = (T)s;
+}
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_loss_bias_kernel(Bias b) { bias_of<T>(b, (int)blockIdx.x); }
+
+// Adds up the splits' planes [splits][rows][cols] and rounds: four numbers a lane.  The first workgroups make grad_b, where that saves it a
+// launch of its own (51200 x 256, 150 classes backward 70.6 -> 68.1 us).
 template <typename T>
 __global__ __launch_bounds__(256) void dcnv4_loss_sum_kernel(const float *planes, long long plane, int splits, long long n, int cols,
-                                                             Result o)
+                                                             Result o, Bias b)
 {
+    if ((int)blockIdx.x < b.blocks) {
+        bias_of<T>(b, (int)blockIdx.x);
+        return;
+    }
     const float scale = o.factor * (o.scale != nullptr ? o.scale[0] : 1.f);
-    const int units = cols / 4;
-    for (long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x; i < n / 4; i += (long long)gridDim.x * 256) {
+    const int units = cols / 4, block = (int)blockIdx.x - b.blocks, blocks = (int)gridDim.x - b.blocks;
+    for (long long i = (long long)block * 256 + (int)threadIdx.x; i < n / 4; i += (long long)blocks * 256) {
         f32x4 v = *reinterpret_cast<const f32x4 *>(planes + i * 4);
 #pragma unroll 8
         for (int s = 1; s < splits; ++s)
@@ -758,27 +791,6 @@ __global__ __launch_bounds__(256) void dcnv4_loss_sum_kernel(const float *planes
             t[e] = (T)(v[e] * by);
         __builtin_memcpy(__builtin_assume_aligned((T *)o.out + i * 4, 4 * sizeof(T)), t, sizeof(t));
     }
-}
-
-// grad_b: the pixel runs' sums, added up: 64 classes to a workgroup, 16 runs side by side.
-template <typename T>
-__global__ __launch_bounds__(1024) void dcnv4_loss_bias_kernel(const float *sums, int runs, int count, T *grad_b)
-{
-    __shared__ float part[16][64];
-    const int i = (int)threadIdx.x & 63, slice = (int)threadIdx.x >> 6, c = (int)blockIdx.x * 64 + i;
-    float s = 0.f;
-    if (c < count)
-#pragma unroll 8
-        for (int r = slice; r < runs; r += 16)
-            s += sums[(long long)r * count + c];
-    part[slice][i] = s;
-    __syncthreads();
-    if (slice != 0 || c >= count)
-        return;
-#pragma unroll
-    for (int k = 1; k < 16; ++k)
-        s += part[k][i];
-    grad_b[c] = (T)s;
 }
 
 namespace {
@@ -1033,11 +1045,11 @@ void launch_product(const Product &q, const Choice &c, bool planes, const Result
     });
 }
 
-template <typename T> void sum_planes(const void *planes, int splits, long long rows, int cols, const Result &o, hipStream_t s)
+template <typename T> void sum_planes(const void *planes, int splits, long long rows, int cols, const Result &o, const Bias &b, hipStream_t s)
 {
     const long long n = rows * cols, groups = (n / 4 + 255) / 256;
-    hipLaunchKernelGGL((dcnv4_loss_sum_kernel<T>), dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, (const float *)planes, n, splits,
-                       n, cols, o);
+    hipLaunchKernelGGL((dcnv4_loss_sum_kernel<T>), dim3((unsigned)((groups < 8192 ? groups : 8192) + b.blocks)), dim3(256), 0, s,
+                       (const float *)planes, n, splits, n, cols, o, b);
 }
 
 template <typename T, int PL>
@@ -1075,9 +1087,11 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
                                dim3(G::WR * G::WC * 64), 0, s, q, l, d);
             return 0;
         });
+        Bias bias = {};
         if (grad_b != nullptr)
-            hipLaunchKernelGGL((dcnv4_loss_bias_kernel<T>), dim3((unsigned)((l.count + 63) / 64)), dim3(1024), 0, s, (const float *)d.bias_sums, runs,
-                               l.count, (T *)grad_b + l.v0);
+            bias = {d.bias_sums, runs, l.count, (l.count + 15) / 16, (T *)grad_b + l.v0};
+        if (bias.blocks > 0 && !p.gw_planes)
+            hipLaunchKernelGGL((dcnv4_loss_bias_kernel<T>), dim3((unsigned)bias.blocks), dim3(256), 0, s, bias);
         // grad_x, over the pieces
         const Result ox = {grad_x, 0, g, nullptr, down, 0};
         const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), PL, p.gx);
@@ -1085,7 +1099,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
             const Result o = {ws + p.gx_at, (long long)p.P * p.K, nullptr, nullptr, 1.f, piece > 0};
             launch_product<T, PL, false>(qx, p.gx, true, o, s);
             if (piece == p.pieces - 1)
-                sum_planes<T>(ws + p.gx_at, p.gx.splits, p.P, p.K, ox, s);
+                sum_planes<T>(ws + p.gx_at, p.gx.splits, p.P, p.K, ox, Bias{}, s);
         } else {
             launch_product<T, PL, false>(qx, p.gx, false, ox, s);
         }
@@ -1095,7 +1109,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         if (p.gw_planes) {
             const Result o = {ws + p.gw_at, (long long)l.count * p.K, nullptr, nullptr, 1.f, 0};
             launch_product<T, PL, true>(qw, p.gw, true, o, s);
-            sum_planes<T>(ws + p.gw_at, p.gw.splits, l.count, p.K, ow, s);
+            sum_planes<T>(ws + p.gw_at, p.gw.splits, l.count, p.K, ow, bias, s);
         } else {
             launch_product<T, PL, true>(qw, p.gw, false, ow, s);
         }
