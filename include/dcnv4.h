@@ -285,7 +285,9 @@ int dcnv4_linear_cross_entropy(const void *x, const void *w, const void *b, cons
 /* Its backward pass, from the forward's lse and grad_loss fp32 [P].  With d = exp(logit - lse) - (v == target), a piece of the classes
  * at a time:
  *     grad_x[p] = grad_loss[p] * sum_v d[p][v] * w[v],   grad_w[v] = sum_p grad_loss[p] * d[p][v] * x[p],   grad_b[v] = sum_p grad_loss[p] * d[p][v]
- * In F16 d is rounded to fp16 (of 2^15 * d, for grad_w and grad_b times grad_loss / a power of two no less than the largest), sums are fp32.
+ * In F16 d is rounded to fp16 (of 2^15 * d) for grad_x and grad_w; grad_w's other operand, x * grad_loss / the largest |grad_loss|, is x itself
+ * where grad_loss is the same in all rows and is rounded to fp16 otherwise, to 2^-11 of it and 2^-17 of x = 1 for rows of down to 2^-32 of the
+ * largest (each power of two below doubles the latter).  Sums are fp32, grad_b is made from fp32 numbers alone.
  * A row that is ignored, or whose grad_loss is 0, counts for nothing and has grad_x 0, whatever x holds there; one with
  * loss NaN has grad_x NaN and makes grad_w NaN.  grad_b may be NULL.  Sums are made in a fixed order.
  * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 1) bytes. */

@@ -9,8 +9,13 @@
 // the LDS reads that transpose 4 x 16 numbers on their way to the registers, so no tensor is laid out a second time.
 // (With copies of w, x and d laid out the other way: 8192 rows, 1024 features, 40009 classes backward 2.3 ms, of which 0.35 in those.)
 //
-// fp16: d lies in [-1, 1] and a probability of 2^-24 is the least that fp16 holds, so it is stored times 2^15.  g goes into x as a part
-// of the largest |g|, so that any loss scale keeps its bits (and a g that is the same in all rows leaves x as it is).
+// fp16: d lies in [-1, 1] and a probability of 2^-24 is the least that fp16 holds, so it is stored times 2^15; it is rounded so once, to
+// half a step of fp16, for both products.  grad_x takes its row's g afterwards, in fp32.  In grad_w's sum rows meet, so g goes into x, as a part of
+// the largest |g|: where g is the same in all rows that leaves x as it is, else it is rounded to fp16 once more.  Rows of less than 2^-8 of the
+// largest lie in planes of x of their own, times 2^8, 2^16 or 2^24, so that no more than eight of x's powers of two go (half of fp16's least
+// step, 2^-25, is 2^-17 of such an x); the planes' products are added up in the same registers, from the smallest on.  Weights that are alike take
+// one plane.  (One plane for all: rows of 10^-6 of the largest kept x to 2 %, of 10^-8 not at all.  51200 x 256, 150 classes backward: one plane 71 us,
+// two 85, four 114; 8192 x 1024, 8192 classes 458, 559, 768.)
 // fp32: every operand is held as three bf16 numbers (8 + 8 + 8 bits, a = h + m + l) and a product is the sum of h*h, h*m, m*h, m*m,
 // h*l, l*h in fp32: what is left out is at most 2^-22 of a product.  (The fp32 matrix instructions have a sixteenth of the bf16 rate.)
 //
@@ -33,6 +38,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kUp = 32768.f, kDown = 1.f / 32768.f;     // what d is stored times, in fp16
+constexpr int kBands = 4, kBandBits = 8;                   // planes of x in fp16 grad_w, and the powers of two of each but the last
 
 // One operand of a product: `count` rows i (or j) and a sum over `length` numbers r, in planes.  As it is: row i at base + i * row_bytes, r
 // contiguous, length a multiple of eight.  Turned: row r at base + r * row_bytes, i contiguous, count a multiple of eight.
@@ -118,12 +124,12 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         rsrc_t r;
         unsigned out;
         int at;
-        __device__ __forceinline__ void step(int t, int t1)
+        __device__ __forceinline__ void step(int t, int t1, int band)
         {
             if constexpr (TURNED) {
                 // (from row t * R on; what lies past a row's end is the next one's, for rows of the result that are dropped)
                 const int left = t < t1 ? min(R, o.length - t * R) : 0;
-                r = make_rsrc(base + (long long)t * R * o.row_bytes, left <= 0 ? 0u : (unsigned)(left * o.row_bytes - (base - o.base)));
+                r = make_rsrc(base + ((long long)band * o.length + (long long)t * R) * o.row_bytes, left <= 0 ? 0u : (unsigned)(left * o.row_bytes - (base - o.base)));
                 out = 0u;
                 at = 0;
             } else {
@@ -157,10 +163,13 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         }
     }
 
-    // acc[m][n]: rows a0 + (wr * WM + m) * 32 of A, rows b0 + (wc * WN + n) * 32 of B, steps t0 to t1 - 1
+    // acc[m][n]: rows a0 + (wr * WM + m) * 32 of A, rows b0 + (wc * WN + n) * 32 of B, steps t0 to t1 - 1.  BANDED: these steps for each of
+    // `bands` A (turned), one behind the other, from the last to the first, each of which counts 2^kBandBits times what is behind it.
+    template <bool BANDED = false>
     static __device__ __forceinline__ void multiply(char *smem, const Operand &a, const Operand &b, int a0, int b0, int t0, int t1,
-                                                    f32x16 (&acc)[WM][WN])
+                                                    f32x16 (&acc)[WM][WN], int bands = 1)
     {
+        static_assert(!BANDED || TA);
         const int tid = (int)threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wr = wave / WC, wc = wave % WC;
@@ -223,10 +232,19 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         constexpr int EARLY = STAGES > 2 ? LOADS * (GROUPS - 1) / GROUPS : 0;          // of a step's loads, before its last group
         constexpr int FLYING = STAGES > 2 ? (STAGES - 3) * LOADS + EARLY : 0;          // that need not have landed there
         static_assert(GROUPS % 2 == 0 && STAGES > 1 && (AHEAD - 1) * LOADS < 64 && FLYING < 64);
+        int asked = t0, band = bands - 1;                  // the step, and its A, that is asked for next
+        auto ask = [&] {
+            sa.step(asked, t1, band);
+            sb.step(asked, t1, 0);
+            ++asked;
+            if (BANDED && asked >= t1 && band > 0) {
+                asked = t0;
+                --band;
+            }
+        };
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
-            sa.step(t0 + s, t1);
-            sb.step(t0 + s, t1);
+            ask();
 #pragma unroll
             for (int j = 0; j < LOADS; ++j)
                 load(j, s);
@@ -237,12 +255,11 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
 #pragma unroll
         for (int f = 0; f < PL * (WM + WN); ++f)
             fetch(smem, 0, f);
-        int at = 0;
+        int at = 0, left = bands - 1;                      // left: A after this one
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const int to = STAGES == 2 ? at : at == 0 ? STAGES - 1 : at - 1;
-            sa.step(t + AHEAD, t1);
-            sb.step(t + AHEAD, t1);
+            ask();
             const char *stage = smem + at * STAGE;
 #pragma unroll
             for (int g = 0; g + 1 < GROUPS; ++g)
@@ -253,6 +270,17 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
             asm volatile("" ::: "memory");
             at = at + 1 == STAGES ? 0 : at + 1;
             products(GROUPS - 1, smem + at * STAGE, 0, EARLY, LOADS, to);
+            if (BANDED && left > 0 && t + 1 == t1) {
+                --left;
+                t = t0 - 1;
+#pragma unroll
+                for (int m = 0; m < WM; ++m)
+#pragma unroll
+                    for (int n = 0; n < WN; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            acc[m][n][r] *= 1.f / (1 << kBandBits);
+            }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (results go where the last loads write)
         __syncthreads();
@@ -462,69 +490,110 @@ __global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *part
 }
 
 // What the backward pass knows of its rows beforehand: g per row (zero where the row is ignored, NaN where its target is no class), and
-// the largest |g| (of finite ones) of each 1024 rows.
+// the largest and least |g| (of finite ones that are not zero; 0 and infinity where there is none) of each 1024 rows.
 __device__ __forceinline__ float row_weight(const float *grad_loss, const Labels &l, long long px)
 {
     const long long t = l.target[px];
     return t == l.ignore ? 0.f : t >= 0 && t < l.V ? grad_loss[px] : __builtin_nanf("");
 }
-__device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
-
-__global__ __launch_bounds__(1024) void dcnv4_loss_rows_kernel(const float *grad_loss, Labels l, float *most, float *g)
+// The plane of a row in fp16 grad_w, from its g over the largest: [2^-8, 1], [2^-16, 2^-8), [2^-24, 2^-16), and what is less.  (Infinities and NaN:
+// the first.)
+__device__ __forceinline__ int band_of(float part)
 {
-    __shared__ float part[16];
-    const int px = (int)blockIdx.x * 1024 + (int)threadIdx.x;
-    float top = 0.f;
-    if (px < l.P) {
-        g[px] = row_weight(grad_loss, l, px);
-        top = finite_size(g[px]);
+    const int below = -__builtin_amdgcn_frexp_expf(part);  // (the part is less than 2^-below)
+    return below > 0 ? min(below / kBandBits, kBands - 1) : 0;
+}
+
+struct Sizes {
+    float most, least;
+    __device__ __forceinline__ void add(float g)
+    {
+        const float v = fabsf(g);
+        if (v > 0.f && v < __builtin_inff()) {
+            most = fmaxf(most, v);
+            least = fminf(least, v);
+        }
     }
+    __device__ __forceinline__ void join(Sizes o)
+    {
+        most = fmaxf(most, o.most);
+        least = fminf(least, o.least);
+    }
+    __device__ __forceinline__ void join_wave()
+    {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        top = fmaxf(top, __shfl_xor(top, d));
+        for (int d = 1; d < 64; d *= 2)
+            join({__shfl_xor(most, d), __shfl_xor(least, d)});
+    }
+};
+
+__global__ __launch_bounds__(1024) void dcnv4_loss_rows_kernel(const float *grad_loss, Labels l, Sizes *sizes, float *g)
+{
+    __shared__ Sizes part[16];
+    const int px = (int)blockIdx.x * 1024 + (int)threadIdx.x;
+    Sizes all = {0.f, __builtin_inff()};
+    if (px < l.P) {
+        const float v = row_weight(grad_loss, l, px);
+        g[px] = v;
+        all.add(v);
+    }
+    all.join_wave();
     if ((threadIdx.x & 63) == 0)
-        part[threadIdx.x >> 6] = top;
+        part[threadIdx.x >> 6] = all;
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int w = 1; w < 16; ++w)
-            top = fmaxf(top, part[w]);
-        most[blockIdx.x] = top;
+            all.join(part[w]);
+        sizes[blockIdx.x] = all;
     }
 }
 
+// What grad_w's product knows of all rows: what its sums are multiplied with in the end, and how many planes of x there are.
+struct Scale {
+    float by;
+    int bands;
+};
+
 // Rows as the products take them: in [rows][cols] -> out [rows][PL planes][pad], zeros behind the columns, fp32 numbers split into three.
-// With g: a row times g / scale, scale the largest |g| (1 if there is none), which goes to scale[0]; rows whose g is zero are
-// zeros, whatever they hold.  Few rows (parts = 0): g and the largest are made here too, a launch less.  Eight numbers a lane.
+// Scaled: a row times g / the largest |g|; fp16: out [bands][rows][pad], a row times 2^(kBandBits * band) too, in the plane of its band, zeros in
+// the others.  Rows whose g is zero are zeros, whatever they hold.  Few rows (parts = 0): g and the largest are made here too, a launch less.  Eight numbers a lane.
 template <typename T, int PL, bool SCALED>
 __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, long long rows, int cols, int pad, unsigned short *out,
-                                                                 float *g, const float *most, int parts, float *scale, const float *grad_loss, Labels l)
+                                                                 float *g, const Sizes *sizes, int parts, Scale *scale, const float *grad_loss, Labels l)
 {
     float inv = 1.f;
+    int bands = 1;
     if constexpr (SCALED) {
-        __shared__ float part[4];
-        float top = 0.f;
+        __shared__ Sizes part[4];
+        Sizes all = {0.f, __builtin_inff()};
         if (parts > 0)
             for (int i = (int)threadIdx.x; i < parts; i += 256)
-                top = fmaxf(top, most[i]);
+                all.join(sizes[i]);
         else
             for (int i = (int)threadIdx.x; i < l.P; i += 256)
-                top = fmaxf(top, finite_size(row_weight(grad_loss, l, i)));
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2)
-            top = fmaxf(top, __shfl_xor(top, d));
+                all.add(row_weight(grad_loss, l, i));
+        all.join_wave();
         if ((threadIdx.x & 63) == 0)
-            part[threadIdx.x >> 6] = top;
+            part[threadIdx.x >> 6] = all;
         __syncthreads();
-        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-        top = top > 0.f ? top : 1.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            all.join(part[w]);
+        if (all.most > 0.f) {
+            inv = all.most;
+            if (PL == 1) {
+                const float least = all.least / inv;
+                bands = least > 0.f ? 1 + band_of(least) : kBands;
+            }
+        }
         if (blockIdx.x == 0 && threadIdx.x == 0)
-            scale[0] = top;
-        inv = top;
+            *scale = {PL == 1 ? inv * kDown : inv, bands};
     }
     const int units = pad / 8, unit = (int)threadIdx.x & 31;
     for (long long row = (long long)blockIdx.x * 8 + ((int)threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * 8) {
         float by = 1.f;
+        int band = 0;
         if constexpr (SCALED) {
             if (parts > 0) {
                 by = g[row];
@@ -534,6 +603,10 @@ __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, lo
                     g[row] = by;
             }
             by /= inv;
+            if (PL == 1) {
+                band = band_of(by);
+                by = ldexpf(by, band * kBandBits);
+            }
         }
         for (int u = unit; u < units; u += 32) {
             float v[8];
@@ -560,7 +633,14 @@ __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, lo
                         s[e] = __builtin_bit_cast(unsigned short, h);
                     }
                 }
-                __builtin_memcpy(__builtin_assume_aligned(out + (row * PL + p) * pad + u * 8, 16), s, sizeof(s));
+                if constexpr (PL == 1) {
+                    u32x4 v4;
+                    __builtin_memcpy(&v4, s, sizeof(s));
+                    for (int b = 0; b < bands; ++b)
+                        *reinterpret_cast<u32x4 *>(out + (b * rows + row) * pad + u * 8) = b == band ? v4 : u32x4{};
+                } else {
+                    __builtin_memcpy(__builtin_assume_aligned(out + (row * PL + p) * pad + u * 8, 16), s, sizeof(s));
+                }
             }
         }
     }
@@ -677,11 +757,16 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 struct Result {
     void *out;                        // [b rows][a rows] of T; or float planes, one per split
     long long plane;                  // floats
-    const float *row_scale;           // by b row, or null
-    const float *scale;               // one number, or null
-    float factor;
+    const float *g;                   // of b rows (grad_x), or null
+    const Scale *scale;               // of all (grad_w), or null
     int add;                          // planes: to what is there
 };
+
+// What a row's sum is multiplied with.
+template <int PL> __device__ __forceinline__ float factor_of(const Result &o, float g)
+{
+    return o.g == nullptr ? o.scale->by : PL == 1 ? g * kDown : g;
+}
 
 // Backward, second part: out[j][i] = scale * sum_r A[i][r] * B[j][r], whole (T) or a split of the sum (float planes).
 // A turned, B turned in the product over pixels (grad_w).
@@ -705,16 +790,18 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
             for (int r = 0; r < 16; ++r)
                 acc[m][n][r] = 0.f;
     const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
-    G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+    if constexpr (PIXELS && PL == 1)
+        G::template multiply<true>(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc, o.scale->bands);
+    else
+        G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
     char *out = smem + wave * (G::OUT / G::kWaves);
     const int i0 = at * G::BM + wr * 32 * WM, j0 = bt * G::BN + wc * 32 * WN;
     constexpr int ES = (int)sizeof(S), ROW = 32 * WM * ES + 16, UNITS = 32 * WM * ES / 16;
     S *to = (S *)o.out + (WHOLE ? 0 : (long long)split * o.plane);
-    const float scale = WHOLE ? o.factor * (o.scale != nullptr ? o.scale[0] : 1.f) : 1.f;
 #pragma unroll
     for (int n = 0; n < WN; ++n) {
         const int j = j0 + n * 32 + row;
-        const float by = WHOLE && o.row_scale != nullptr && j < q.b.count ? scale * o.row_scale[j] : scale;
+        const float by = WHOLE ? factor_of<PL>(o, o.g != nullptr && j < q.b.count ? o.g[j] : 0.f) : 1.f;
 #pragma unroll
         for (int m = 0; m < WM; ++m)
 #pragma unroll
@@ -777,14 +864,13 @@ __global__ __launch_bounds__(256) void dcnv4_loss_sum_kernel(const float *planes
         bias_of<T>(b, (int)blockIdx.x);
         return;
     }
-    const float scale = o.factor * (o.scale != nullptr ? o.scale[0] : 1.f);
     const int units = cols / 4, block = (int)blockIdx.x - b.blocks, blocks = (int)gridDim.x - b.blocks;
     for (long long i = (long long)block * 256 + (int)threadIdx.x; i < n / 4; i += (long long)blocks * 256) {
         f32x4 v = *reinterpret_cast<const f32x4 *>(planes + i * 4);
 #pragma unroll 8
         for (int s = 1; s < splits; ++s)
             v += *reinterpret_cast<const f32x4 *>(planes + s * plane + i * 4);
-        const float by = o.row_scale != nullptr ? scale * o.row_scale[i / units] : scale;
+        const float by = factor_of<sizeof(T) == 2 ? 1 : 3>(o, o.g != nullptr ? o.g[i / units] : 0.f);
         T t[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -878,7 +964,7 @@ struct Plan {
     Choice logits, gx, gw;
     bool gx_planes, gw_planes;
     // bytes from the start of the workspace
-    long long scale, most, g, d, bias_sums, x_scaled, x_split, w_split, gx_at, gw_at, partial, hit, bytes;
+    long long scale, sizes, g, d, bias_sums, x_scaled, x_split, w_split, gx_at, gw_at, partial, hit, bytes;
 };
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -932,11 +1018,11 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
         p.gw = choose_product(p.pl, K, p.vc, p.P, true);
         p.gx_planes = p.gx.splits > 1 || p.pieces > 1;
         p.gw_planes = p.gw.splits > 1;
-        p.scale = take(4);
-        p.most = take((P + 1023) / 1024 * 4);
+        p.scale = take(sizeof(Scale));
+        p.sizes = take((P + 1023) / 1024 * (long long)sizeof(Sizes));
         p.g = take(P * 4);
         p.d = take(P * p.pl * p.vp * 2);
-        p.x_scaled = take(P * p.pl * p.kp * 2);
+        p.x_scaled = take(P * (p.pl == 1 ? kBands : p.pl) * p.kp * 2);
         p.bias_sums = take(round_up(P, 256) / 32 * p.vc * 4);
         if (p.gx_planes)
             p.gx_at = take(p.gx.splits * P * K * 4);
@@ -997,7 +1083,7 @@ unsigned row_groups(long long rows) { return (unsigned)((rows + 7) / 8 < 8192 ? 
 void split_rows(const void *in, long long rows, int cols, int pad, void *out, hipStream_t s)
 {
     hipLaunchKernelGGL((dcnv4_loss_rows_in_kernel<float, 3, false>), dim3(row_groups(rows)), dim3(256), 0, s, (const float *)in, rows, cols, pad,
-                       (unsigned short *)out, (float *)nullptr, (const float *)nullptr, 0, (float *)nullptr, (const float *)nullptr, Labels{});
+                       (unsigned short *)out, (float *)nullptr, (const Sizes *)nullptr, 0, (Scale *)nullptr, (const float *)nullptr, Labels{});
 }
 
 template <typename T, int PL> int loss_forward(const Plan &p, const void *x, const void *w, const Labels &labels, float *loss, float *lse, char *ws,
@@ -1056,17 +1142,18 @@ template <typename T, int PL>
 int loss_backward(const Plan &p, const void *x, const void *w, const Labels &labels, const float *lse, const float *grad_loss, void *grad_x,
                   void *grad_w, void *grad_b, char *ws, hipStream_t s)
 {
-    float *scale = (float *)(ws + p.scale), *most = (float *)(ws + p.most), *g = (float *)(ws + p.g);
+    Scale *scale = (Scale *)(ws + p.scale);
+    Sizes *sizes = (Sizes *)(ws + p.sizes);
+    float *g = (float *)(ws + p.g);
     const int parts = p.P <= kFewRows ? 0 : (p.P + 1023) / 1024;
     if (parts > 0)
-        hipLaunchKernelGGL(dcnv4_loss_rows_kernel, dim3((unsigned)parts), dim3(1024), 0, s, grad_loss, labels, most, g);
+        hipLaunchKernelGGL(dcnv4_loss_rows_kernel, dim3((unsigned)parts), dim3(1024), 0, s, grad_loss, labels, sizes, g);
     hipLaunchKernelGGL((dcnv4_loss_rows_in_kernel<T, PL, true>), dim3(row_groups(p.P)), dim3(256), 0, s, (const T *)x, (long long)p.P, p.K, p.kp,
-                       (unsigned short *)(ws + p.x_scaled), g, (const float *)most, parts, scale, grad_loss, labels);
+                       (unsigned short *)(ws + p.x_scaled), g, (const Sizes *)sizes, parts, scale, grad_loss, labels);
     if (PL == 3)
         split_rows(x, p.P, p.K, p.kp, ws + p.x_split, s);
     const Operand xo = rows_of(PL == 3 ? (const void *)(ws + p.x_split) : x, p.P, p.kp, PL, p.kp);
     const Operand xg = turned(rows_of(ws + p.x_scaled, p.P, p.K, PL, p.kp));
-    const float down = PL == 1 ? kDown : 1.f;
     for (int piece = 0; piece < p.pieces; ++piece) {
         Labels l = labels;
         l.v0 = piece * p.vc;
@@ -1093,10 +1180,10 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         if (bias.blocks > 0 && !p.gw_planes)
             hipLaunchKernelGGL((dcnv4_loss_bias_kernel<T>), dim3((unsigned)bias.blocks), dim3(256), 0, s, bias);
         // grad_x, over the pieces
-        const Result ox = {grad_x, 0, g, nullptr, down, 0};
+        const Result ox = {grad_x, 0, g, nullptr, 0};
         const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), PL, p.gx);
         if (p.gx_planes) {
-            const Result o = {ws + p.gx_at, (long long)p.P * p.K, nullptr, nullptr, 1.f, piece > 0};
+            const Result o = {ws + p.gx_at, (long long)p.P * p.K, nullptr, nullptr, piece > 0};
             launch_product<T, PL, false>(qx, p.gx, true, o, s);
             if (piece == p.pieces - 1)
                 sum_planes<T>(ws + p.gx_at, p.gx.splits, p.P, p.K, ox, Bias{}, s);
@@ -1104,10 +1191,10 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
             launch_product<T, PL, false>(qx, p.gx, false, ox, s);
         }
         // grad_w of the piece
-        const Result ow = {(char *)grad_w + (long long)l.v0 * p.K * p.es, 0, nullptr, scale, down, 0};
+        const Result ow = {(char *)grad_w + (long long)l.v0 * p.K * p.es, 0, nullptr, scale, 0};
         const Product qw = product_of(xg, turned(rows_of(d.d, p.P, l.count, PL, vp)), PL, p.gw);
         if (p.gw_planes) {
-            const Result o = {ws + p.gw_at, (long long)l.count * p.K, nullptr, nullptr, 1.f, 0};
+            const Result o = {ws + p.gw_at, (long long)l.count * p.K, nullptr, scale, 0};
             launch_product<T, PL, true>(qw, p.gw, true, o, s);
             sum_planes<T>(ws + p.gw_at, p.gw.splits, l.count, p.K, ow, bias, s);
         } else {
