@@ -463,9 +463,10 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     }
 }
 
-// Joins the tiles' maxima and sums: 16 pixels to a workgroup, 16 tiles side by side.
-__global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *partial, int tiles, const float *target_logit, Labels l, float *loss,
-                                                              float *lse)
+// Joins the tiles' maxima and sums: 16 pixels to a workgroup, 16 tiles side by side.  Of a piece of the classes: what the pieces before left in
+// `all` (first: nothing) comes in last, and goes there again before the last piece gives the loss.
+__global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *partial, int tiles, float2 *all, bool first, bool last,
+                                                              const float *target_logit, Labels l, float *loss, float *lse)
 {
     __shared__ float2 part[16][17];
     const int i = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4, px = (int)blockIdx.x * 16 + i;
@@ -486,7 +487,12 @@ __global__ __launch_bounds__(256) void dcnv4_loss_join_kernel(const float2 *part
 #pragma unroll
     for (int s = 1; s < 16; ++s)
         join(part[s][i]);
-    finish_row(l, px, top, sum, target_logit[px], loss, lse);
+    if (!first)
+        join(all[px]);
+    if (last)
+        finish_row(l, px, top, sum, target_logit[px], loss, lse);
+    else
+        all[px] = make_float2(top, sum);
 }
 
 // What the backward pass knows of its rows beforehand: g per row (zero where the row is ignored, NaN where its target is no class), and
@@ -888,11 +894,13 @@ enum { kSmall, kMiddle, kLarge };
 constexpr int kUnits = 256;
 constexpr int kFewRows = 512;        // that every workgroup looks through by itself (2000: as long as the launch it saves)
 constexpr int kLossMaxRows = 1 << 20, kLossMaxClasses = 1 << 22;
-// Classes of a piece: d takes P * classes numbers in each layout, this many at most.
+// Classes of a piece: d takes P * classes numbers, this many at most (and P * 256 at least).
 constexpr long long kPieceNumbers = 1ll << 27;
 constexpr long long kMaxPiece = 1 << 20;                   // (256 rows of d, in three planes, stay below 2 GiB)
 // ... and fp32 weights, split, this many
 constexpr long long kPieceWeights = 1ll << 27;
+// ... and the forward pass leaves a maximum and a sum per row and tile of classes, this many at most, which are joined piece by piece.
+constexpr long long kPiecePartials = 1ll << 25;
 // Logits of a launch: a grid has fewer than 2^32 lanes, and the smallest tile's make 16 logits each.
 constexpr long long kLaunchLogits = 1ll << 35;
 
@@ -964,7 +972,7 @@ struct Plan {
     Choice logits, gx, gw;
     bool gx_planes, gw_planes;
     // bytes from the start of the workspace
-    long long scale, sizes, g, d, bias_sums, x_scaled, x_split, w_split, gx_at, gw_at, partial, hit, bytes;
+    long long scale, sizes, g, d, bias_sums, x_scaled, x_split, w_split, gx_at, gw_at, partial, all, hit, bytes;
 };
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -989,15 +997,20 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
     if (g_loss.piece)
         most = g_loss.piece;
     most = most < 256 ? 256 : most > kMaxPiece ? kMaxPiece : most;
-    if (p.pl == 1 && !backward)
-        most = V;                                          // (nothing of a piece is kept)
+    if (p.pl == 1 && !backward && !g_loss.piece)
+        most = V;                                          // (w is read as it lies, and there is no d)
     most = most < kLaunchLogits / P ? most : kLaunchLogits / P;
+    p.logits = choose_product(p.pl, V < most ? V : most, P, p.kp, false);
+    const int bm = shape_of(p.pl, p.logits.shape).bm;
+    if (!backward && most > kPiecePartials / P * bm)
+        most = kPiecePartials / P * bm;
     p.pieces = (int)((V + most - 1) / most);
     p.vc = (int)round_up((V + p.pieces - 1) / p.pieces, 256);
     p.vc = p.vc < V ? p.vc : V;
     p.pieces = (V + p.vc - 1) / p.vc;
     p.vp = (int)round_up(p.vc, 64);
-    p.logits = choose_product(p.pl, p.vc, P, p.kp, false);
+    if (backward)
+        p.logits = choose_product(p.pl, p.vc, P, p.kp, false);
     long long at = 0;
     auto take = [&](long long bytes) {
         const long long here = at;
@@ -1009,9 +1022,9 @@ int make_plan(Plan *out, long long P, int K, int V, int dtype, bool backward)
         p.w_split = take((long long)p.vc * 6 * p.kp);
     }
     if (!backward) {
-        const int bm = shape_of(p.pl, p.logits.shape).bm;
-        const long long tiles = (long long)(p.pieces - 1) * ((p.vc + bm - 1) / bm) + (V - (p.pieces - 1) * p.vc + bm - 1) / bm;
-        p.partial = take(tiles * P * 8);
+        p.partial = take((p.vc + bm - 1) / bm * P * 8);
+        if (p.pieces > 1)
+            p.all = take(P * 8);
         p.hit = take(P * 4);
     } else {
         p.gx = choose_product(p.pl, K, P, p.vp, true);
@@ -1092,7 +1105,6 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
     if (PL == 3)
         split_rows(x, p.P, p.K, p.kp, ws + p.x_split, s);
     const Operand b = rows_of(PL == 3 ? (const void *)(ws + p.x_split) : x, p.P, p.kp, PL, p.kp);
-    int tiles = 0;
     for (int piece = 0; piece < p.pieces; ++piece) {
         Labels l = labels;
         l.v0 = piece * p.vc;
@@ -1105,15 +1117,14 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
             hipLaunchKernelGGL((dcnv4_loss_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
-                               dim3(G::WR * G::WC * 64), 0, s, q, l, one ? nullptr : (float2 *)(ws + p.partial) + (long long)tiles * p.P,
+                               dim3(G::WR * G::WC * 64), 0, s, q, l, one ? nullptr : (float2 *)(ws + p.partial),
                                (float *)(ws + p.hit), loss, lse);
             return 0;
         });
-        tiles += q.a_tiles;
+        if (!one)
+            hipLaunchKernelGGL(dcnv4_loss_join_kernel, dim3((unsigned)((p.P + 15) / 16)), dim3(256), 0, s, (const float2 *)(ws + p.partial), q.a_tiles,
+                               (float2 *)(ws + p.all), piece == 0, piece == p.pieces - 1, (const float *)(ws + p.hit), labels, loss, lse);
     }
-    if (tiles > 1)
-        hipLaunchKernelGGL(dcnv4_loss_join_kernel, dim3((unsigned)((p.P + 15) / 16)), dim3(256), 0, s, (const float2 *)(ws + p.partial), tiles,
-                       (const float *)(ws + p.hit), labels, loss, lse);
     return launched();
 }
 
