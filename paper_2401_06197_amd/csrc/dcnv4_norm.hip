@@ -470,10 +470,10 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
             }
             if (!AHEAD && gamma != nullptr)
                 gm[0] = load8<T, WHOLE>(gamma + c, n, false);
-            // (behind the row grad_y is zero, and so is every sum's term)
+            // (behind the row both are zero, and so is every sum's term: mean * rstd may be more than fp32 holds)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[j][e] = (xh[j][e] - mean) * rstd;
+                xh[j][e] = (WHOLE ? n > 0 : e < n) ? (xh[j][e] - mean) * rstd : 0.f;
                 dg[j][e] = __builtin_fmaf(g[j][e], xh[j][e], dg[j][e]);
                 db[j][e] += g[j][e];
                 if (gamma != nullptr)
