@@ -481,6 +481,9 @@ def dcnv4_module_forward_static(x, w_om, b_om, G, out, w_in=None, b_in=None, w_o
 
 # Operators on rows [..., C].  Optional tensors may be None; statistics and losses are float32.  (Small calls are bound by this module:
 # a layer norm of 49 x 1024 takes the GPU 3 us.  So checks make nothing that a call without fault does not need.)
+# With `stream`, results that the caller does not bring are memory of that stream, as the workspaces are: memory of the current one may still be
+# read there by what was queued before, and would go back to it while the call writes.  Who uses them on another stream waits for the call and, where
+# they are given back before that use has ended, marks them (torch.Tensor.record_stream).
 
 def _rows(x):
     shape = x.shape
@@ -509,9 +512,12 @@ def _check_plain(name, t, at, shape, dtype):
         raise ValueError(f"dcnv4: {name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on x's device")
 
 
-def _new_like(x):
-    """_uninitialised(x, x.shape), faster (1.2 us, 1.8 with the shape)."""
+def _new_like(x, stream):
+    """_uninitialised(x, x.shape), faster (1.2 us, 1.8 with the shape); of the stream that the call runs on."""
     import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new_like(x, None)
     return torch.empty_like(x) if type(x) is torch.Tensor else _uninitialised(x, x.shape)
 
 
@@ -524,9 +530,14 @@ def _new(x, shape, dtype):
     return torch.empty_like(x) if shape == x.shape else x.new_empty(shape)
 
 
-def _outputs(x, out, specs):
-    """The output tensors: those of `out`, checked, or new ones.  specs: (name, shape, dtype), None for one that is not wanted."""
+def _outputs(x, out, specs, stream):
+    """The output tensors: those of `out`, checked, or new ones of the stream that the call runs on.  specs: (name, shape, dtype), None for one that
+    is not wanted."""
     if out is None:
+        if stream is not None:
+            import torch
+            with torch.cuda.stream(stream):
+                return _outputs(x, None, specs, None)
         return [None if s is None else _new(x, s[1], s[2]) for s in specs]
     out = list(out) if isinstance(out, (tuple, list)) else [out]
     if len(out) != len(specs):
@@ -586,9 +597,9 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
     mean = rstd = None
     if stats:
         stat, f32 = x.shape[:-1], torch.float32
-        y, mean, rstd = _outputs(x, out, (("y", x.shape, x.dtype), ("mean", stat, f32), ("rstd", stat, f32)))
+        y, mean, rstd = _outputs(x, out, (("y", x.shape, x.dtype), ("mean", stat, f32), ("rstd", stat, f32)), stream)
     else:
-        y = _new_like(x) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),))[0]
+        y = _new_like(x, stream) if out is None else _outputs(x, out, (("y", x.shape, x.dtype),), stream)[0]
     args = (x.data_ptr(), None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(), y.data_ptr(),
             None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), P, C, float(eps), _dtype_code(x),
             _stream_ptr(stream, x.device))
@@ -608,10 +619,10 @@ def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=
     _check_plain("mean", mean, at, shape[:-1], torch.float32)
     _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
     if gamma is None:
-        (gx, gg, gb), size = _outputs(x, out, (("grad_x", shape, dt), None, None)), 0
+        (gx, gg, gb), size = _outputs(x, out, (("grad_x", shape, dt), None, None), stream), 0
         space = None
     else:
-        gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
+        gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
         space, size = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), ptr(gx), None if gg is None else ptr(gg),
@@ -629,7 +640,7 @@ def dcnv4_dropout(x, p, seed, offset=0, offset_on_device=None, residual=None, ou
     offset as the kernel runs (captured graphs)."""
     shape = x.shape
     _check_like(x, (("residual", residual, shape),))
-    y = _new_like(x) if out is None else _outputs(x, out, (("out", shape, x.dtype),))[0]
+    y = _new_like(x, stream) if out is None else _outputs(x, out, (("out", shape, x.dtype),), stream)[0]
     args = (x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64,
             _offset_ptr(x, offset_on_device), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
@@ -642,7 +653,7 @@ def dcnv4_dropout_backward(grad_y, p, seed, offset=0, offset_on_device=None, out
     """grad_x of dcnv4_dropout with the same p, seed and offset (that of the residual is grad_y itself)."""
     shape = grad_y.shape
     _check_all(grad_y, ())
-    gx = _new_like(grad_y) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),))[0]
+    gx = _new_like(grad_y, stream) if out is None else _outputs(grad_y, out, (("out", shape, grad_y.dtype),), stream)[0]
     args = (grad_y.data_ptr(), gx.data_ptr(), grad_y.numel(), float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(grad_y, offset_on_device),
             _dtype_code(grad_y), _stream_ptr(stream, grad_y.device))
     if prepare_only:
@@ -659,7 +670,7 @@ def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, of
     shape, dt, f32 = x.shape, x.dtype, torch.float32
     _check_like(x, (("residual", residual, shape), ("gamma", gamma, (C,)), ("beta", beta, (C,))))
     stat = shape[:-1]
-    z, y, mean, rstd = _outputs(x, out, (("z", shape, dt), ("y", shape, dt), ("mean", stat, f32), ("rstd", stat, f32)))
+    z, y, mean, rstd = _outputs(x, out, (("z", shape, dt), ("y", shape, dt), ("mean", stat, f32), ("rstd", stat, f32)), stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(residual), None if gamma is None else ptr(gamma), None if beta is None else ptr(beta), ptr(z), ptr(y), ptr(mean),
             ptr(rstd), P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(x, offset_on_device), float(eps), _dtype_code(x),
@@ -682,10 +693,10 @@ def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed,
     _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
     specs = (("grad_x", shape, dt), ("grad_residual", shape, dt))
     if gamma is None:
-        (gx, gr, gg, gb), size = _outputs(z, out, specs + (None, None)), 0
+        (gx, gr, gg, gb), size = _outputs(z, out, specs + (None, None), stream), 0
         space = None
     else:
-        gx, gr, gg, gb = _outputs(z, out, specs + (("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)))
+        gx, gr, gg, gb = _outputs(z, out, specs + (("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
         space, size = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(z), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), None if grad_z is None else ptr(grad_z), ptr(gx),
@@ -719,7 +730,7 @@ def dcnv4_linear_cross_entropy(x, w, target, b=None, ignore_index=-100, workspac
     import torch
     P, K, V, space, size = _loss_args(x, w, target, b, workspace, False, stream)
     stat, f32 = x.shape[:-1], torch.float32
-    loss, lse = _outputs(x, out, (("loss", stat, f32), ("lse", stat, f32)))
+    loss, lse = _outputs(x, out, (("loss", stat, f32), ("lse", stat, f32)), stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(loss), ptr(lse), ptr(space), size, P, K, V, int(ignore_index),
             _dtype_code(x), _stream_ptr(stream, x.device))
@@ -737,7 +748,7 @@ def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ig
     shape, dt, at = x.shape, x.dtype, x.get_device()
     _check_plain("lse", lse, at, shape[:-1], torch.float32)
     _check_plain("grad_loss", grad_loss, at, shape[:-1], torch.float32)
-    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_w", w.shape, dt), None if b is None else ("grad_b", (V,), dt)))
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_w", w.shape, dt), None if b is None else ("grad_b", (V,), dt)), stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), ptr(w), None if b is None else ptr(b), ptr(target), ptr(lse), ptr(grad_loss), ptr(gx), ptr(gw), None if gb is None else ptr(gb),
             ptr(space), size, P, K, V, int(ignore_index), _dtype_code(x), _stream_ptr(stream, x.device))
