@@ -3,6 +3,11 @@
 The tensor arguments are torch tensors on the GPU (torch is used for device memory and
 streams, nothing else); every step of the operator runs inside libdcnv4.so.  If the
 library has not been built the import of it fails loudly -- there is no fallback path.
+
+With `stream`, results and workspaces that the caller does not bring are memory of that stream, as torch's are of the current one:
+memory of the current one may still be read there by what was queued before, and would go back to it while the call writes.  Who
+uses such results on another stream waits for the call first and, where they are given back before that use has ended, marks them
+(torch.Tensor.record_stream).
 """
 import ctypes
 import os
@@ -184,11 +189,23 @@ def _check_all(x, named):
             _check(name, t, x)
 
 
-def _uninitialised(x, shape):
-    """A plain tensor of x's type on its device, whatever subclass x is of.  (new_empty keeps the subclass; it takes 1.2 us where
-    torch.empty takes 1.6.)"""
+def _uninitialised(x, shape, stream=None):
+    """A plain tensor of x's type on its device, whatever subclass x is of, and of the stream that the call runs on.  (new_empty keeps the
+    subclass; it takes 1.2 us where torch.empty takes 1.6.)"""
     import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _uninitialised(x, shape)
     return x.new_empty(shape) if type(x) is torch.Tensor else torch.empty(shape, dtype=x.dtype, device=x.device)
+
+
+def _empty_like(stream, *tensors):
+    """torch.empty_like of each, of the stream that the call runs on."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _empty_like(None, *tensors)
+    return tuple(map(torch.empty_like, tensors))
 
 
 def _stream_ptr(stream, device):
@@ -256,7 +273,7 @@ def dcnv4_forward(x, offset, mask, kernel=3, stride=1, pad=1, dilation=1, offset
     geo, yshape = _shape_args(x, offset, mask, kernel, stride, pad, dilation)
     _check_all(x, (("offset", offset), ("mask", mask)))
     if out is None:
-        out = _uninitialised(x, yshape)
+        out = _uninitialised(x, yshape, stream)
     else:
         _check("out", out, x)
         if tuple(out.shape) != yshape:
@@ -282,13 +299,12 @@ def dcnv4_backward_softmax(x, offset, mask_logits, grad_y, **kw):
 def dcnv4_backward(x, offset, mask, grad_y, kernel=3, stride=1, pad=1, dilation=1, offset_scale=1.0,
                    out=None, stream=None, prepare_only=False, _entry="dcnv4_backward"):
     """(grad_x, grad_offset, grad_mask) of dcnv4_forward for upstream gradient grad_y."""
-    import torch
     geo, yshape = _shape_args(x, offset, mask, kernel, stride, pad, dilation)
     _check_all(x, (("offset", offset), ("mask", mask), ("grad_y", grad_y)))
     if grad_y.shape != yshape:
         raise ValueError("dcnv4: grad_y has the wrong shape")
     if out is None:
-        gx, go, gm = torch.empty_like(x), torch.empty_like(offset), torch.empty_like(mask)
+        gx, go, gm = _empty_like(stream, x, offset, mask)
     else:
         gx, go, gm = out
         for name, t, ref in (("grad_x", gx, x), ("grad_offset", go, offset), ("grad_mask", gm, mask)):
@@ -326,7 +342,7 @@ def dcnv4_forward_merged(x, offset_mask, kernel=3, stride=1, pad=1, dilation=1, 
     geo, yshape = _merged_shape_args(x, offset_mask, kernel, stride, pad, dilation)
     _check_all(x, (("offset_mask", offset_mask),))
     if out is None:
-        out = _uninitialised(x, yshape)
+        out = _uninitialised(x, yshape, stream)
     else:
         _check("out", out, x)
         if tuple(out.shape) != yshape:
@@ -342,13 +358,12 @@ def dcnv4_forward_merged(x, offset_mask, kernel=3, stride=1, pad=1, dilation=1, 
 def dcnv4_backward_merged(x, offset_mask, grad_y, kernel=3, stride=1, pad=1, dilation=1, offset_scale=1.0,
                           out=None, stream=None, prepare_only=False):
     """(grad_x, grad_offset_mask) of dcnv4_forward_merged; grad_offset_mask is laid out like offset_mask."""
-    import torch
     geo, yshape = _merged_shape_args(x, offset_mask, kernel, stride, pad, dilation)
     _check_all(x, (("offset_mask", offset_mask), ("grad_y", grad_y)))
     if grad_y.shape != yshape:
         raise ValueError("dcnv4: grad_y has the wrong shape")
     if out is None:
-        gx, gom = torch.empty_like(x), torch.empty_like(offset_mask)
+        gx, gom = _empty_like(stream, x, offset_mask)
     else:
         gx, gom = out
         for name, t, ref in (("grad_x", gx, x), ("grad_offset_mask", gom, offset_mask)):
@@ -366,14 +381,13 @@ def dcnv4_backward_merged(x, offset_mask, grad_y, kernel=3, stride=1, pad=1, dil
 def dcnv4_linear(x, w, b=None, out=None, stream=None, prepare_only=False):
     """y[..., o] = sum_k x[..., k] * w[o, k] + b[o]: a linear layer over the last axis of x (a 1x1
     point-wise convolution of an NHWC map), on the matrix cores."""
-    import torch
     if x.dim() < 2 or w.dim() != 2 or w.shape[1] != x.shape[-1] or (b is not None and tuple(b.shape) != (w.shape[0],)):
         raise ValueError("dcnv4: expected x [..., K], w [Nout, K], b [Nout]")
     for name, t in (("x", x), ("w", w)) + ((("b", b),) if b is not None else ()):
         _check(name, t, x)
     yshape = tuple(x.shape[:-1]) + (w.shape[0],)
     if out is None:
-        out = torch.empty(yshape, dtype=x.dtype, device=x.device)
+        out = _uninitialised(x, yshape, stream)
     else:
         _check("out", out, x)
         if tuple(out.shape) != yshape:
@@ -395,7 +409,7 @@ def dcnv4_depthwise3x3(x, w, b=None, out=None, stream=None):
     for name, t in (("x", x), ("w", w)) + ((("b", b),) if b is not None else ()):
         _check(name, t, x)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty_like(stream, x)[0]
     else:
         _check("out", out, x)
         if out.shape != x.shape:
@@ -421,7 +435,6 @@ def dcnv4_module_forward(x, w_om, b_om, G, w_in=None, b_in=None, w_out=None, b_o
     (row g*32 + e: entry e of group g; 0..17 offsets, 18..26 scalars, 27..31 ignored); w_in, w_out
     [C, C] or both None (the lightweight variant); w_dw [3, 3, C] / b_dw [C]: the optional depthwise
     convolution in front of the offset/scalar layer."""
-    import torch
     if x.dim() != 4 or x.shape[3] % G:
         raise ValueError("dcnv4: expected x [N,H,W,C] with C a multiple of G")
     N, H, W, C = x.shape
@@ -439,11 +452,11 @@ def dcnv4_module_forward(x, w_om, b_om, G, w_in=None, b_in=None, w_out=None, b_o
     light = w_in is None
     need = dcnv4_module_workspace_bytes(N, H, W, G, C // G, _dtype_code(x), light, w_dw is not None)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+        workspace = _workspace(x, None, need, stream)[0]
     elif not workspace.is_cuda or workspace.device != x.device or not workspace.is_contiguous():
         raise ValueError("dcnv4: workspace must be a contiguous tensor on x's device")
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty_like(stream, x)[0]
     else:
         _check("out", out, x)
         if out.shape != x.shape:
@@ -481,9 +494,6 @@ def dcnv4_module_forward_static(x, w_om, b_om, G, out, w_in=None, b_in=None, w_o
 
 # Operators on rows [..., C].  Optional tensors may be None; statistics and losses are float32.  (Small calls are bound by this module:
 # a layer norm of 49 x 1024 takes the GPU 3 us.  So checks make nothing that a call without fault does not need.)
-# With `stream`, results that the caller does not bring are memory of that stream, as the workspaces are: memory of the current one may still be
-# read there by what was queued before, and would go back to it while the call writes.  Who uses them on another stream waits for the call and, where
-# they are given back before that use has ended, marks them (torch.Tensor.record_stream).
 
 def _rows(x):
     shape = x.shape

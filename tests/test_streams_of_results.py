@@ -43,3 +43,13 @@ def test_results_and_workspaces(made, stream):
     out = [torch.zeros((3, 8))]
     del made[:]
     assert dcn._outputs(x, out, (("y", x.shape, f32),), stream)[0] is out[0] and not made
+
+
+@pytest.mark.parametrize("stream", [None, "side"])
+def test_results_of_the_operator_and_the_module(made, stream):
+    x, offset = torch.zeros((1, 2, 2, 4)), torch.zeros((1, 2, 2, 1, 9, 2))
+    assert dcn._uninitialised(x, (1, 3, 3, 4), stream).shape == (1, 3, 3, 4)
+    assert dcn._uninitialised(torch.nn.Parameter(x), (2, 2), stream).shape == (2, 2)
+    a, b = dcn._empty_like(stream, x, offset)
+    assert a.shape == x.shape and b.shape == offset.shape
+    assert made == [stream] * 4
