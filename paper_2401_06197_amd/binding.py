@@ -619,27 +619,27 @@ def dcnv4_layer_norm(x, gamma=None, beta=None, eps=1e-6, stats=False, out=None, 
     return (y, mean, rstd) if stats else y
 
 
-def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=None, stream=None, prepare_only=False):
-    """(grad_x, grad_gamma, grad_beta) of dcnv4_layer_norm; the last two are None where gamma is None (a norm without
-    parameters)."""
+def dcnv4_layer_norm_backward(x, gamma, mean, rstd, grad_y, workspace=None, out=None, stream=None, prepare_only=False, beta=None):
+    """(grad_x, grad_gamma, grad_beta) of dcnv4_layer_norm.  grad_gamma is None where gamma is; grad_beta too, unless beta is given (a norm
+    with beta alone)."""
     import torch
     P, C = _rows(x)
     shape, dt, at = x.shape, x.dtype, x.get_device()
-    _check_like(x, (("gamma", gamma, (C,)), ("grad_y", grad_y, shape)))
+    _check_like(x, (("gamma", gamma, (C,)), ("beta", beta, (C,)), ("grad_y", grad_y, shape)))
     _check_plain("mean", mean, at, shape[:-1], torch.float32)
     _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
-    if gamma is None:
+    if gamma is None and beta is None:
         (gx, gg, gb), size = _outputs(x, out, (("grad_x", shape, dt), None, None), stream), 0
         space = None
     else:
-        gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
+        gx, gg, gb = _outputs(x, out, (("grad_x", shape, dt), None if gamma is None else ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
         space, size = _workspace(x, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(x), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), ptr(gx), None if gg is None else ptr(gg),
             None if gb is None else ptr(gb), None if space is None else ptr(space), size, P, C, _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
-        return _prepared(args, out, *(() if gamma is None else (workspace,)))
+        return _prepared(args, out, *(() if space is None else (workspace,)))
     _call(x.device, "dcnv4_layer_norm_backward", args)
     return gx, gg, gb
 
@@ -692,28 +692,28 @@ def dcnv4_dropout_add_layer_norm(x, residual, gamma, beta, p, seed, offset=0, of
 
 
 def dcnv4_dropout_add_layer_norm_backward(z, gamma, mean, rstd, grad_y, p, seed, offset=0, offset_on_device=None, grad_z=None,
-                                          workspace=None, out=None, stream=None, prepare_only=False):
+                                          workspace=None, out=None, stream=None, prepare_only=False, beta=None):
     """(grad_x, grad_residual, grad_gamma, grad_beta) of dcnv4_dropout_add_layer_norm; grad_z: the gradient of z from what else
-    reads it.  The last two are None where gamma is None."""
+    reads it.  The last two are None as in dcnv4_layer_norm_backward."""
     import torch
     P, C = _rows(z)
     shape, dt, at = z.shape, z.dtype, z.get_device()
-    _check_like(z, (("gamma", gamma, (C,)), ("grad_y", grad_y, shape), ("grad_z", grad_z, shape)))
+    _check_like(z, (("gamma", gamma, (C,)), ("beta", beta, (C,)), ("grad_y", grad_y, shape), ("grad_z", grad_z, shape)))
     _check_plain("mean", mean, at, shape[:-1], torch.float32)
     _check_plain("rstd", rstd, at, shape[:-1], torch.float32)
     specs = (("grad_x", shape, dt), ("grad_residual", shape, dt))
-    if gamma is None:
+    if gamma is None and beta is None:
         (gx, gr, gg, gb), size = _outputs(z, out, specs + (None, None), stream), 0
         space = None
     else:
-        gx, gr, gg, gb = _outputs(z, out, specs + (("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
+        gx, gr, gg, gb = _outputs(z, out, specs + (None if gamma is None else ("grad_gamma", (C,), dt), ("grad_beta", (C,), dt)), stream)
         space, size = _workspace(z, workspace, dcnv4_layer_norm_workspace_bytes(P, C) if workspace is None else 0, stream)
     ptr = torch.Tensor.data_ptr
     args = (ptr(z), None if gamma is None else ptr(gamma), ptr(mean), ptr(rstd), ptr(grad_y), None if grad_z is None else ptr(grad_z), ptr(gx),
             ptr(gr), None if gg is None else ptr(gg), None if gb is None else ptr(gb), None if space is None else ptr(space), size,
             P, C, float(p), int(seed) & _MASK64, int(offset) & _MASK64, _offset_ptr(z, offset_on_device), _dtype_code(z), _stream_ptr(stream, z.device))
     if prepare_only:
-        return _prepared(args, out, *(() if gamma is None else (workspace,)))
+        return _prepared(args, out, *(() if space is None else (workspace,)))
     _call(z.device, "dcnv4_dropout_add_layer_norm_backward", args)
     return gx, gr, gg, gb
 

@@ -31,3 +31,28 @@ def test_gradient_of_large_constant_rows(C):
     assert not got[1].any() and got[2].isfinite().all()
     branch = dcn.dcnv4_dropout_add_layer_norm_backward(x, gamma, mean, rstd, gy, 0.0, 1)
     assert torch.equal(branch[0], got[0]) and torch.equal(branch[1], got[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("P,C", [(1, 5), (700, 72), (90, 1030)])
+def test_gradient_of_a_norm_with_beta_alone(P, C, dtype):
+    """beta has its gradient without gamma, which then is a gamma of ones: the same numbers, bit for bit."""
+    x, res, gy, gz = (torch.randn((P, C), device="cuda").to(dtype) for _ in range(4))
+    beta, ones = torch.randn(C, device="cuda").to(dtype), torch.ones(C, device="cuda", dtype=dtype)
+    y, mean, rstd = dcn.dcnv4_layer_norm(x, None, beta, stats=True)
+    got = dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy, beta=beta)
+    want = dcn.dcnv4_layer_norm_backward(x, ones, mean, rstd, gy)
+    assert torch.equal(got[0], want[0]) and got[1] is None and torch.equal(got[2], want[2])
+    assert dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy)[1:] == (None, None)
+    z, _, mean, rstd = dcn.dcnv4_dropout_add_layer_norm(x, res, None, beta, 0.3, 7)
+    got = dcn.dcnv4_dropout_add_layer_norm_backward(z, None, mean, rstd, gy, 0.3, 7, grad_z=gz, beta=beta)
+    want = dcn.dcnv4_dropout_add_layer_norm_backward(z, ones, mean, rstd, gy, 0.3, 7, grad_z=gz)
+    assert got[2] is None and all(torch.equal(got[i], want[i]) for i in (0, 1, 3))
+    work = torch.empty(dcn.dcnv4_layer_norm_workspace_bytes(P, C), dtype=torch.uint8, device="cuda")
+    out = (torch.empty_like(x), None, torch.empty_like(beta))
+    again = dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy, beta=beta, workspace=work, out=out)
+    assert again[2] is out[2]
+    with pytest.raises(ValueError):
+        dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy, beta=beta, out=out, prepare_only=True)
+    with pytest.raises(ValueError):
+        dcn.dcnv4_layer_norm_backward(x, None, mean, rstd, gy, beta=beta[:-1])
