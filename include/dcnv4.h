@@ -219,8 +219,9 @@ long long dcnv4_module_static_workspace_limit(void);
 
 /* Operators of a training step around the module, on rows: x [P][C], C channels (or features) of P pixels.  As everywhere:
  * DEVICE pointers, dense, 16-byte aligned, tensors of element type `dtype`, arithmetic and statistics in fp32, one rounding
- * to nearest at each store, outputs must not alias inputs, nothing is allocated, nothing is kept between calls.  A workspace is the
- * caller's and needs no initial values; two calls, or two captured graphs, that may run at the same time need one each. */
+ * to nearest at each store (what else the cross entropy rounds is said there), outputs must not alias inputs, nothing is allocated,
+ * nothing is kept between calls.  A workspace is the caller's and needs no initial values; two calls, or two captured graphs, that may run at
+ * the same time need one each. */
 
 /* Layer norm over the channels of each row (biased variance, as normalisation layers have it):
  *     y = (x - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps)
@@ -276,7 +277,7 @@ int dcnv4_dropout_add_layer_norm_backward(const void *z, const void *gamma, cons
  * has loss 0; one whose target is neither that nor a class has loss NaN.  Logits and sums are fp32 (F32: products of operands
  * held as three bf16 numbers, fp32's accuracy for numbers above 2^-100; x and w must be finite and below 3.3e38; F16 follows fp16's infinities).  b may
  * hold -infinity: that class has probability 0.
- * Needs K * element size a multiple of 32 bytes, K and P up to 2^20, V up to 2^22 (else DCNV4_ERR_UNSUPPORTED); any V and P.
+ * Needs K * element size a multiple of 32 bytes, and at most 2^20 rows, 2^20 features and 2^22 classes (else DCNV4_ERR_UNSUPPORTED).
  * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 0) bytes. */
 int dcnv4_linear_cross_entropy(const void *x, const void *w, const void *b, const long long *target, float *loss, float *lse,
                                void *workspace, long long workspace_bytes, long long P, int K, int V,
@@ -288,7 +289,7 @@ int dcnv4_linear_cross_entropy(const void *x, const void *w, const void *b, cons
  * In F16 d is rounded to fp16 (of 2^15 * d) for grad_x and grad_w; grad_w's other operand, x * grad_loss / the largest |grad_loss|, is x itself
  * where grad_loss is the same in all rows and is rounded to fp16 otherwise, to 2^-11 of it and 2^-17 of x = 1 for rows of down to 2^-32 of the
  * largest (each power of two below doubles the latter).  Sums are fp32, grad_b is made from fp32 numbers alone.
- * A row that is ignored, or whose grad_loss is 0, counts for nothing and has grad_x 0, whatever x holds there; one with
+ * A row that is ignored, or whose grad_loss is 0, counts for nothing and has grad_x 0, whatever x holds there (w being finite); one with
  * loss NaN has grad_x NaN and makes grad_w NaN.  grad_b may be NULL.  Sums are made in a fixed order.
  * `workspace`: at least dcnv4_linear_cross_entropy_workspace_bytes(..., backward = 1) bytes. */
 int dcnv4_linear_cross_entropy_backward(const void *x, const void *w, const void *b, const long long *target,

@@ -673,10 +673,13 @@ int check_rows(long long P, int C, int dtype)
 
 // Calls f with the lanes of a row and a lane's runs of eight channels, as constants: the fewest lanes that hold the row with one run each,
 // up to a wave; with two up to 1024 channels, then two, four and eight waves.  (Two rows side by side in a workgroup of four
-// waves each rather than eight waves with one run: twice the loads on their way.)  Forward, up to 1536 channels: three runs and no
-// barriers (16368 x 1025 fp16: 20 us, by two waves 28; backward, whose sums leave it no registers to load ahead, 41 and 44, 11184 x 1500 42 and 35).
-// Up to 4096 channels in fp32 eight waves with one run after all (4096 x 4096: branch end 50.6 and 71 us, with two 56 and 76; fp16 31.7 and 41,
-// with two 29.7 and 42, norm backward 30.3 and 28.9).
+// waves each rather than eight waves with one run: twice the loads on their way.)  Both sides of the two exceptions, in us for 16.8 million elements:
+// Forward, up to 1536 channels: three runs and no barriers.  1032, 1280 and 1536 channels in fp16 norm 17.8, 14.1, 13.2 (by two waves 20.7, 17.4, 15.1),
+// branch end 29, 27, 27 (37, 32, 29); 1100 and 1499, 20 and 17 (27, 22); in fp32 0 to 6 % less.  Backward, whose sums leave it no registers
+// to load ahead: 16368 x 1025 fp16 41 (44 by two waves), 11184 x 1500 42 and 35.
+// fp32, 2049 to 4096 channels: eight waves with one run.  Norms forward and backward together at 2056, 2816, 3584 and 4096 channels 88, 78, 78, 78 (with
+// two 80, 77, 82, 79), branch ends 135, 123, 124, 121 (132, 130, 136, 133).  fp16, with one run: norms 65, 54, 48, 46 (as it is 54, 45, 46, 45), branch
+// ends 90, 74, 68, 69 (89, 74, 73, 71).
 template <typename T, bool BACK, typename F> int by_width(int C, F &&f)
 {
     const int runs = (C + 7) / 8;
