@@ -13,9 +13,9 @@
 // half a step of fp16, for both products.  grad_x takes its row's g afterwards, in fp32.  In grad_w's sum rows meet, so g goes into x, as a part of
 // the largest |g|: where g is the same in all rows that leaves x as it is, else it is rounded to fp16 once more.  Rows of less than 2^-8 of the
 // largest lie in planes of x of their own, times 2^8, 2^16 or 2^24, so that no more than eight of x's powers of two go (half of fp16's least
-// step, 2^-25, is 2^-17 of such an x); the planes' products are added up in the same registers, from the smallest on.  Weights that are alike take
-// one plane.  (One plane for all: rows of 10^-6 of the largest kept x to 2 %, of 10^-8 not at all.  51200 x 256, 150 classes backward: one plane 71 us,
-// two 85, four 114; 8192 x 1024, 8192 classes 458, 559, 768.)
+// step, 2^-25, is 2^-17 of such an x); the planes' products are added up in the same registers, one plane after the other.  Weights that are alike take
+// one plane.  (One plane for all: rows of 10^-6 of the largest kept x to 2 %, of 10^-8 not at all.  51200 x 256, 150 classes backward: one plane 70 us,
+// two 81, four 106; 8192 x 1024, 8192 classes 454, 553, 754.)
 // fp32: every operand is held as three bf16 numbers (8 + 8 + 8 bits, a = h + m + l) and a product is the sum of h*h, h*m, m*h, m*m,
 // h*l, l*h in fp32: what is left out is at most 2^-22 of a product.  (The fp32 matrix instructions have a sixteenth of the bf16 rate.)
 //
@@ -124,12 +124,12 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         rsrc_t r;
         unsigned out;
         int at;
-        __device__ __forceinline__ void step(int t, int t1, int band)
+        __device__ __forceinline__ void step(int t, int t1)
         {
             if constexpr (TURNED) {
                 // (from row t * R on; what lies past a row's end is the next one's, for rows of the result that are dropped)
                 const int left = t < t1 ? min(R, o.length - t * R) : 0;
-                r = make_rsrc(base + ((long long)band * o.length + (long long)t * R) * o.row_bytes, left <= 0 ? 0u : (unsigned)(left * o.row_bytes - (base - o.base)));
+                r = make_rsrc(base + (long long)t * R * o.row_bytes, left <= 0 ? 0u : (unsigned)(left * o.row_bytes - (base - o.base)));
                 out = 0u;
                 at = 0;
             } else {
@@ -163,13 +163,10 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         }
     }
 
-    // acc[m][n]: rows a0 + (wr * WM + m) * 32 of A, rows b0 + (wc * WN + n) * 32 of B, steps t0 to t1 - 1.  BANDED: these steps for each of
-    // `bands` A (turned), one behind the other, from the last to the first, each of which counts 2^kBandBits times what is behind it.
-    template <bool BANDED = false>
+    // acc[m][n]: rows a0 + (wr * WM + m) * 32 of A, rows b0 + (wc * WN + n) * 32 of B, steps t0 to t1 - 1
     static __device__ __forceinline__ void multiply(char *smem, const Operand &a, const Operand &b, int a0, int b0, int t0, int t1,
-                                                    f32x16 (&acc)[WM][WN], int bands = 1)
+                                                    f32x16 (&acc)[WM][WN])
     {
-        static_assert(!BANDED || TA);
         const int tid = (int)threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wr = wave / WC, wc = wave % WC;
@@ -232,19 +229,10 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
         constexpr int EARLY = STAGES > 2 ? LOADS * (GROUPS - 1) / GROUPS : 0;          // of a step's loads, before its last group
         constexpr int FLYING = STAGES > 2 ? (STAGES - 3) * LOADS + EARLY : 0;          // that need not have landed there
         static_assert(GROUPS % 2 == 0 && STAGES > 1 && (AHEAD - 1) * LOADS < 64 && FLYING < 64);
-        int asked = t0, band = bands - 1;                  // the step, and its A, that is asked for next
-        auto ask = [&] {
-            sa.step(asked, t1, band);
-            sb.step(asked, t1, 0);
-            ++asked;
-            if (BANDED && asked >= t1 && band > 0) {
-                asked = t0;
-                --band;
-            }
-        };
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
-            ask();
+            sa.step(t0 + s, t1);
+            sb.step(t0 + s, t1);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j)
                 load(j, s);
@@ -255,11 +243,12 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
 #pragma unroll
         for (int f = 0; f < PL * (WM + WN); ++f)
             fetch(smem, 0, f);
-        int at = 0, left = bands - 1;                      // left: A after this one
+        int at = 0;
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const int to = STAGES == 2 ? at : at == 0 ? STAGES - 1 : at - 1;
-            ask();
+            sa.step(t + AHEAD, t1);
+            sb.step(t + AHEAD, t1);
             const char *stage = smem + at * STAGE;
 #pragma unroll
             for (int g = 0; g + 1 < GROUPS; ++g)
@@ -270,17 +259,6 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
             asm volatile("" ::: "memory");
             at = at + 1 == STAGES ? 0 : at + 1;
             products(GROUPS - 1, smem + at * STAGE, 0, EARLY, LOADS, to);
-            if (BANDED && left > 0 && t + 1 == t1) {
-                --left;
-                t = t0 - 1;
-#pragma unroll
-                for (int m = 0; m < WM; ++m)
-#pragma unroll
-                    for (int n = 0; n < WN; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            acc[m][n][r] *= 1.f / (1 << kBandBits);
-            }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (results go where the last loads write)
         __syncthreads();
@@ -594,7 +572,7 @@ __global__ __launch_bounds__(256) void dcnv4_loss_rows_in_kernel(const T *in, lo
             }
         }
         if (blockIdx.x == 0 && threadIdx.x == 0)
-            *scale = {PL == 1 ? inv * kDown : inv, bands};
+            *scale = {PL == 1 ? ldexpf(inv * kDown, (1 - bands) * kBandBits) : inv, bands};
     }
     const int units = pad / 8, unit = (int)threadIdx.x & 31;
     for (long long row = (long long)blockIdx.x * 8 + ((int)threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * 8) {
@@ -796,10 +774,26 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
             for (int r = 0; r < 16; ++r)
                 acc[m][n][r] = 0.f;
     const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
-    if constexpr (PIXELS && PL == 1)
-        G::template multiply<true>(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc, o.scale->bands);
-    else
-        G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+    G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+    if constexpr (PIXELS && PL == 1) {
+        // The other planes of x, each 2^kBandBits times less, in code of their own.  (One loop over the steps of all planes: scalar work between steps
+        // and the wait for `bands` in front of the first, 6 % of the time of 8192 x 1024, 13336 classes.)
+        const int bands = o.scale->bands;
+        Operand a = q.a;
+#pragma unroll 1
+        for (int band = 1; band < bands; ++band) {
+            a.base += a.length * a.row_bytes;
+#pragma unroll
+            for (int m = 0; m < WM; ++m)
+#pragma unroll
+                for (int n = 0; n < WN; ++n) {
+                    asm volatile("" : "+v"(acc[m][n]));
+                    acc[m][n] *= (float)(1 << kBandBits);
+                    asm volatile("" : "+v"(acc[m][n]));
+                }
+            G::multiply(smem, a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+        }
+    }
     char *out = smem + wave * (G::OUT / G::kWaves);
     const int i0 = at * G::BM + wr * 32 * WM, j0 = bt * G::BN + wc * 32 * WN;
     constexpr int ES = (int)sizeof(S), ROW = 32 * WM * ES + 16, UNITS = 32 * WM * ES / 16;
