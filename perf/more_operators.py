@@ -12,11 +12,11 @@ Block ends: z = residual + gate * scale * first(x), y = second(z); first and sec
 missing; scale per channel, gate per image.  Forms: "post" has the first norm, "pre" the second, "both" both.
 
 AdamW: m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2, p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v / (1 - b2^t)) + eps),
-g = grad * factor.  States of 8 bits: m and r = sqrt(v) in e4m3 times an fp32 scale per 256 elements of a tensor, the largest
-magnitude / 448.  m is rounded to nearest; r to one of its two neighbours, up where the 16 bits of the Philox 4x32 generator
-with ten rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011) say so, and never from above
-zero to zero.  Key = seed; counter = (i / 8 + tensor * 2^40, t), 64 bits each; element i takes number i % 8 of the block's
-eight halves, low half of a word first.
+g = grad * factor.  States of 8 bits: m and r = sqrt(v) in e4m3 times an fp32 scale per 256 elements of a tensor, which is their
+largest magnitude / 448 (below 2^-100: zeros); what is rounded is m or r times 448 / that magnitude.  m is rounded to nearest,
+r to one of its two neighbours, up where the 16 bits of the Philox 4x32 generator with ten rounds (Salmon, Moraes, Dror, Shaw:
+Parallel random numbers: as easy as 1, 2, 3; 2011) say so, and never from above zero to zero.  Key = seed; counter =
+(i / 8 + tensor * 2^40, t), 64 bits each; element i takes number i % 8 of the block's eight halves, low half of a word first.
 """
 import math
 
@@ -268,13 +268,15 @@ def _philox(first, step, seed):
 
 def _to_8_bits(v, bits):
     """(what is stored, scales) of blocks [.., 256]: to nearest, or by 16 random bits."""
-    scale = v.abs().amax(-1, keepdim=True) / 448.0
-    t = torch.where(scale > 0, v / scale, torch.zeros_like(v)).clamp(-448.0, 448.0)
+    top = v.abs().amax(-1, keepdim=True)
+    top = torch.where(top >= 2.0 ** -100, top, torch.zeros_like(top))
+    scale = top * (1.0 / 448.0)
+    t = torch.where(top > 0, v * (torch.full_like(top, 448.0) / top), torch.zeros_like(v)).clamp(-448.0, 448.0)
     if bits is not None:
         fine = ((t.view(torch.int32) + (bits << 4)) & ~0xFFFFF).view(torch.float32)
         coarse = (((t * 2.0 ** 25).int() + bits) >> 16).float() / 512.0
         rounded = torch.where(t >= 2.0 ** -6, fine, coarse)
-        t = torch.where(v > 0, rounded.clamp(min=2.0 ** -9), torch.zeros_like(t))
+        t = torch.where(t > 0, rounded.clamp(min=2.0 ** -9), torch.zeros_like(t))
     return t.to(torch.float8_e4m3fn), scale
 
 
