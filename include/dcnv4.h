@@ -300,6 +300,32 @@ int dcnv4_linear_cross_entropy_backward(const void *x, const void *w, const void
 /* Bytes of workspace the two need; -1 for arguments that they refuse.  Host-only helper. */
 long long dcnv4_linear_cross_entropy_workspace_bytes(long long P, int K, int V, int dtype, int backward);
 
+/* One tensor of dcnv4_adamw: device pointers to n elements each, in HOST memory itself. */
+typedef struct {
+    long long n;
+    float *param;             /* fp32, updated */
+    const void *grad;         /* of the call's dtype */
+    void *m, *v;              /* states, updated: fp32; or 8 bits (e4m3) of m and of sqrt(v) */
+    float *scales;            /* states of 8 bits: [(n + 255) / 256][2], of m and of sqrt(v), 8-byte aligned; else ignored */
+    void *copy;               /* F16: param rounded to fp16 after the step (what the forward pass reads), or NULL */
+    double lr, weight_decay;
+} dcnv4_adamw_tensor;
+
+/* A step of AdamW (decoupled weight decay) over `count` tensors, t = step + the number at step_on_device:
+ *     g = grad * f0,   m = beta1 * m + (1 - beta1) * g,   v = beta2 * v + (1 - beta2) * g^2
+ *     param = param * (1 - lr * f1 * weight_decay) - lr * f1 / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * tensors: host memory, read during the call only.  Each n from 1 to 2^36; no two buffers may share memory.  `dtype`: that of the gradients (and copies).
+ * step_on_device: NULL, or the device address of one 64-bit number (8-byte aligned; t is 1 where the sum is less).  factors_on_device:
+ * NULL (f0 = f1 = 1), or the device address of two fp32 numbers f0, f1 (8-byte aligned): a loss scale's inverse times what clips gradients, and a schedule's
+ * factor.  Where f0 is infinite or NaN the step changes nothing (a loss scale that was too large).  Both are for captured graphs, whose
+ * arguments stay what they were.  state_bits: 32, or 8: m and r = sqrt(v) are stored as e4m3 (fp8, largest number 448, zeros to start with), times a scale
+ * of its own for each 256 elements of the tensor: their largest magnitude / 448 (zeros for blocks below 2^-100).  m * 448 / that magnitude is rounded to nearest; r so
+ * scaled to one of its two neighbours, up with the probability that keeps its mean (random bits of dcnv4_dropout's generator with key `seed` and
+ * counter (i / 8 + number of the tensor * 2^40, t), 16 for element i as there), and never from above zero to zero.  Gradients must be finite where f0 is.
+ * 0 <= beta < 1, eps > 0 (a normal fp32 number), step >= 1 (0 with step_on_device). */
+int dcnv4_adamw(const dcnv4_adamw_tensor *tensors, int count, double beta1, double beta2, double eps, long long step,
+                const void *step_on_device, const void *factors_on_device, unsigned long long seed, int state_bits, int dtype, void *stream);
+
 /* Bytes the ideal memory-access model of Sec. 3.2 ("2HWC + 27HWG", every value touched
  * once) assigns to one forward call: x + offset + mask + y.  Host-only helper. */
 long long dcnv4_forward_algorithmic_bytes(int N, int H, int W, int G, int Cg,

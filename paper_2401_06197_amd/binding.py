@@ -28,12 +28,19 @@ EXPORTS = (
     "dcnv4_dropout", "dcnv4_dropout_backward",
     "dcnv4_dropout_add_layer_norm", "dcnv4_dropout_add_layer_norm_backward",
     "dcnv4_linear_cross_entropy", "dcnv4_linear_cross_entropy_backward", "dcnv4_linear_cross_entropy_workspace_bytes",
+    "dcnv4_adamw",
     "dcnv4_forward_algorithmic_bytes", "dcnv4_backward_algorithmic_bytes",
     "dcnv4_forward_merged_algorithmic_bytes", "dcnv4_backward_merged_algorithmic_bytes",
     "dcnv4_set_option", "dcnv4_last_kernel_name", "dcnv4_status_string",
 )
 
 _lib = None
+
+
+class AdamwTensor(ctypes.Structure):
+    """dcnv4_adamw_tensor."""
+    _fields_ = [("n", ctypes.c_longlong), ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("lr", ctypes.c_double), ("weight_decay", ctypes.c_double)]
 
 
 class Dcnv4Error(RuntimeError):
@@ -103,6 +110,9 @@ def load_library():
     for f in (lib.dcnv4_layer_norm, lib.dcnv4_layer_norm_backward, lib.dcnv4_dropout, lib.dcnv4_dropout_backward,
               lib.dcnv4_dropout_add_layer_norm, lib.dcnv4_dropout_add_layer_norm_backward):
         f.restype = ci
+    cd = ctypes.c_double
+    lib.dcnv4_adamw.argtypes = [ctypes.POINTER(AdamwTensor), ci, cd, cd, cd, ll, vp, vp, ull, ci, ci, vp]
+    lib.dcnv4_adamw.restype = ci
     lib.dcnv4_set_option.argtypes = [ctypes.c_char_p, ci]
     lib.dcnv4_set_option.restype = ci
     lib.dcnv4_last_kernel_name.argtypes = [ci]
@@ -766,3 +776,96 @@ def dcnv4_linear_cross_entropy_backward(x, w, target, lse, grad_loss, b=None, ig
         return _prepared(args, out, workspace)
     _call(x.device, "dcnv4_linear_cross_entropy_backward", args)
     return gx, gw, gb
+
+
+class AdamwPlan:
+    """The tensors of a dcnv4_adamw_step, checked and listed once (dcnv4_adamw_plan makes it).  It holds the tensors themselves: their
+    gradients are read where they are at each step."""
+
+    def __init__(self, records, held, device, state_bits, dtype):
+        self.records, self.held, self.device, self.state_bits, self.dtype = records, held, device, state_bits, dtype
+
+    def __len__(self):
+        return len(self.records)
+
+    def set(self, lr=None, weight_decay=None):
+        """Other learning rates or weight decays from the next step on: a number, or one for each tensor."""
+        for name, values in (("lr", lr), ("weight_decay", weight_decay)):
+            if values is not None:
+                for record, value in zip(self.records, _each(values, len(self), name)):
+                    setattr(record, name, value)
+
+
+def _each(values, count, name):
+    values = [float(v) for v in values] if isinstance(values, (list, tuple)) else [float(values)] * count
+    if len(values) != count:
+        raise ValueError(f"dcnv4: {name} must be a number, or one for each of {count} tensors")
+    return values
+
+
+def dcnv4_adamw_plan(params, grads, exp_avgs, exp_avg_sqs, lr, weight_decay=0.0, scales=None, copies=None):
+    """What dcnv4_adamw_step takes: lists of as many tensors each, of any shapes.  params float32; grads all float32 or all float16; exp_avgs and
+    exp_avg_sqs all float32, or, for states of 8 bits, all torch.float8_e4m3fn (m, and the root of v), with `scales`: float32 [(n + 255) // 256, 2]
+    for a tensor of n elements (m is exp_avg * scales[:, 0], the root of v exp_avg_sq * scales[:, 1], a scale for each 256 elements; zeros to
+    start with).  copies (with float16 gradients): float16 tensors, or None in the place of one, that get the parameters after each step.  lr,
+    weight_decay: a number, or one for each tensor."""
+    import torch
+    params, grads, ms, vs = list(params), list(grads), list(exp_avgs), list(exp_avg_sqs)
+    count = len(params)
+    lists = [("grads", grads), ("exp_avgs", ms), ("exp_avg_sqs", vs)]
+    scales = [None] * count if scales is None else list(scales)
+    copies = [None] * count if copies is None else list(copies)
+    lists += [("scales", scales), ("copies", copies)]
+    if count < 1 or any(len(l) != count for _, l in lists):
+        raise ValueError("dcnv4: expected lists of as many tensors each, one at least")
+    if not params[0].is_cuda:
+        raise ValueError("dcnv4: params must be GPU tensors")
+    at, device, state = params[0].get_device(), params[0].device, ms[0].dtype
+    if state is not torch.float32 and state is not torch.float8_e4m3fn:
+        raise TypeError(f"dcnv4: unsupported state dtype {state}")
+    eight, dtype = state is torch.float8_e4m3fn, _dtype_code(grads[0])
+    written, read = [], []
+    for i, (p, g, m, v, s, c) in enumerate(zip(params, grads, ms, vs, scales, copies)):
+        n, shape = p.numel(), p.shape
+        _check_plain(f"params[{i}]", p, at, shape, torch.float32)
+        _check_plain(f"grads[{i}]", g, at, shape, grads[0].dtype)
+        _check_plain(f"exp_avgs[{i}]", m, at, shape, state)
+        _check_plain(f"exp_avg_sqs[{i}]", v, at, shape, state)
+        if eight != (s is not None):
+            raise ValueError("dcnv4: states of 8 bits come with scales, and no others")
+        if eight:
+            _check_plain(f"scales[{i}]", s, at, ((n + 255) // 256, 2), torch.float32)
+        if c is not None:
+            if dtype != DCNV4_F16:
+                raise ValueError("dcnv4: copies come with float16 gradients")
+            _check_plain(f"copies[{i}]", c, at, shape, torch.float16)
+        written += [(t.data_ptr(), t.data_ptr() + t.nbytes, True) for t in (p, m, v, s, c) if t is not None]
+        read.append((g.data_ptr(), g.data_ptr() + g.nbytes, False))
+    # what is written overlaps nothing else (gradients may)
+    end, last = 0, False
+    for first, after, out in sorted(written + read):
+        if first < end and (out or last):
+            raise ValueError("dcnv4: parameters, states and copies must not share memory")
+        if after > end:
+            end, last = after, out
+    records = (AdamwTensor * count)()
+    ptr = lambda t: None if t is None else t.data_ptr()
+    for r, p, g, m, v, s, c in zip(records, params, grads, ms, vs, scales, copies):
+        r.n, r.param, r.grad, r.m, r.v, r.scales, r.copy = p.numel(), ptr(p), ptr(g), ptr(m), ptr(v), ptr(s), ptr(c)
+    plan = AdamwPlan(records, (params, grads, ms, vs, scales, copies), device, 8 if eight else 32, dtype)
+    plan.set(lr=lr, weight_decay=weight_decay)
+    return plan
+
+
+def dcnv4_adamw_step(plan, step, betas=(0.9, 0.999), eps=1e-8, seed=0, step_on_device=None, factors_on_device=None, stream=None):
+    """A step of AdamW (include/dcnv4.h) over the plan's tensors, in place.  step: the number of this step, from 1 on; step_on_device: one int64 on
+    the GPU that is added to it (captured graphs).  factors_on_device: two float32 on the GPU, which gradients and learning rates are multiplied
+    with; a first one that is not finite leaves everything as it is.  seed: of the rounding of states of 8 bits."""
+    import torch
+    factors = None
+    if factors_on_device is not None:
+        _check_plain("factors_on_device", factors_on_device, plan.device.index, (2,), torch.float32)
+        factors = factors_on_device.data_ptr()
+    args = (plan.records, len(plan), float(betas[0]), float(betas[1]), float(eps), int(step), _offset_ptr(plan.held[0][0], step_on_device), factors,
+            int(seed) & _MASK64, plan.state_bits, plan.dtype, _stream_ptr(stream, plan.device))
+    _call(plan.device, "dcnv4_adamw", args)
