@@ -221,7 +221,7 @@ def _run_own(s):
     if op in ("end", "end_train"):
         first = (s["gamma1"], s["beta1"]) if "gamma1" in s else None
         second = (s["gamma2"], s["beta2"]) if "gamma2" in s else None
-        z, y, *stats = dcn.dcnv4_norm_scale_add_norm(s["x"], s["residual"], s["scale"], s["gate"], first, second, eps=NORM_EPS)
+        z, y, *stats = dcn.dcnv4_norm_scale_add_norm(s["x"], s["residual"], s["scale"], s["gate"], first, second, eps=NORM_EPS, stats=op != "end")
         if op == "end":
             return z, y
         return (z, y, *dcn.dcnv4_norm_scale_add_norm_backward(s["x"], z, s["scale"], s["gate"], first, second, stats, s["grad_y"], s["grad_z"],
