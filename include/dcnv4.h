@@ -271,6 +271,34 @@ int dcnv4_dropout_add_layer_norm_backward(const void *z, const void *gamma, cons
                                           long long P, int C, float p, unsigned long long seed, unsigned long long offset,
                                           const void *offset_on_device, int dtype, void *stream);
 
+/* The end of a residual block with its norms, in one pass:
+ *     b = first norm of x (DCNV4_FIRST_NORM; else b = x),   z = residual + gate * scale * b,   y = second norm of z as stored (DCNV4_SECOND_NORM)
+ * The norms as in dcnv4_layer_norm with gamma1, beta1 and gamma2, beta2 [C], each NULL for ones or zeros, and one eps.  `norms`: which there are, or 0.
+ * scale [C] (of `dtype`) or NULL (ones).  gate: fp32, one for each of `gates` images of P / gates rows, or NULL with gates = 0 (ones); a gate of 0 leaves
+ * z = residual, whatever x holds.  x, residual, z, y [P][C]; y NULL without a second norm.  mean1, rstd1, mean2, rstd2: fp32 [P] for the
+ * backward pass, or NULL.  C from 1 to 8192; with gates, P below 2^31 and a multiple of gates, gates up to 2^20. */
+enum { DCNV4_FIRST_NORM = 1, DCNV4_SECOND_NORM = 2 };
+int dcnv4_norm_scale_add_norm(const void *x, const void *residual, const void *gamma1, const void *beta1, const void *scale, const float *gate,
+                              const void *gamma2, const void *beta2, void *z, void *y, float *mean1, float *rstd1, float *mean2, float *rstd2,
+                              long long P, int C, int gates, int norms, float eps, int dtype, void *stream);
+
+/* Its backward pass.  grad_y: the gradient of y; grad_z: that of z from what else reads it (NULL for none, with a second norm).  With gz the sum of grad_z
+ * and the second norm's grad_x at z (before its rounding), and h = gz * gate * scale:
+ *     grad_residual = gz (without a second norm that is grad_z itself, and nothing is written: NULL)
+ *     grad_x = the first norm's gradient for h (or h),    grad_scale [C] = sum over the rows of gz * gate * b,
+ *     grad_gate [gates] = sum over the image's rows and channels of gz * scale * b (fp32),   grad_gamma1, ... [C] as in dcnv4_layer_norm_backward
+ * Any of grad_scale, grad_gate and the norms' four may be NULL where not wanted (all: no workspace is needed).  Rows with a gate of 0 have
+ * grad_x 0 and count for nothing, whatever x holds, but in grad_gate.  Sums are fp32 in a fixed order.  z is read with a second norm only.
+ * `workspace`: at least dcnv4_norm_scale_add_norm_workspace_bytes(P, C, gates) bytes. */
+int dcnv4_norm_scale_add_norm_backward(const void *x, const void *z, const void *gamma1, const void *beta1, const void *scale, const float *gate,
+                                       const void *gamma2, const float *mean1, const float *rstd1, const float *mean2, const float *rstd2,
+                                       const void *grad_y, const void *grad_z, void *grad_x, void *grad_residual, void *grad_scale, float *grad_gate,
+                                       void *grad_gamma1, void *grad_beta1, void *grad_gamma2, void *grad_beta2, void *workspace,
+                                       long long workspace_bytes, long long P, int C, int gates, int norms, int dtype, void *stream);
+
+/* Bytes of workspace it needs; -1 for a bad argument.  Host-only helper. */
+long long dcnv4_norm_scale_add_norm_workspace_bytes(long long P, int C, int gates);
+
 /* Softmax cross entropy out of the last linear layer (a classifier's, or each pixel's), without its logits being stored:
  *     logit[p][v] = sum_k x[p][k] * w[v][k] + b[v],   lse[p] = log sum_v exp(logit[p][v]),   loss[p] = lse[p] - logit[p][target[p]]
  * x [P][K], w [V][K], b [V] or NULL; target: 64-bit class numbers [P]; loss, lse: fp32 [P].  A row whose target is ignore_index

@@ -355,34 +355,8 @@ __global__ __launch_bounds__(norm_threads(L)) void dcnv4_norm_backward_kernel(No
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 v[e] = k == 0 ? dg[j][e] : db[j][e];
-            if constexpr (R > 1) {
-                // rows side by side in a wave first: lanes 8, 4, 2, 1 further round (of 16), then rows of 16 and halves
-                constexpr int G = L < 64 ? L : 64, W = norm_threads(L) / 64;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if constexpr (G < 16) v[e] += dpp<0x128>(v[e]);
-                    if constexpr (G < 8) v[e] += dpp<0x124>(v[e]);
-                    if constexpr (G < 4) v[e] += dpp<0x122>(v[e]);
-                    if constexpr (G < 2) v[e] += dpp<0x121>(v[e]);
-                    if constexpr (G < 32) v[e] = add_rows(v[e]);
-                    if constexpr (G < 64) v[e] = add_halves(v[e]);
-                }
-                // then the waves: all of them (rows of a wave and less), or those with the same part of a row
-                constexpr int PARTS = L < 64 ? 1 : L / 64;
-                const int wave = (int)threadIdx.x >> 6, in = l % G;
-                __syncthreads();                           // all have read what was there before
-                if ((int)(threadIdx.x & 63) < G)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        sums[(wave * 8 + e) * G + in] = v[e];
-                __syncthreads();
-                if (first == 0)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int w = PARTS; w < W; w += PARTS)
-                            v[e] += sums[((w + wave) * 8 + e) * G + in];
-            }
+            if constexpr (R > 1)
+                add_rows_of_workgroup<L, norm_threads(L)>(v, sums);
             if (first == 0)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)

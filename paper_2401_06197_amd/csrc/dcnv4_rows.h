@@ -177,6 +177,38 @@ template <int L, int N> __device__ __forceinline__ void row_sums(float (&v)[N], 
     }
 }
 
+// Eight numbers of each lane summed over the rows that THREADS lanes hold side by side, L lanes a row, in the lanes of the first row.
+// `sums`: THREADS * 8 numbers.
+template <int L, int THREADS> __device__ __forceinline__ void add_rows_of_workgroup(float (&v)[8], float *sums)
+{
+    // rows side by side in a wave first: lanes 8, 4, 2, 1 further round (of 16), then rows of 16 and halves
+    constexpr int G = L < 64 ? L : 64, W = THREADS / 64;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (G < 16) v[e] += dpp<0x128>(v[e]);
+        if constexpr (G < 8) v[e] += dpp<0x124>(v[e]);
+        if constexpr (G < 4) v[e] += dpp<0x122>(v[e]);
+        if constexpr (G < 2) v[e] += dpp<0x121>(v[e]);
+        if constexpr (G < 32) v[e] = add_rows(v[e]);
+        if constexpr (G < 64) v[e] = add_halves(v[e]);
+    }
+    // then the waves: all of them (rows of a wave and less), or those with the same part of a row
+    constexpr int PARTS = L < 64 ? 1 : L / 64;
+    const int wave = (int)threadIdx.x >> 6, in = (int)threadIdx.x % L % G;
+    __syncthreads();                                       // all have read what was there before
+    if ((int)(threadIdx.x & 63) < G)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sums[(wave * 8 + e) * G + in] = v[e];
+    __syncthreads();
+    if ((int)threadIdx.x < L)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int w = PARTS; w < W; w += PARTS)
+                v[e] += sums[((w + wave) * 8 + e) * G + in];
+}
+
 constexpr int norm_threads(int L) { return L >= 256 ? 512 : 256; }
 
 // Where a lane's run j lies in its row, in runs: side by side in a wave, then run after run, then the next wave's.

@@ -60,3 +60,82 @@ def adamw(p, g, m, v, lr, wd, betas, eps, t, factors=(1.0, 1.0)):
     lr = lr * factors[1]
     move = lr / (1 - betas[0] ** t) * m / (np.sqrt(v / (1 - betas[1] ** t)) + eps)
     return p * (1 - lr * wd) - move, m, v, np.abs(move)
+
+
+E24 = 2.0 ** -24
+
+
+def norm(x, gamma, beta, eps):
+    mean = x.mean(-1)
+    rstd = 1 / np.sqrt(((x - mean[..., None]) ** 2).mean(-1) + eps)
+    return (x - mean[..., None]) * rstd[..., None] * gamma + beta, mean, rstd
+
+
+def norm_backward(x, mean, rstd, g, dg, k):
+    """The gradient at x for g at the unit rows, xhat, and how far fp32 sums of k terms in a chain, and dg of g, may take them."""
+    mean, rstd = mean[..., None], rstd[..., None]
+    xh, dxh = (x - mean) * rstd, 4 * E24 * (np.abs(x) + np.abs(mean)) * np.abs(rstd)
+    avg = lambda v: v.mean(-1, keepdims=True)
+    a, b = avg(g), avg(g * xh)
+    da = avg(dg) + k * E24 * avg(np.abs(g))
+    db = avg(np.abs(xh) * dg + np.abs(g) * dxh) + k * E24 * avg(np.abs(g * xh))
+    gx = rstd * (g - a - xh * b)
+    dgx = rstd * (dg + da + np.abs(xh) * db + dxh * np.abs(b)) + 8 * E24 * rstd * (np.abs(g) + np.abs(a) + np.abs(xh * b))
+    return gx, dgx, xh, dxh
+
+
+def end(x, residual, scale, gate, first, eps):
+    """z, and what it is made of: b.  scale, gate [N] and first = (gamma, beta) are arrays or None."""
+    x = x.astype(np.float64)
+    b = x if first is None else norm(x, *first, eps)[0]
+    by = np.ones(x.shape[:1]) if gate is None else gate.astype(np.float64)
+    by = by.reshape(-1, *[1] * (x.ndim - 1)) * (1.0 if scale is None else scale)
+    return residual.astype(np.float64) + np.where(by == 0, 0.0, by * b), b
+
+
+def end_backward(x, z, scale, gate, first, second, stats, gy, gz, k=64, rows=256):
+    """{name: (gradient, how far fp32 sums may take it)}; k, rows: terms in a chain of a row's sum and of one over rows."""
+    f = lambda a: None if a is None else np.asarray(a, dtype=np.float64)
+    x, z, gy, gz, scale, gate = map(f, (x, z, gy, gz, scale, gate))
+    pixels = tuple(range(x.ndim - 1))
+    out = {}
+    add = lambda v, dv: (v.sum(pixels), dv.sum(pixels) + rows * E24 * np.abs(v).sum(pixels))
+    g, dg = (np.zeros(x.shape) if gz is None else gz), np.zeros(x.shape)
+    if second is not None:
+        gx, dgx, zh, dzh = norm_backward(z, stats[2], stats[3], gy * second[0], 2 * E24 * np.abs(gy * second[0]), k)
+        g, dg = g + gx, dgx + 2 * E24 * (np.abs(g) + np.abs(gx))
+        out["grad_gamma2"] = add(gy * zh, np.abs(gy) * dzh + 2 * E24 * np.abs(gy * zh))
+        out["grad_beta2"] = add(gy, 0 * gy)
+    out["grad_residual"] = g, dg
+    by = np.ones(x.shape[:1]) if gate is None else gate
+    by = np.broadcast_to(by.reshape(-1, *[1] * (x.ndim - 1)), x.shape)
+    sc = np.ones(x.shape[-1]) if scale is None else scale
+    if first is not None:
+        xh = (x - stats[0][..., None]) * stats[1][..., None]
+        dxh = 4 * E24 * (np.abs(x) + np.abs(stats[0][..., None])) * stats[1][..., None]
+        gamma, beta = first
+    else:
+        xh, dxh, gamma, beta = x, 0 * x, np.ones(x.shape[-1]), np.zeros(x.shape[-1])
+    b, db = xh * gamma + beta, dxh * np.abs(gamma) + 2 * E24 * (np.abs(xh * gamma) + np.abs(beta))
+    image = tuple(range(1, x.ndim))
+    t, dt = g * sc * b, np.abs(sc) * (np.abs(g) * db + dg * np.abs(b)) + 4 * E24 * np.abs(g * sc * b)
+    out["grad_gate"] = t.sum(image), dt.sum(image) + (k + rows) * E24 * np.abs(t).sum(image)
+    on = by != 0
+    q, dq = np.where(on, by * g, 0), np.where(on, np.abs(by) * dg + 2 * E24 * np.abs(by * g), 0)
+    xz, dxz = np.where(on, xh, 0), np.where(on, dxh, 0)
+    s1, ds1 = add(q * xz, np.abs(q) * dxz + dq * np.abs(xz) + 2 * E24 * np.abs(q * xz))
+    s0, ds0 = add(q, dq)
+    if first is None:
+        out["grad_scale"] = s1, ds1
+    else:
+        out["grad_scale"] = gamma * s1 + beta * s0, np.abs(gamma) * ds1 + np.abs(beta) * ds0 + 4 * E24 * (np.abs(gamma * s1) + np.abs(beta * s0))
+        out["grad_gamma1"] = sc * s1, np.abs(sc) * ds1 + 2 * E24 * np.abs(sc * s1)
+        out["grad_beta1"] = sc * s0, np.abs(sc) * ds0 + 2 * E24 * np.abs(sc * s0)
+    h, dh = q * sc * gamma, np.abs(sc * gamma) * dq + 4 * E24 * np.abs(q * sc * gamma)
+    if first is None:
+        out["grad_x"] = h, dh
+    else:
+        xs, m, r = (np.where(on, a, 0) for a in (x, np.broadcast_to(stats[0][..., None], x.shape), np.broadcast_to(stats[1][..., None], x.shape)))
+        gx, dgx, _, _ = norm_backward(xs, m[..., 0], r[..., 0], h, dh, k)
+        out["grad_x"] = np.where(on, gx, 0), np.where(on, dgx, 0)
+    return out

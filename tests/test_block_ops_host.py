@@ -63,3 +63,71 @@ def test_plain_8_bit_numbers_are_the_types():
     # and keeps the mean
     x = np.full(200000, 3.3)
     assert abs(ref.e4m3_by(x, rng.integers(0, 65536, x.size).astype(float)).mean() - 3.3) < 5 * 0.125 / np.sqrt(x.size)
+
+
+def without(count, i, value=None):
+    ptrs = [A] * count
+    ptrs[i] = value
+    return tuple(ptrs)
+
+
+def end(ptrs=(A,) * 14, P=6, C=16, gates=2, norms=3, eps=1e-6, dtype=0):
+    return dcn.load_library().dcnv4_norm_scale_add_norm(*ptrs, P, C, gates, norms, eps, dtype, None)
+
+
+def end_back(ptrs=(A,) * 22, size=1 << 30, P=6, C=16, gates=2, norms=3, dtype=0):
+    return dcn.load_library().dcnv4_norm_scale_add_norm_backward(*ptrs, size, P, C, gates, norms, dtype, None)
+
+
+def test_block_end_validates_on_the_host():
+    for i in (0, 1, 5, 8, 9):
+        assert end(without(14, i)) == 1
+    for i in (0, 1, 7, 8, 9, 10, 11, 13, 14, 5, 21):
+        assert end_back(without(22, i)) == 1, i
+    assert end_back(without(22, 12), norms=1) == 1                # without a second norm, grad_z is the gradient
+    for i in range(14):
+        assert end(without(14, i, A + 8)) == 4
+    for i in range(22):
+        assert end_back(without(22, i, A + 8)) == 4
+    for call in (end, end_back):
+        assert call(P=0) == 2 and call(C=0) == 2 and call(P=-1) == 2 and call(gates=-1) == 2 and call(gates=4) == 2
+        assert call(C=8193) == 3 and call(dtype=2) == 3 and call(norms=4) == 3 and call(norms=-1) == 3
+        assert call(P=1 << 31) == 3 and call(P=(1 << 20) + 1, gates=(1 << 20) + 1) == 3
+    assert end(eps=-1.0) == 3 and end(eps=float("nan")) == 3 and end(eps=float("inf")) == 3
+    need = dcn.dcnv4_norm_scale_add_norm_workspace_bytes
+    assert end_back(size=need(6, 16, 2) - 1) == 2 and end_back(gates=0) == 2
+    assert need(0, 16, 0) == -1 and need(5, 16, 2) == -1 and need(4, 9000, 0) == -1 and need(6, 16, 2) > need(6, 16, 0) > 0
+    assert need(10 ** 9, 8192, 0) < 1 << 30
+
+
+@pytest.mark.parametrize("form", ["", "f", "s", "fs"])
+def test_gradient_of_the_plain_block_end_against_differences(form):
+    rng = np.random.default_rng(1)
+    r = lambda *s: rng.standard_normal(s)
+    shape, eps = (2, 3, 5), 1e-3
+    v = {"x": r(*shape), "residual": r(*shape), "scale": r(5), "gate": np.array([0.0, 1.3]), "gamma1": r(5), "beta1": r(5), "gamma2": r(5), "beta2": r(5)}
+    gy, gz = r(*shape), r(*shape)
+
+    def forward(v):
+        z, _ = ref.end(v["x"], v["residual"], v["scale"], v["gate"], (v["gamma1"], v["beta1"]) if "f" in form else None, eps)
+        return z, ref.norm(z, v["gamma2"], v["beta2"], eps)[0] if "s" in form else None
+
+    def value(v):
+        z, y = forward(v)
+        return (z * gz).sum() + (0 if y is None else (y * gy).sum())
+
+    z, _ = forward(v)
+    _, m1, r1 = ref.norm(v["x"], 1.0, 0.0, eps)
+    _, m2, r2 = ref.norm(z, 1.0, 0.0, eps)
+    got = ref.end_backward(v["x"], z, v["scale"], v["gate"], (v["gamma1"], v["beta1"]) if "f" in form else None,
+                           (v["gamma2"], v["beta2"]) if "s" in form else None, (m1, r1, m2, r2), gy, gz)
+    step = 1e-6
+    for name, (grad, _) in got.items():
+        at = name[len("grad_"):]
+        for i in range(grad.size):
+            moved = []
+            for sign in (1, -1):
+                w = {k: a.copy() for k, a in v.items()}
+                w[at].reshape(-1)[i] += sign * step
+                moved.append(value(w))
+            assert abs((moved[0] - moved[1]) / (2 * step) - grad.reshape(-1)[i]) < 1e-6, (name, i)
