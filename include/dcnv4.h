@@ -153,6 +153,40 @@ int dcnv4_backward_softmax(const void *x, const void *offset, const void *mask_l
 int dcnv4_linear(const void *x, const void *w, const void *b, void *y,
                  long long P, int K, int Nout, int dtype, void *stream);
 
+/* Its backward pass, from grad_y [P][Nout]:
+ *     grad_x[p] = sum_o grad_y[p][o] * w[o],   grad_w[o] = sum_p grad_y[p][o] * x[p],   grad_b[o] = sum_p grad_y[p][o]
+ * Each of the three may be NULL where not wanted (not all); x is read for grad_w alone, w for grad_x alone.  Sums are fp32 in a fixed order, rounded once in
+ * F16.  F32: operands as three bf16 numbers, fp32's accuracy for numbers above 2^-100; finite and below 3.3e38.
+ * Needs K and Nout multiples of 8, at most 2^24 rows, K and Nout at most 2^20 (else DCNV4_ERR_UNSUPPORTED).
+ * `workspace`: at least dcnv4_linear_backward_workspace_bytes() bytes. */
+int dcnv4_linear_backward(const void *x, const void *w, const void *grad_y, void *grad_x, void *grad_w, void *grad_b, void *workspace,
+                          long long workspace_bytes, long long P, int K, int Nout, int dtype, void *stream);
+
+/* Bytes of workspace it needs; -1 for arguments that it refuses.  Host-only helper. */
+long long dcnv4_linear_backward_workspace_bytes(long long P, int K, int Nout, int dtype);
+
+/* The gated layer of a block's feed-forward part, both projections, the activation and the product in one kernel:
+ *     a = x w[0]^T + b[0],   u = x w[1]^T + b[1],   h = act(a) * u
+ * act: DCNV4_SILU (a / (1 + exp(-a))) or DCNV4_GELU (a times the normal distribution function).  x [P][K], w [2][F][K], b [2][F] or NULL, h [P][F].
+ * Nothing but h is stored, with one rounding.  F32 as in dcnv4_linear_backward.  Needs K and F multiples of 8, at most 2^24 rows,
+ * K at most 2^20, F at most 2^19, and w below 2 GiB (F32: below 1.33) (else DCNV4_ERR_UNSUPPORTED).
+ * `workspace`: at least dcnv4_gated_linear_workspace_bytes(..., backward = 0) bytes, NULL where that is 0 (F16). */
+enum { DCNV4_SILU = 0, DCNV4_GELU = 1 };
+int dcnv4_gated_linear(const void *x, const void *w, const void *b, void *h, void *workspace, long long workspace_bytes, long long P, int K, int F,
+                       int activation, int dtype, void *stream);
+
+/* Its backward pass, from grad_h [P][F]; a and u are made again.  With da = grad_h * u * act'(a) and du = grad_h * act(a):
+ *     grad_x[p] = sum_f da[p][f] * w[0][f] + du[p][f] * w[1][f],   grad_w = (sum_p da[p][f] * x[p], sum_p du[p][f] * x[p]),   grad_b = sums over the rows
+ * Each of the three may be NULL where not wanted (not all).  In F16 da and du are rounded to fp16, times a power of two that puts the largest finite
+ * |grad_h| into [2, 4), for grad_x and grad_w: they keep all of fp16's bits down to 2^-16 of it, and u * act'(a) and act(a) have to be less than 16000.
+ * grad_b is made from fp32 numbers alone.  Sums are fp32 in a fixed order.
+ * `workspace`: at least dcnv4_gated_linear_workspace_bytes(..., backward = 1) bytes. */
+int dcnv4_gated_linear_backward(const void *x, const void *w, const void *b, const void *grad_h, void *grad_x, void *grad_w, void *grad_b, void *workspace,
+                                long long workspace_bytes, long long P, int K, int F, int activation, int dtype, void *stream);
+
+/* Bytes of workspace the two need; -1 for arguments that they refuse.  Host-only helper. */
+long long dcnv4_gated_linear_workspace_bytes(long long P, int K, int F, int dtype, int backward);
+
 /* The 3x3 depthwise convolution of the separable structure that computes offsets and scalars in the
  * module (Sec. 3.2 "Micro design"), zero padding, stride 1, channel-last:
  *     y[n,h,w,c] = b[c] + sum_{i,j in 0..2} w[i][j][c] * x[n, h+i-1, w+j-1, c]      (x = 0 outside the map)
@@ -400,6 +434,8 @@ long long dcnv4_backward_merged_algorithmic_bytes(int N, int H, int W, int G, in
  *   "loss_tile"   tile of the cross entropy's products, classes x pixels: 1 = 64x64, 2 = 128x128, 3 = 256x256 (fp32: 256x128)
  *   "loss_splits" workgroups that share a sum of its gradients (1..64)
  *   "loss_piece"  classes of a piece (rounded up to a multiple of 256); these three change the size of its workspace
+ *   "layer_tile"  tile of the gated layer's and the layers' gradients' products, as "loss_tile"
+ *   "layer_splits" workgroups that share a sum of those gradients (1..64); both change the size of their workspaces
  *   "gom_coop"    1 = the fp32 grad_offset/grad_mask pass moves its values through per-wave LDS slices
  *                 even for whole groups (default: each lane reads and writes its own pixel's values)
  *   "gx_threads"  workgroup size of the staged grad_x kernel (256, 512 or 768)

@@ -28,6 +28,8 @@ EXPORTS = (
     "dcnv4_dropout", "dcnv4_dropout_backward",
     "dcnv4_dropout_add_layer_norm", "dcnv4_dropout_add_layer_norm_backward",
     "dcnv4_linear_cross_entropy", "dcnv4_linear_cross_entropy_backward", "dcnv4_linear_cross_entropy_workspace_bytes",
+    "dcnv4_linear_backward", "dcnv4_linear_backward_workspace_bytes",
+    "dcnv4_gated_linear", "dcnv4_gated_linear_backward", "dcnv4_gated_linear_workspace_bytes",
     "dcnv4_norm_scale_add_norm", "dcnv4_norm_scale_add_norm_backward", "dcnv4_norm_scale_add_norm_workspace_bytes",
     "dcnv4_adamw",
     "dcnv4_forward_algorithmic_bytes", "dcnv4_backward_algorithmic_bytes",
@@ -111,6 +113,13 @@ def load_library():
     for f in (lib.dcnv4_layer_norm, lib.dcnv4_layer_norm_backward, lib.dcnv4_dropout, lib.dcnv4_dropout_backward,
               lib.dcnv4_dropout_add_layer_norm, lib.dcnv4_dropout_add_layer_norm_backward):
         f.restype = ci
+    lib.dcnv4_linear_backward.argtypes = [vp] * 7 + [ll, ll, ci, ci, ci, vp]
+    lib.dcnv4_gated_linear.argtypes = [vp] * 5 + [ll, ll, ci, ci, ci, ci, vp]
+    lib.dcnv4_gated_linear_backward.argtypes = [vp] * 8 + [ll, ll, ci, ci, ci, ci, vp]
+    lib.dcnv4_linear_backward.restype = lib.dcnv4_gated_linear.restype = lib.dcnv4_gated_linear_backward.restype = ci
+    lib.dcnv4_linear_backward_workspace_bytes.argtypes = [ll, ci, ci, ci]
+    lib.dcnv4_gated_linear_workspace_bytes.argtypes = [ll, ci, ci, ci, ci]
+    lib.dcnv4_linear_backward_workspace_bytes.restype = lib.dcnv4_gated_linear_workspace_bytes.restype = ll
     lib.dcnv4_norm_scale_add_norm.argtypes = [vp] * 14 + [ll, ci, ci, ci, cf, ci, vp]
     lib.dcnv4_norm_scale_add_norm_backward.argtypes = [vp] * 22 + [ll, ll, ci, ci, ci, ci, vp]
     lib.dcnv4_norm_scale_add_norm.restype = lib.dcnv4_norm_scale_add_norm_backward.restype = ci
@@ -872,6 +881,76 @@ def dcnv4_norm_scale_add_norm_backward(x, z, scale, gate, first, second, stats, 
         return _prepared(args, out, *(() if space is None else (workspace,)))
     _call(x.device, "dcnv4_norm_scale_add_norm_backward", args)
     return (results[0], grad_z if second is None else results[1], *results[2:])
+
+
+def dcnv4_linear_backward_workspace_bytes(P, K, Nout, dtype):
+    return int(load_library().dcnv4_linear_backward_workspace_bytes(P, K, Nout, dtype))
+
+
+def dcnv4_linear_backward(x, w, grad_y, b=None, need_x=True, workspace=None, out=None, stream=None, prepare_only=False):
+    """(grad_x, grad_w, grad_b) of dcnv4_linear for grad_y [..., Nout]; grad_b is None where b is, grad_x with need_x=False (a first layer)."""
+    P, K = _rows(x)
+    if w.dim() != 2 or w.shape[1] != K:
+        raise ValueError("dcnv4: expected x [..., K], w [Nout, K]")
+    N, shape, dt = w.shape[0], x.shape, x.dtype
+    _check_like(x, (("w", w, w.shape), ("b", b, (N,)), ("grad_y", grad_y, (*shape[:-1], N))))
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt), None if b is None else ("grad_b", (N,), dt)), stream)
+    space, size = _workspace(x, workspace, dcnv4_linear_backward_workspace_bytes(P, K, N, _dtype_code(x)) if workspace is None else 0, stream)
+    args = (x.data_ptr(), w.data_ptr(), grad_y.data_ptr(), _ptr(gx), gw.data_ptr(), _ptr(gb), space.data_ptr(), size, P, K, N, _dtype_code(x),
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return _prepared(args, out, workspace)
+    _call(x.device, "dcnv4_linear_backward", args)
+    return gx, gw, gb
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def dcnv4_gated_linear_workspace_bytes(P, K, F, dtype, backward):
+    return int(load_library().dcnv4_gated_linear_workspace_bytes(P, K, F, dtype, int(bool(backward))))
+
+
+def _gated_args(x, w, b, activation):
+    P, K = _rows(x)
+    if w.dim() != 3 or w.shape[0] != 2 or w.shape[2] != K:
+        raise ValueError("dcnv4: expected x [..., K], w [2, F, K]")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"dcnv4: activation must be one of {', '.join(ACTIVATIONS)}")
+    F = w.shape[1]
+    _check_like(x, (("w", w, w.shape), ("b", b, (2, F))))
+    return P, K, F, ACTIVATIONS[activation]
+
+
+def dcnv4_gated_linear(x, w, b=None, activation="silu", workspace=None, out=None, stream=None, prepare_only=False):
+    """h = act(x w[0]^T + b[0]) * (x w[1]^T + b[1]): x [..., K], w [2, F, K], b [2, F], h [..., F]; activation "silu" or "gelu" (with erf)."""
+    P, K, F, act = _gated_args(x, w, b, activation)
+    h, = _outputs(x, out, (("h", (*x.shape[:-1], F), x.dtype),), stream)
+    code = _dtype_code(x)
+    space, size = None, 0
+    if code == DCNV4_F32 or workspace is not None:
+        space, size = _workspace(x, workspace, dcnv4_gated_linear_workspace_bytes(P, K, F, code, False) if workspace is None else 0, stream)
+    args = (x.data_ptr(), w.data_ptr(), _ptr(b), h.data_ptr(), _ptr(space), size, P, K, F, act, code, _stream_ptr(stream, x.device))
+    if prepare_only:
+        return _prepared(args, out, *(() if code == DCNV4_F16 else (workspace,)))
+    _call(x.device, "dcnv4_gated_linear", args)
+    return h
+
+
+def dcnv4_gated_linear_backward(x, w, grad_h, b=None, activation="silu", need_x=True, workspace=None, out=None, stream=None, prepare_only=False):
+    """(grad_x, grad_w, grad_b) of dcnv4_gated_linear for grad_h [..., F]; grad_b is None where b is, grad_x with need_x=False (a first layer)."""
+    P, K, F, act = _gated_args(x, w, b, activation)
+    shape, dt = x.shape, x.dtype
+    _check_like(x, (("grad_h", grad_h, (*shape[:-1], F)),))
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt), None if b is None else ("grad_b", (2, F), dt)), stream)
+    code = _dtype_code(x)
+    space, size = _workspace(x, workspace, dcnv4_gated_linear_workspace_bytes(P, K, F, code, True) if workspace is None else 0, stream)
+    args = (x.data_ptr(), w.data_ptr(), _ptr(b), grad_h.data_ptr(), _ptr(gx), gw.data_ptr(), _ptr(gb), space.data_ptr(), size, P, K, F, act, code,
+            _stream_ptr(stream, x.device))
+    if prepare_only:
+        return _prepared(args, out, workspace)
+    _call(x.device, "dcnv4_gated_linear_backward", args)
+    return gx, gw, gb
 
 
 class AdamwPlan:

@@ -1,0 +1,814 @@
+// Layers of a network's blocks and their gradients (dcnv4_gated_linear, its backward pass and that of dcnv4_linear, of include/dcnv4.h).
+//
+// The gated layer: a = x Wg^T + bg, u = x Wu^T + bu, h = act(a) * u, in one kernel: a workgroup makes a tile of pairs (a, u) x pixels on the matrix cores,
+// where a lane has both numbers of a pair, and stores h alone.  Backward: the tile again, out of it and grad_h
+//     da = grad_h * u * act'(a),   du = grad_h * act(a)
+// stored in 16 bits as d [P][2F], and the two products
+//     grad_x[p] = sum_j d[p][j] * w[j],    grad_w[j] = sum_p d[p][j] * x[p]
+// whose operands lie as they are and are turned on the way from LDS to registers where the product wants them turned.  grad_b's sums are of d before it
+// is rounded.  a and u are not kept from the forward pass: they would be 2F numbers a row, twice what h takes, written and read; making them again costs
+// a third of the whole step's products.
+//
+// fp16: d is rounded to fp16 once, for both products, times a power of two that puts the largest |grad_h| into [2, 4): u * act'(a) and act(a) may be as
+// large as 16000 before d is infinite, and d of down to 2^-16 of the largest grad_h keeps all bits.  fp32: operands as three bf16 numbers, six products.
+#include <math.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "dcnv4_product.h"
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// act(a) and its derivative.  EXACT (fp32): by the library's functions.  Else, for results of 11 bits: the hardware's exp2 and reciprocal, and
+// the normal distribution function of -|a| as exp(-a^2 / 2) * t * p(t), t = 1 / (1 + 0.43 |a| / sqrt 2), p of degree 7: erfc(z) exp(z^2) is
+// smooth in such a t; the coefficients are a minimax fit of it, 1.8e-7 relative, made for this for z up to 12.
+struct Act {
+    float value, slope;
+};
+template <int ACT, bool EXACT> __device__ __forceinline__ Act activation(float a)
+{
+    if constexpr (ACT == DCNV4_SILU) {
+        const float s = EXACT ? 1.f / (1.f + expf(-a)) : __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -kLog2e));
+        const float v = a * s;
+        return {v, __builtin_fmaf(v, 1.f - s, s)};
+    } else {
+        const float square = a * a;
+        float lower, bell;                                 // the distribution function at -|a|, exp(-a^2 / 2)
+        if constexpr (EXACT) {
+            bell = expf(-.5f * square);
+            lower = .5f * erfcf(fabsf(a) * .70710678118654752440f);
+        } else {
+            bell = __builtin_amdgcn_exp2f(square * (-.5f * kLog2e));
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(a), .43f * .70710678118654752440f, 1.f));
+            float p = .0709221512f;
+            p = __builtin_fmaf(p, t, -.299080256f);
+            p = __builtin_fmaf(p, t, .364815278f);
+            p = __builtin_fmaf(p, t, -.0688891833f);
+            p = __builtin_fmaf(p, t, .238243611f);
+            p = __builtin_fmaf(p, t, .207459638f);
+            p = __builtin_fmaf(p, t, .243989955f);
+            p = __builtin_fmaf(p, t, .242538629f);
+            lower = .5f * t * p * bell;
+        }
+        const float phi = a < 0.f ? lower : 1.f - lower;
+        return {a * phi, __builtin_fmaf(a * .39894228040143267794f, bell, phi)};
+    }
+}
+
+struct Pairs {
+    const void *bias;                                      // [2][F] of the layer's type, or null
+    int F, P;
+};
+
+// Pair of a wave's acc[m][n][4 * a + c] (a < 2), from its first.
+__device__ __forceinline__ int pair_of(int m, int a, int kb) { return 16 * m + 8 * a + 4 * kb; }
+
+template <typename T, int WM, int WN>
+__device__ __forceinline__ void start_with_bias(const Pairs &l, int first, int kb, f32x16 (&acc)[WM][WN])
+{
+    typedef T four __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            four b = {};
+            if (l.bias != nullptr)                         // (F is a multiple of eight: four are inside or outside)
+                b = *reinterpret_cast<const four *>((const T *)l.bias + min(first + pair_of(m, a & 1, kb), l.F - 4) + (a < 2 ? 0 : l.F));
+#pragma unroll
+            for (int n = 0; n < WN; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[m][n][4 * a + e] = (float)b[e];
+        }
+}
+
+}  // namespace
+
+// h of a tile.
+template <typename T, int PL, int ACT, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_gated_kernel(Product q, Pairs l, T *h)
+{
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, false, false, true> G;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
+        return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
+    const int first = at * (G::BM / 2) + wr * 16 * WM, px0 = bt * G::BN + wc * 32 * WN;
+    f32x16 acc[WM][WN];
+    start_with_bias<T, WM, WN>(l, first, kb, acc);
+    G::multiply(smem, q.a, q.b, at * (G::BM / 2), bt * G::BN, 0, q.steps, acc);
+    // 32 pixels at a time, each a run of 16 * WM numbers
+    char *out = smem + wave * (G::OUT / G::kWaves);
+    constexpr int ES = (int)sizeof(T), ROW = 16 * WM * ES + 16, UNITS = 16 * WM * ES / 16;
+#pragma unroll
+    for (int n = 0; n < WN; ++n) {
+#pragma unroll
+        for (int m = 0; m < WM; ++m)
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                T t[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    t[c] = (T)(activation<ACT, PL == 3>(acc[m][n][4 * a + c]).value * acc[m][n][4 * (a + 2) + c]);
+                __builtin_memcpy(out + row * ROW + pair_of(m, a, kb) * ES, t, sizeof(t));
+            }
+        // (the same wave wrote and reads)
+#pragma unroll
+        for (int it = 0; it < (UNITS + 1) / 2; ++it) {
+            const int e = it * 64 + lane, u = e % UNITS, r = e / UNITS, px = px0 + n * 32 + r, f = first + u * (16 / ES);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(out + r * ROW + u * 16);
+            if (px < l.P && f < l.F)
+                *reinterpret_cast<u32x4 *>(h + (long long)px * l.F + f) = v;
+        }
+    }
+}
+
+namespace {
+
+// What a product's result is multiplied with in the end, where its operand was scaled.
+struct Scale {
+    float by;
+};
+
+struct Deltas {
+    const void *grad_h;
+    unsigned short *d;                                     // [P][PL planes][2F]
+    float *bias_sums;                                      // [pixel runs of 32 * WN][2F], or null
+    const float *most;                                     // fp16: largest |grad_h| of `parts` parts
+    int parts;
+    Scale *scale;                                          // fp16: what undoes d's factor
+};
+
+struct Result {
+    void *out;                                             // [b rows][a rows] of T; or float planes, one per split
+    long long plane;                                       // floats
+    const Scale *scale;                                    // or null
+};
+
+}  // namespace
+
+// The largest finite |grad_h| of a workgroup's part of n numbers (a multiple of eight).
+__global__ __launch_bounds__(256) void dcnv4_gated_most_kernel(const unsigned short *g, long long n, float *most)
+{
+    typedef unsigned short us8 __attribute__((ext_vector_type(8)));
+    __shared__ unsigned short part[4];
+    us8 top = {};
+    auto add = [&](us8 v) {
+        v &= (unsigned short)0x7fff;                       // (fp16's bits without the sign are in the numbers' order)
+        top = __builtin_elementwise_max(top, v < (unsigned short)0x7c00 ? v : us8{});
+    };
+    const long long units = n / 8, stride = (long long)gridDim.x * 256;
+    const us8 *p = reinterpret_cast<const us8 *>(g);
+    long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x;
+    for (; i + 3 * stride < units; i += 4 * stride) {
+        const us8 a = p[i], b = p[i + stride], c = p[i + 2 * stride], d = p[i + 3 * stride];
+        add(a);
+        add(b);
+        add(c);
+        add(d);
+    }
+    for (; i < units; i += stride)
+        add(p[i]);
+    int v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v = max(v, (int)top[e]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+        v = max(v, __shfl_xor(v, d));
+    if ((threadIdx.x & 63) == 0)
+        part[threadIdx.x >> 6] = (unsigned short)v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        v = max(max((int)part[0], (int)part[1]), max((int)part[2], (int)part[3]));
+        most[blockIdx.x] = (float)__builtin_bit_cast(_Float16, (unsigned short)v);
+    }
+}
+
+// The tile again, and d out of it.
+template <typename T, int PL, int ACT, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_gated_delta_kernel(Product q, Pairs l, Deltas d)
+{
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, false, false, true> G;
+    typedef T four __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
+    __shared__ float tops[G::kWaves];
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
+        return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
+    const int first = at * (G::BM / 2) + wr * 16 * WM, px0 = bt * G::BN + wc * 32 * WN;
+    float up = 1.f;
+    if constexpr (PL == 1) {
+        float top = 0.f;
+        for (int i = (int)threadIdx.x; i < d.parts; i += G::kThreads)
+            top = fmaxf(top, d.most[i]);
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2)
+            top = fmaxf(top, __shfl_xor(top, s));
+        if (lane == 0)
+            tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < G::kWaves; ++w)
+            top = fmaxf(top, tops[w]);
+        const int e = top > 0.f ? 2 - __builtin_amdgcn_frexp_expf(top) : 0;
+        up = ldexpf(1.f, e);
+        if (at == 0 && bt == 0 && threadIdx.x == 0)
+            d.scale->by = ldexpf(1.f, -e);
+    }
+    f32x16 acc[WM][WN];
+    start_with_bias<T, WM, WN>(l, first, kb, acc);
+    G::multiply(smem, q.a, q.b, at * (G::BM / 2), bt * G::BN, 0, q.steps, acc);
+#pragma unroll
+    for (int n = 0; n < WN; ++n) {
+        const int px = px0 + n * 32 + row;
+        four g[WM][2];
+#pragma unroll
+        for (int m = 0; m < WM; ++m)
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const int f = first + pair_of(m, a, kb);
+                g[m][a] = four{};
+                if (px < l.P && f < l.F)
+                    g[m][a] = *reinterpret_cast<const four *>((const T *)d.grad_h + (long long)px * l.F + f);
+            }
+#pragma unroll
+        for (int m = 0; m < WM; ++m)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const Act v = activation<ACT, PL == 3>(acc[m][n][4 * a + c]);
+                    const float gh = (float)g[m][a][c];
+                    acc[m][n][4 * a + c] = gh * acc[m][n][4 * (a + 2) + c] * v.slope;
+                    acc[m][n][4 * (a + 2) + c] = gh * v.value;
+                }
+    }
+    if (d.bias_sums != nullptr) {
+        // over the pixels of a lane, then of 32 lanes; lane i of them stores number i
+#pragma unroll
+        for (int m = 0; m < WM; ++m) {
+            float mine = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float s = 0.f;
+#pragma unroll
+                for (int n = 0; n < WN; ++n)
+                    s += acc[m][n][r];
+                s = sum_of_32(s);
+                mine = (row & 15) == r ? s : mine;
+            }
+            const int r = row & 15, f = first + pair_of(m, r >> 2 & 1, kb) + (r & 3);
+            if (row < 16 && f < l.F)
+                d.bias_sums[((long long)(bt * WC + wc) * 2 + (r >> 3)) * l.F + f] = mine;
+        }
+    }
+    // results in 16 bits, PL planes one after the other: 32 pixels at a time, each 16 * WM numbers of da and as many of du
+    char *out = smem + wave * (G::OUT / G::kWaves);
+    constexpr int HALF = 16 * WM * 2, ROW = 2 * HALF + 16, UNITS = 2 * HALF / 16;
+#pragma unroll
+    for (int n = 0; n < WN; ++n) {
+#pragma unroll
+        for (int p = 0; p < PL; ++p) {
+#pragma unroll
+            for (int m = 0; m < WM; ++m)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    unsigned short s[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float v = acc[m][n][4 * a + c];
+                        if constexpr (PL == 1) {
+                            s[c] = __builtin_bit_cast(unsigned short, (_Float16)(v * up));
+                        } else {
+                            const __bf16 b = (__bf16)v;
+                            acc[m][n][4 * a + c] = v - (float)b;
+                            s[c] = __builtin_bit_cast(unsigned short, b);
+                        }
+                    }
+                    *reinterpret_cast<u32x2 *>(out + row * ROW + (a < 2 ? 0 : HALF) + pair_of(m, a & 1, kb) * 2) =
+                        u32x2{(unsigned)s[0] | (unsigned)s[1] << 16, (unsigned)s[2] | (unsigned)s[3] << 16};
+                }
+            // (the same wave wrote and reads)
+#pragma unroll
+            for (int it = 0; it < UNITS / 2; ++it) {
+                const int e = it * 64 + lane, u = e % UNITS, r = e / UNITS, px = px0 + n * 32 + r;
+                const int half = u >= UNITS / 2 ? 1 : 0, f = first + (u - half * (UNITS / 2)) * 8;
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(out + r * ROW + u * 16);
+                if (px < l.P && f < l.F)
+                    *reinterpret_cast<u32x4 *>(d.d + (((long long)px * PL + p) * 2 + half) * l.F + f) = v;
+            }
+        }
+    }
+}
+
+// out[j][i] = scale * sum_r A[i][r] * B[j][r], whole (T) or a split of the sum (float planes).  A turned; B turned in the product over pixels (grad_w).
+template <typename T, bool WHOLE, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_layer_product_kernel(Product q, Result o)
+{
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
+    typedef std::conditional_t<WHOLE, T, float> S;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
+    int at, bt, split;
+    if (!tile_of(q, at, bt, split))
+        return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
+    f32x16 acc[WM][WN];
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+        for (int n = 0; n < WN; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[m][n][r] = 0.f;
+    const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
+    G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+    const float by = WHOLE && o.scale != nullptr ? o.scale->by : 1.f;
+    char *out = smem + wave * (G::OUT / G::kWaves);
+    const int i0 = at * G::BM + wr * 32 * WM, j0 = bt * G::BN + wc * 32 * WN;
+    constexpr int ES = (int)sizeof(S), ROW = 32 * WM * ES + 16, UNITS = 32 * WM * ES / 16;
+    S *to = (S *)o.out + (WHOLE ? 0 : (long long)split * o.plane);
+#pragma unroll
+    for (int n = 0; n < WN; ++n) {
+#pragma unroll
+        for (int m = 0; m < WM; ++m)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                S s[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    s[c] = (S)(acc[m][n][4 * a + c] * by);
+                __builtin_memcpy(out + row * ROW + (32 * m + 8 * a + 4 * kb) * ES, s, sizeof(s));
+            }
+#pragma unroll
+        for (int it = 0; it < UNITS / 2; ++it) {
+            const int e = it * 64 + lane, u = e % UNITS, r = e / UNITS, j = j0 + n * 32 + r, i = i0 + u * (16 / ES);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(out + r * ROW + u * 16);
+            if (j < q.b.count && i < q.a.count)
+                *reinterpret_cast<u32x4 *>(to + (long long)j * q.a.count + i) = v;
+        }
+    }
+}
+
+// Adds up the splits' planes [splits][n] and rounds: four numbers a lane.  The first workgroups make grad_b, where that saves it a launch.
+template <typename T>
+__global__ __launch_bounds__(256) void dcnv4_layer_sum_kernel(const float *planes, int splits, long long n, Result o, Bias b)
+{
+    if ((int)blockIdx.x < b.blocks) {
+        bias_of<T>(b, (int)blockIdx.x);
+        return;
+    }
+    const int block = (int)blockIdx.x - b.blocks, blocks = (int)gridDim.x - b.blocks;
+    const float by = o.scale != nullptr ? o.scale->by : 1.f;
+    for (long long i = (long long)block * 256 + (int)threadIdx.x; i < n / 4; i += (long long)blocks * 256) {
+        f32x4 v = *reinterpret_cast<const f32x4 *>(planes + i * 4);
+#pragma unroll 8
+        for (int s = 1; s < splits; ++s)
+            v += *reinterpret_cast<const f32x4 *>(planes + s * n + i * 4);
+        T t[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            t[e] = (T)(v[e] * by);
+        __builtin_memcpy(__builtin_assume_aligned((T *)o.out + i * 4, 4 * sizeof(T)), t, sizeof(t));
+    }
+}
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_bias_kernel(Bias b) { bias_of<T>(b, (int)blockIdx.x); }
+
+// fp32 rows as the products take them: in [rows][cols] -> out [rows][3 planes][pad] of bf16, zeros behind the columns.  Eight numbers a lane.
+__global__ __launch_bounds__(256) void dcnv4_layer_split_kernel(const float *in, long long rows, int cols, int pad, unsigned short *out)
+{
+    const int units = pad / 8;
+    const long long all = rows * units;
+    for (long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const long long row = i / units;
+        const int u = (int)(i - row * units);
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (u * 8 < cols)                                  // (columns come in eights)
+            __builtin_memcpy(v, __builtin_assume_aligned(in + row * cols + u * 8, 16), sizeof(v));
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            unsigned short s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const __bf16 b = (__bf16)v[e];
+                v[e] -= (float)b;
+                s[e] = __builtin_bit_cast(unsigned short, b);
+            }
+            __builtin_memcpy(__builtin_assume_aligned(out + (row * 3 + p) * pad + u * 8, 16), s, sizeof(s));
+        }
+    }
+}
+
+// Sums over runs of rows of g [P][N] (N a multiple of eight): out [runs][N].  Eight columns a lane; `lanes` of them side by side, 256 / lanes rows.
+template <typename T>
+__global__ __launch_bounds__(256) void dcnv4_layer_columns_kernel(const T *g, int P, int N, int lanes_log, int rows, float *out)
+{
+    typedef T eight __attribute__((ext_vector_type(8)));
+    __shared__ float part[256][9];
+    const int lanes = 1 << lanes_log, side = 256 >> lanes_log, l = (int)threadIdx.x & (lanes - 1), s = (int)threadIdx.x >> lanes_log;
+    const int c = ((int)blockIdx.x * lanes + l) * 8, r0 = (int)blockIdx.y * rows, r1 = min(r0 + rows, P);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < N)
+#pragma unroll 4
+        for (int r = r0 + s; r < r1; r += side) {
+            const eight t = *reinterpret_cast<const eight *>(g + (long long)r * N + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] += (float)t[e];
+        }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        part[threadIdx.x][e] = v[e];
+    __syncthreads();
+    // eight lanes' numbers side by side: a lane a column, over the rows in order
+    for (int i = (int)threadIdx.x; i < lanes * 8; i += 256) {
+        float sum = 0.f;
+        for (int k = 0; k < side; ++k)
+            sum += part[k * lanes + (i >> 3)][i & 7];
+        const int col = (int)blockIdx.x * lanes * 8 + i;
+        if (col < N)
+            out[(long long)blockIdx.y * N + col] = sum;
+    }
+}
+
+namespace {
+
+struct LayerOptions {
+    int tile = 0, splits = 0;          // as loss_tile and loss_splits
+} g_layers;
+
+// One more limit than the products': byte offsets inside a gated layer's weights are 32 bits (fp32: of three planes of 16 bits).
+constexpr int kLayerMaxRows = 1 << 24, kLayerMaxWidth = 1 << 20;
+
+bool fits(int pl, const Choice &c, long long m, long long n)
+{
+    const Shape &s = shape_of(pl, c.shape);
+    return c.shape >= 0 && ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn) * c.splits < (1 << 22);     // (a grid has fewer than 2^32 lanes)
+}
+
+struct LayerPlan {
+    int pl, es, P, K, N, kp, np;       // N: results of the layer (gated: 2F); padded in split operands
+    Choice forward, gx, gw;
+    int most_parts, columns_runs, columns_rows;
+    // bytes from the start of the workspace
+    long long x_split, w_split, g_split, d, scale, most, bias_sums, gx_at, gw_at, bytes;
+};
+
+int check_layer(long long P, int K, int N, int dtype)
+{
+    if (P < 1 || K < 1 || N < 1)
+        return DCNV4_ERR_SHAPE;
+    if ((dtype != DCNV4_F32 && dtype != DCNV4_F16) || K % 8 || N % 8 || P > kLayerMaxRows || K > kLayerMaxWidth ||
+        N > kLayerMaxWidth)
+        return DCNV4_ERR_UNSUPPORTED;
+    return DCNV4_OK;
+}
+
+struct Room {
+    long long at = 0;
+    long long take(long long bytes)
+    {
+        const long long here = at;
+        at += (long long)align256((size_t)bytes);
+        return here;
+    }
+};
+
+// The two products of a gradient, and room for their planes: [P][K] over N numbers, [N][K] over P.
+bool plan_gradients(LayerPlan &p, Room &room)
+{
+    p.gx = choose_product(p.pl, p.K, p.P, p.np, true, g_layers.tile, g_layers.splits);
+    p.gw = choose_product(p.pl, p.K, p.N, p.P, true, g_layers.tile, g_layers.splits);
+    if (!fits(p.pl, p.gx, p.K, p.P) || !fits(p.pl, p.gw, p.K, p.N))
+        return false;
+    if (p.gx.splits > 1)
+        p.gx_at = room.take((long long)p.gx.splits * p.P * p.K * 4);
+    if (p.gw.splits > 1)
+        p.gw_at = room.take((long long)p.gw.splits * p.N * p.K * 4);
+    return true;
+}
+
+int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backward)
+{
+    if (F < 1)
+        return DCNV4_ERR_SHAPE;
+    if (F > kLayerMaxWidth / 2)
+        return DCNV4_ERR_UNSUPPORTED;
+    if (const int rc = check_layer(P, K, F, dtype))
+        return rc;
+    LayerPlan p = {};
+    p.es = esize(dtype);
+    p.pl = dtype == DCNV4_F16 ? 1 : 3;
+    p.P = (int)P;
+    p.K = K;
+    p.N = p.np = 2 * F;
+    p.kp = p.pl == 1 ? K : (int)round_up(K, 32);
+    if ((long long)p.N * p.pl * p.kp * 2 >= 0x7fffffffLL)
+        return DCNV4_ERR_UNSUPPORTED;
+    p.forward = choose_product(p.pl, p.N, P, p.kp, false, g_layers.tile, 0);
+    if (!fits(p.pl, p.forward, p.N, P))
+        return DCNV4_ERR_UNSUPPORTED;
+    Room room;
+    if (p.pl == 3) {
+        p.x_split = room.take(P * 6 * p.kp);
+        p.w_split = room.take((long long)p.N * 6 * p.kp);
+    }
+    if (backward) {
+        p.most_parts = (int)(P * F / 8 / 1024 < 512 ? P * F / 8 / 1024 + 1 : 512);
+        p.scale = room.take(sizeof(Scale));
+        p.most = room.take(p.most_parts * 4);
+        p.d = room.take(P * p.pl * p.N * 2);
+        p.bias_sums = room.take(round_up(P, 256) / 32 * p.N * 4);
+        if (!plan_gradients(p, room))
+            return DCNV4_ERR_UNSUPPORTED;
+    }
+    p.bytes = room.at;
+    *out = p;
+    return DCNV4_OK;
+}
+
+int plan_linear_backward(LayerPlan *out, long long P, int K, int N, int dtype)
+{
+    if (const int rc = check_layer(P, K, N, dtype))
+        return rc;
+    LayerPlan p = {};
+    p.es = esize(dtype);
+    p.pl = dtype == DCNV4_F16 ? 1 : 3;
+    p.P = (int)P;
+    p.K = K;
+    p.N = N;
+    p.kp = p.pl == 1 ? K : (int)round_up(K, 32);
+    p.np = N;
+    Room room;
+    if (p.pl == 3) {
+        p.x_split = room.take(P * 6 * p.kp);
+        p.w_split = room.take((long long)N * 6 * p.kp);
+        p.g_split = room.take(P * 6 * p.np);
+    }
+    // runs of rows: two workgroups to a unit, 32 rows at least
+    const long long across = (N / 8 + 63) / 64;
+    long long runs = across < 512 ? 512 / across : 1;
+    p.columns_rows = (int)round_up((P + runs - 1) / runs, 32);
+    p.columns_runs = (int)((P + p.columns_rows - 1) / p.columns_rows);
+    p.bias_sums = room.take((long long)p.columns_runs * N * 4);
+    if (!plan_gradients(p, room))
+        return DCNV4_ERR_UNSUPPORTED;
+    p.bytes = room.at;
+    *out = p;
+    return DCNV4_OK;
+}
+
+void split_rows(const void *in, long long rows, int cols, int pad, void *out, hipStream_t s)
+{
+    const long long groups = (rows * (pad / 8) + 255) / 256;
+    hipLaunchKernelGGL(dcnv4_layer_split_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, (const float *)in, rows, cols, pad,
+                       (unsigned short *)out);
+}
+
+template <typename T, int PL, bool PIXELS> void launch_product(const Product &q, const Choice &c, const Result &o, hipStream_t s)
+{
+    with_tile<PL>(c.shape, [&](auto t) {
+        typedef decltype(t) G;
+        const dim3 grid((unsigned)(q.per_xcd * kXcds)), block(G::WR * G::WC * 64);
+        if (c.splits > 1)
+            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, false, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
+        else
+            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, true, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
+        return 0;
+    });
+}
+
+template <typename T> void sum_planes(const void *planes, int splits, long long n, const Result &o, const Bias &b, hipStream_t s)
+{
+    const long long groups = (n / 4 + 255) / 256;
+    hipLaunchKernelGGL((dcnv4_layer_sum_kernel<T>), dim3((unsigned)((groups < 8192 ? groups : 8192) + b.blocks)), dim3(256), 0, s, (const float *)planes,
+                       splits, n, o, b);
+}
+
+// grad_x, grad_w and, out of the runs' sums, grad_b (each may be null) of a layer with rows w [N][K], x [P][K], d [P][N] as operands.
+template <typename T, int PL>
+void gradients(const LayerPlan &p, const Operand &x, const Operand &w, const Operand &d, const Scale *scale, Bias b, void *grad_x, void *grad_w, char *ws,
+               hipStream_t s)
+{
+    if (grad_x) {
+        const Result o = {grad_x, 0, scale};
+        const Product q = product_of(turned(w), d, PL, p.gx);
+        const Result planes = {ws + p.gx_at, (long long)p.P * p.K, nullptr};
+        launch_product<T, PL, false>(q, p.gx, p.gx.splits > 1 ? planes : o, s);
+        if (p.gx.splits > 1)
+            sum_planes<T>(ws + p.gx_at, p.gx.splits, planes.plane, o, Bias{}, s);
+    }
+    if (grad_w) {
+        const Result o = {grad_w, 0, scale};
+        const Product q = product_of(turned(x), turned(d), PL, p.gw);
+        const Result planes = {ws + p.gw_at, (long long)p.N * p.K, nullptr};
+        launch_product<T, PL, true>(q, p.gw, p.gw.splits > 1 ? planes : o, s);
+        if (p.gw.splits > 1) {
+            sum_planes<T>(ws + p.gw_at, p.gw.splits, planes.plane, o, b, s);
+            b.blocks = 0;
+        }
+    }
+    if (b.blocks > 0)
+        hipLaunchKernelGGL((dcnv4_layer_bias_kernel<T>), dim3((unsigned)b.blocks), dim3(256), 0, s, b);
+}
+
+template <typename F> void by_activation(int act, F &&f)
+{
+    if (act == DCNV4_SILU)
+        f(std::integral_constant<int, DCNV4_SILU>());
+    else
+        f(std::integral_constant<int, DCNV4_GELU>());
+}
+
+// x and w as the products take them
+template <int PL> void operands(const LayerPlan &p, const void *x, const void *w, char *ws, bool with_x, bool with_w, Operand *xo, Operand *wo, hipStream_t s)
+{
+    if (PL == 3) {
+        if (with_x)
+            split_rows(x, p.P, p.K, p.kp, ws + p.x_split, s);
+        if (with_w)
+            split_rows(w, p.N, p.K, p.kp, ws + p.w_split, s);
+    }
+    *xo = rows_of(PL == 3 ? (const void *)(ws + p.x_split) : x, p.P, p.kp, PL, p.kp);
+    *wo = rows_of(PL == 3 ? (const void *)(ws + p.w_split) : w, p.N, p.kp, PL, p.kp);
+}
+
+// The operand's rows of K numbers (its planes are kp apart).
+Operand narrowed(Operand o, int K)
+{
+    o.length = K;
+    return o;
+}
+
+template <typename T, int PL>
+int gated_forward(const LayerPlan &p, const void *x, const void *w, const Pairs &l, int act, void *h, char *ws, hipStream_t s)
+{
+    Operand xo, wo;
+    operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
+    wo.count = l.F;
+    const Product q = product_of(wo, xo, PL, p.forward, true);
+    by_activation(act, [&](auto A) {
+        with_tile<PL>(p.forward.shape, [&](auto t) {
+            typedef decltype(t) G;
+            hipLaunchKernelGGL((dcnv4_gated_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
+                               dim3(G::WR * G::WC * 64), 0, s, q, l, (T *)h);
+            return 0;
+        });
+    });
+    return launched();
+}
+
+template <typename T, int PL>
+int gated_backward(const LayerPlan &p, const void *x, const void *w, const Pairs &l, int act, const void *grad_h, void *grad_x, void *grad_w, void *grad_b,
+                   char *ws, hipStream_t s)
+{
+    if (PL == 1)
+        hipLaunchKernelGGL(dcnv4_gated_most_kernel, dim3((unsigned)p.most_parts), dim3(256), 0, s, (const unsigned short *)grad_h, (long long)p.P * l.F,
+                           (float *)(ws + p.most));
+    Operand xo, wo;
+    operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
+    Operand pairs = wo;
+    pairs.count = l.F;
+    const Product q = product_of(pairs, xo, PL, p.forward, true);
+    Scale *scale = PL == 1 ? (Scale *)(ws + p.scale) : nullptr;
+    const Deltas d = {grad_h, (unsigned short *)(ws + p.d), grad_b ? (float *)(ws + p.bias_sums) : nullptr, (const float *)(ws + p.most), p.most_parts, scale};
+    int runs = 0;
+    by_activation(act, [&](auto A) {
+        with_tile<PL>(p.forward.shape, [&](auto t) {
+            typedef decltype(t) G;
+            runs = q.b_tiles * G::WC;
+            hipLaunchKernelGGL((dcnv4_gated_delta_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
+                               dim3(G::WR * G::WC * 64), 0, s, q, l, d);
+            return 0;
+        });
+    });
+    Bias b = {};
+    if (grad_b)
+        b = {d.bias_sums, runs, p.N, (p.N + 15) / 16, grad_b};
+    gradients<T, PL>(p, narrowed(xo, p.K), narrowed(wo, p.K), rows_of(d.d, p.P, p.N, PL, p.N), scale, b, grad_x, grad_w, ws, s);
+    return launched();
+}
+
+template <typename T, int PL>
+int linear_backward(const LayerPlan &p, const void *x, const void *w, const void *grad_y, void *grad_x, void *grad_w, void *grad_b, char *ws, hipStream_t s)
+{
+    Operand xo, wo;
+    operands<PL>(p, x, w, ws, grad_w != nullptr, grad_x != nullptr, &xo, &wo, s);
+    if (PL == 3 && (grad_x || grad_w))
+        split_rows(grad_y, p.P, p.N, p.np, ws + p.g_split, s);
+    Bias b = {};
+    if (grad_b) {
+        b = {(const float *)(ws + p.bias_sums), p.columns_runs, p.N, (p.N + 15) / 16, grad_b};
+        int log = 0;
+        while (log < 6 && (8 << log) < p.N)
+            ++log;
+        hipLaunchKernelGGL((dcnv4_layer_columns_kernel<T>), dim3((unsigned)((p.N / 8 + (1 << log) - 1) >> log), (unsigned)p.columns_runs), dim3(256), 0, s,
+                           (const T *)grad_y, p.P, p.N, log, p.columns_rows, (float *)(ws + p.bias_sums));
+    }
+    gradients<T, PL>(p, narrowed(xo, p.K), narrowed(wo, p.K), rows_of(PL == 3 ? (const void *)(ws + p.g_split) : grad_y, p.P, p.N, PL, p.np), nullptr, b, grad_x,
+                     grad_w, ws, s);
+    return launched();
+}
+
+bool off16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+}  // namespace
+
+int layers_set_option(const char *key, int value)
+{
+    if (!strcmp(key, "reset"))
+        g_layers = LayerOptions();
+    else if (!strcmp(key, "layer_tile") && value >= 0 && value <= 3)
+        g_layers.tile = value;
+    else if (!strcmp(key, "layer_splits") && value >= 0 && value <= 64)
+        g_layers.splits = value;
+    else
+        return DCNV4_ERR_UNSUPPORTED;
+    return DCNV4_OK;
+}
+
+extern "C" {
+
+long long dcnv4_gated_linear_workspace_bytes(long long P, int K, int F, int dtype, int backward)
+{
+    LayerPlan p;
+    return plan_gated(&p, P, K, F, dtype, backward != 0) == DCNV4_OK ? p.bytes : -1;
+}
+
+int dcnv4_gated_linear(const void *x, const void *w, const void *b, void *h, void *workspace, long long workspace_bytes, long long P, int K, int F,
+                       int activation, int dtype, void *stream)
+{
+    if (!x || !w || !h)
+        return DCNV4_ERR_NULL;
+    LayerPlan p;
+    const int rc = plan_gated(&p, P, K, F, dtype, false);
+    if (rc)
+        return rc;
+    if (activation != DCNV4_SILU && activation != DCNV4_GELU)
+        return DCNV4_ERR_UNSUPPORTED;
+    if (p.bytes > 0 && !workspace)
+        return DCNV4_ERR_NULL;
+    if (p.bytes > 0 && workspace_bytes < p.bytes)
+        return DCNV4_ERR_SHAPE;
+    if (off16(x) || off16(w) || off16(b) || off16(h) || off16(workspace))
+        return DCNV4_ERR_ALIGN;
+    const Pairs l = {b, F, p.P};
+    hipStream_t s = (hipStream_t)stream;
+    return dtype == DCNV4_F16 ? gated_forward<_Float16, 1>(p, x, w, l, activation, h, (char *)workspace, s)
+                              : gated_forward<float, 3>(p, x, w, l, activation, h, (char *)workspace, s);
+}
+
+int dcnv4_gated_linear_backward(const void *x, const void *w, const void *b, const void *grad_h, void *grad_x, void *grad_w, void *grad_b, void *workspace,
+                                long long workspace_bytes, long long P, int K, int F, int activation, int dtype, void *stream)
+{
+    if (!x || !w || !grad_h || (!grad_x && !grad_w && !grad_b) || !workspace)
+        return DCNV4_ERR_NULL;
+    LayerPlan p;
+    const int rc = plan_gated(&p, P, K, F, dtype, true);
+    if (rc)
+        return rc;
+    if (activation != DCNV4_SILU && activation != DCNV4_GELU)
+        return DCNV4_ERR_UNSUPPORTED;
+    if (workspace_bytes < p.bytes)
+        return DCNV4_ERR_SHAPE;
+    if (off16(x) || off16(w) || off16(b) || off16(grad_h) || off16(grad_x) || off16(grad_w) || off16(grad_b) || off16(workspace))
+        return DCNV4_ERR_ALIGN;
+    const Pairs l = {b, F, p.P};
+    hipStream_t s = (hipStream_t)stream;
+    return dtype == DCNV4_F16 ? gated_backward<_Float16, 1>(p, x, w, l, activation, grad_h, grad_x, grad_w, grad_b, (char *)workspace, s)
+                              : gated_backward<float, 3>(p, x, w, l, activation, grad_h, grad_x, grad_w, grad_b, (char *)workspace, s);
+}
+
+long long dcnv4_linear_backward_workspace_bytes(long long P, int K, int Nout, int dtype)
+{
+    LayerPlan p;
+    return plan_linear_backward(&p, P, K, Nout, dtype) == DCNV4_OK ? p.bytes : -1;
+}
+
+int dcnv4_linear_backward(const void *x, const void *w, const void *grad_y, void *grad_x, void *grad_w, void *grad_b, void *workspace,
+                          long long workspace_bytes, long long P, int K, int Nout, int dtype, void *stream)
+{
+    if (!grad_y || (!grad_x && !grad_w && !grad_b) || (grad_x && !w) || (grad_w && !x) || !workspace)
+        return DCNV4_ERR_NULL;
+    LayerPlan p;
+    const int rc = plan_linear_backward(&p, P, K, Nout, dtype);
+    if (rc)
+        return rc;
+    if (workspace_bytes < p.bytes)
+        return DCNV4_ERR_SHAPE;
+    if (off16(x) || off16(w) || off16(grad_y) || off16(grad_x) || off16(grad_w) || off16(grad_b) || off16(workspace))
+        return DCNV4_ERR_ALIGN;
+    hipStream_t s = (hipStream_t)stream;
+    return dtype == DCNV4_F16 ? linear_backward<_Float16, 1>(p, x, w, grad_y, grad_x, grad_w, grad_b, (char *)workspace, s)
+                              : linear_backward<float, 3>(p, x, w, grad_y, grad_x, grad_w, grad_b, (char *)workspace, s);
+}
+
+}  // extern "C"

@@ -139,3 +139,60 @@ def end_backward(x, z, scale, gate, first, second, stats, gy, gz, k=64, rows=256
         gx, dgx, _, _ = norm_backward(xs, m[..., 0], r[..., 0], h, dh, k)
         out["grad_x"] = np.where(on, gx, 0), np.where(on, dgx, 0)
     return out
+
+
+
+
+def activation(a, act):
+    """act(a) and its derivative."""
+    from scipy.special import expit, ndtr
+    if act == "silu":
+        s = expit(a)
+        return a * s, s * (1 + a * expit(-a))
+    return a * ndtr(a), ndtr(a) + a * np.exp(-a * a / 2) / np.sqrt(2 * np.pi)
+
+
+def products_off(terms, size, f16):
+    """How far a sum of products on the matrix units may be off: 16 at a time, one after the other, `size` being the sum of magnitudes; fp32 operands as three
+    bf16 numbers take six passes and leave out 2^-22 of each."""
+    return (terms / 16 + 32) * E24 * size if f16 else (6 * (terms / 16) + 64) * E24 * size + 2.0 ** -22 * size
+
+
+def gated(x, w, b, act, f16):
+    """h, how far fp32 arithmetic may take it, and what the backward pass needs."""
+    x, w = x.astype(np.float64), w.astype(np.float64)
+    b = np.zeros(w.shape[:2]) if b is None else b.astype(np.float64)
+    a, u = x @ w[0].T + b[0], x @ w[1].T + b[1]
+    size = [np.abs(x) @ np.abs(w[i]).T + np.abs(b[i]) for i in (0, 1)]
+    da, du = (products_off(x.shape[-1], s, f16) for s in size)
+    value, slope = activation(a, act)
+    # the functions: fp16's results by exp2 and a reciprocal of an argument that was rounded (a or a^2 / 2 times 2^-24 and a few steps)
+    off = (a * a + np.abs(a) + 16) * E24
+    dv, ds = (np.abs(slope) + da) * da + off * (np.abs(value) + 2.0 ** -30), 1.2 * da + off * (np.abs(slope) + np.abs(a))
+    return value * u, np.abs(u) * dv + np.abs(value) * du + dv * du + 2 * E24 * np.abs(value * u), (a, u, da, du, value, slope, dv, ds)
+
+
+def gated_backward(x, w, gh, parts, f16):
+    """{name: (gradient, how far it may be off before its own rounding)}."""
+    x, w, gh = x.astype(np.float64), w.astype(np.float64), gh.astype(np.float64)
+    a, u, da, du, value, slope, dv, ds = parts
+    d = np.concatenate([gh * u * slope, gh * value], -1)
+    off = np.concatenate([np.abs(gh) * (np.abs(u) * ds + np.abs(slope) * du + du * ds), np.abs(gh) * dv], -1) + 4 * E24 * np.abs(d)
+    top = np.abs(gh).max()
+    rounded = off + (2.0 ** -11 * np.abs(d) + 2.0 ** -25 * top / 2 if f16 else 2.0 ** -23 * np.abs(d))
+    both = w.reshape(-1, w.shape[-1])
+    lead = (-1, d.shape[-1])
+    d2, r2, o2, x2 = d.reshape(lead), rounded.reshape(lead), off.reshape(lead), x.reshape(-1, x.shape[-1])
+    gx = (d2 @ both, r2 @ np.abs(both) + products_off(both.shape[0], np.abs(d2) @ np.abs(both), f16))
+    gw = (d2.T @ x2, r2.T @ np.abs(x2) + products_off(x2.shape[0], np.abs(d2).T @ np.abs(x2), f16))
+    gb = (d2.sum(0), o2.sum(0) + (x2.shape[0] / 32 + 64) * E24 * np.abs(d2).sum(0))
+    return {"grad_x": tuple(v.reshape(x.shape) for v in gx), "grad_w": tuple(v.reshape(w.shape) for v in gw), "grad_b": tuple(v.reshape(w.shape[:2]) for v in gb)}
+
+
+def linear_backward(x, w, gy, f16):
+    x, w, gy = (v.astype(np.float64) for v in (x, w, gy))
+    x2, g2 = x.reshape(-1, x.shape[-1]), gy.reshape(-1, gy.shape[-1])
+    gx = (g2 @ w, products_off(w.shape[0], np.abs(g2) @ np.abs(w), f16))
+    gw = (g2.T @ x2, products_off(x2.shape[0], np.abs(g2).T @ np.abs(x2), f16))
+    return {"grad_x": tuple(v.reshape(x.shape) for v in gx), "grad_w": gw,
+            "grad_b": (g2.sum(0), (x2.shape[0] / 256 + 320) * E24 * np.abs(g2).sum(0))}

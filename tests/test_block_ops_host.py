@@ -131,3 +131,65 @@ def test_gradient_of_the_plain_block_end_against_differences(form):
                 w[at].reshape(-1)[i] += sign * step
                 moved.append(value(w))
             assert abs((moved[0] - moved[1]) / (2 * step) - grad.reshape(-1)[i]) < 1e-6, (name, i)
+
+
+def gated(ptrs=(A,) * 5, size=1 << 40, P=5, K=32, F=16, act=0, dtype=0):
+    return dcn.load_library().dcnv4_gated_linear(*ptrs, size, P, K, F, act, dtype, None)
+
+
+def gated_back(ptrs=(A,) * 8, size=1 << 40, P=5, K=32, F=16, act=0, dtype=0):
+    return dcn.load_library().dcnv4_gated_linear_backward(*ptrs, size, P, K, F, act, dtype, None)
+
+
+def linear_back(ptrs=(A,) * 7, size=1 << 40, P=5, K=32, F=16, act=0, dtype=0):
+    return dcn.load_library().dcnv4_linear_backward(*ptrs, size, P, K, F, dtype, None)
+
+
+def test_layers_validate_on_the_host():
+    for call, count, needed in ((gated, 5, (0, 1, 3, 4)), (gated_back, 8, (0, 1, 3, 7)), (linear_back, 7, (0, 1, 2, 6))):
+        for i in range(count):
+            if i in needed:
+                assert call(without(count, i)) == 1, (call, i)
+            assert call(without(count, i, A + 8)) == 4
+        assert call(P=0) == 2 and call(K=0) == 2 and call(F=0) == 2 and call(F=-8) == 2
+        assert call(K=12) == 3 and call(K=20, dtype=1) == 3 and call(F=12) == 3 and call(dtype=2) == 3
+        assert call(P=(1 << 24) + 1) == 3 and call(K=1 << 21) == 3 and call(F=1 << 21) == 3
+    assert gated(act=2) == 3 and gated_back(act=-1) == 3
+    assert gated(K=1 << 14, F=1 << 15, dtype=1) == 3 and gated(K=1 << 14, F=1 << 14, dtype=0) == 3       # weights past 32-bit offsets
+    none = lambda count, *at: tuple(None if i in at else A for i in range(count))
+    assert gated_back(none(8, 4, 5, 6)) == 1 and linear_back(none(7, 3, 4, 5)) == 1
+    bytes_of = dcn.dcnv4_gated_linear_workspace_bytes
+    assert bytes_of(5, 32, 16, 1, False) == 0 and bytes_of(5, 32, 16, 0, False) > 0 and bytes_of(0, 32, 16, 0, True) == -1
+    for dtype in (0, 1):
+        assert gated_back(size=bytes_of(5, 32, 16, dtype, True) - 1, dtype=dtype) == 2
+        assert linear_back(size=dcn.dcnv4_linear_backward_workspace_bytes(5, 32, 16, dtype) - 1, dtype=dtype) == 2
+    assert gated(size=bytes_of(5, 32, 16, 0, False) - 1) == 2
+    for key, bad in (("layer_tile", 4), ("layer_splits", 65), ("layer_tile", -1)):
+        with pytest.raises(dcn.Dcnv4Error):
+            dcn.dcnv4_set_option(key, bad)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradient_of_the_plain_gated_layer_against_differences(act):
+    rng = np.random.default_rng(2)
+    v = {"x": rng.standard_normal((3, 4)), "w": rng.standard_normal((2, 5, 4)), "b": rng.standard_normal((2, 5))}
+    gh = rng.standard_normal((3, 5))
+    _, _, parts = ref.gated(v["x"], v["w"], v["b"], act, True)
+    step = 1e-6
+    for name, (grad, _) in ref.gated_backward(v["x"], v["w"], gh, parts, True).items():
+        for i in range(grad.size):
+            moved = []
+            for sign in (1, -1):
+                u = {k: a.copy() for k, a in v.items()}
+                u[name[5:]].reshape(-1)[i] += sign * step
+                moved.append((ref.gated(u["x"], u["w"], u["b"], act, True)[0] * gh).sum())
+            assert abs((moved[0] - moved[1]) / (2 * step) - grad.reshape(-1)[i]) < 1e-7, (name, i)
+
+
+def test_layers_refuse_host_tensors():
+    import torch
+    x, w, g = torch.zeros((3, 8)), torch.zeros((2, 8, 8)), torch.zeros((3, 8))
+    for call in (lambda: dcn.dcnv4_gated_linear(x, w), lambda: dcn.dcnv4_gated_linear_backward(x, w, g), lambda: dcn.dcnv4_linear_backward(x, w[0], g),
+                 lambda: dcn.dcnv4_norm_scale_add_norm(x, x), lambda: dcn.dcnv4_norm_scale_add_norm_backward(x, x, None, None, None, None, (None,) * 4, None, x)):
+        with pytest.raises(ValueError, match="x must be a GPU tensor"):
+            call()

@@ -10,7 +10,8 @@ from paper_2401_06197_amd import binding as dcn
 
 READELF = "/opt/rocm/llvm/bin/llvm-readelf"
 pytestmark = pytest.mark.skipif(not os.path.exists(READELF), reason="no llvm-readelf")
-PARTS = ("dcnv4_end_kernel", "dcnv4_end_backward_kernel", "dcnv4_end_join_kernel", "dcnv4_adamw_kernel")
+PARTS = ("dcnv4_end_kernel", "dcnv4_end_backward_kernel", "dcnv4_end_join_kernel", "dcnv4_adamw_kernel", "dcnv4_gated_kernel",
+         "dcnv4_gated_delta_kernel", "dcnv4_gated_most_kernel", "dcnv4_layer_")
 
 
 def kernels(tmp_path):

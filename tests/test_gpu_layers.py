@@ -1,0 +1,246 @@
+"""The gated layer, its gradient and that of the linear layer against plain double-precision forms, through the C ABI.
+
+Tolerances.  A result is rounded once: half a step of its type, in fp16 at least half of the smallest step, 2^-25.  Before that, sums of products on the
+matrix units (block_ref.products_off), functions of their results, and, in the gated layer's gradient in fp16, d rounded to half a step, which the sums carry on
+(block_ref.gated_backward).  These bounds add magnitudes; that roundings do not all point one way is held beside them: as 2-norms a gradient's error is at
+most that of two roundings of half a step each (uniform ones: 0.58 of that each), and 16 steps of fp32."""
+import numpy as np
+import pytest
+import torch
+
+import block_ref as ref
+from paper_2401_06197_amd import binding as dcn
+
+pytestmark = pytest.mark.gpu
+
+NP = {"f32": np.float32, "f16": np.float16}
+U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11}
+LEAST = {"f32": 0.0, "f16": 2.0 ** -25}
+
+
+def gpu(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def close(name, got, want, slack, dtype):
+    got = got.cpu().numpy().astype(np.float64)
+    assert got.shape == want.shape, (name, got.shape, want.shape)
+    lim = (1 + U[dtype]) * slack + U[dtype] * np.abs(want) + LEAST[dtype]
+    # (65504 is fp16's largest number, and 65504 + 16 the first that rounds to infinity)
+    over = (dtype == "f16") & (np.abs(want) + slack >= 65520) & (got == np.copysign(np.inf, want))
+    got, want = np.where(over, 0, got), np.where(over, 0, want)
+    bad = ~(np.abs(got - want) <= lim)
+    if bad.any():
+        at = np.unravel_index(np.argmax(np.where(bad, np.abs(got - want) / np.maximum(lim, 1e-300), 0)), bad.shape)
+        raise AssertionError(f"{name}: {int(bad.sum())} of {bad.size} off; at {at} got {got[at]!r}, want {want[at]!r}, limit {lim[at]!r}")
+    if want.size > 64 and np.abs(want).max() > 2.0 ** -10:
+        off = np.linalg.norm(got - want) / np.linalg.norm(want)
+        assert off <= (2 * U[dtype] if dtype == "f16" else 16 * 2.0 ** -23), (name, off)
+
+
+def draw(lead, K, F, dtype, seed, bias=True, size=0.05):
+    rng = np.random.default_rng(seed)
+    r = lambda *s: rng.standard_normal(s)
+    lead = lead if isinstance(lead, tuple) else (lead,)
+    t = {"x": r(*lead, K), "w": r(2, F, K) / np.sqrt(K), "b": 0.3 * r(2, F) if bias else None, "gh": size * r(*lead, F)}
+    return {k: None if v is None else v.astype(NP[dtype]) for k, v in t.items()}
+
+
+def check(t, dtype, act):
+    x, w, b, gh = (gpu(t[k]) for k in ("x", "w", "b", "gh"))
+    h = dcn.dcnv4_gated_linear(x, w, b, activation=act)
+    want, slack, parts = ref.gated(t["x"], t["w"], t["b"], act, dtype == "f16")
+    close("h", h, want, slack, dtype)
+    back = dict(zip(("grad_x", "grad_w", "grad_b"), dcn.dcnv4_gated_linear_backward(x, w, gh, b, activation=act)))
+    for name, (want, slack) in ref.gated_backward(t["x"], t["w"], t["gh"], parts, dtype == "f16").items():
+        if name == "grad_b" and b is None:
+            assert back[name] is None
+        else:
+            close(name, back[name], want, slack, dtype)
+
+
+# one row and few, odd numbers of rows, widths that end inside every tile
+SIZES = {"f16": [(1, 16, 8), (3, 32, 8), (2, 48, 264), (65, 48, 72), (257, 80, 136), (300, 16, 1000), (1000, 160, 264), (513, 272, 40), (49, 1024, 328), (130, 528, 520), (90, 24, 32), (140, 136, 72)],
+         "f32": [(1, 8, 8), (3, 24, 16), (65, 40, 72), (257, 88, 136), (300, 16, 520), (700, 160, 264), (49, 512, 200)]}
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("tile", [0, 1, 2, 3])
+@pytest.mark.parametrize("dtype,size", [(d, s) for d in SIZES for s in SIZES[d]])
+def test_gated_layer(dtype, size, tile, act):
+    dcn.dcnv4_set_option("layer_tile", tile)
+    check(draw(*size, dtype, sum(size)), dtype, act)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("splits", [2, 3, 64])
+def test_sums_in_parts(dtype, splits):
+    dcn.dcnv4_set_option("layer_splits", splits)
+    check(draw(700, 48, 136, dtype, 2), dtype, "silu")
+    check(draw(700, 48, 136, dtype, 2, bias=False), dtype, "gelu")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_many_axes_and_no_bias(dtype):
+    check(draw((2, 3, 7), 32, 40, dtype, 3, bias=False), dtype, "silu")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_steep_and_flat_parts_of_the_activation(dtype, act):
+    """a from -60 to 60."""
+    t = draw(400, 32, 64, dtype, 4)
+    t["x"][:, 0] = np.linspace(-60, 60, 400)
+    t["w"][0, :, 0] = 1
+    check(t, dtype, act)
+
+
+@pytest.mark.parametrize("size", [1e-6, 6e-8, 1.0, 2e4])
+def test_sizes_of_gradients_in_fp16(size):
+    """d takes a power of two of its own: gradients of the least numbers of fp16 keep their bits in grad_w, large ones do not overflow."""
+    t = draw(300, 48, 72, "f16", 5, size=size)
+    t["gh"] = np.clip(t["gh"].astype(np.float64), -60000, 60000).astype(np.float16)
+    if size > 1e3:
+        t["w"] *= NP["f16"](0.125)
+        t["x"] *= NP["f16"](0.125)
+    check(t, "f16", "silu")
+    t["gh"][:] = 0
+    check(t, "f16", "silu")
+
+
+def test_a_row_that_is_not_finite_stays_a_row():
+    t = draw(200, 64, 72, "f16", 6)
+    x, w, b, gh = (gpu(t[k]) for k in ("x", "w", "b", "gh"))
+    clean = dcn.dcnv4_gated_linear(x, w, b), dcn.dcnv4_gated_linear_backward(x, w, gh, b)[0]
+    x[77] = float("nan")
+    x[150, 3] = float("inf")
+    dirty = dcn.dcnv4_gated_linear(x, w, b), dcn.dcnv4_gated_linear_backward(x, w, gh, b)[0]
+    keep = torch.ones(200, dtype=torch.bool, device="cuda")
+    keep[[77, 150]] = False
+    for a, c in zip(clean, dirty):
+        assert torch.equal(a[keep], c[keep]) and bool(torch.isnan(c[77]).all())
+    # an infinite grad_h: not the size that d goes by
+    x, gh = gpu(t["x"]), gpu(t["gh"])
+    clean = dcn.dcnv4_gated_linear_backward(x, w, gh, b)[0]
+    gh[5, 2] = float("inf")
+    dirty = dcn.dcnv4_gated_linear_backward(x, w, gh, b)[0]
+    keep = torch.arange(200, device="cuda") != 5
+    assert torch.equal(clean[keep], dirty[keep]) and not bool(torch.isfinite(dirty[5]).any())
+
+
+LINEAR = {"f16": [(1, 16, 8), (3, 32, 40), (65, 48, 1000), (300, 272, 72), (2000, 96, 136), (513, 1040, 264), (200, 136, 48)],
+          "f32": [(1, 8, 8), (3, 24, 40), (65, 40, 520), (300, 88, 72), (1200, 96, 136), (130, 520, 264)]}
+
+
+@pytest.mark.parametrize("tile,splits", [(0, 0), (1, 0), (2, 0), (3, 0), (0, 5)])
+@pytest.mark.parametrize("dtype,size", [(d, s) for d in LINEAR for s in LINEAR[d]])
+def test_linear_backward(dtype, size, tile, splits):
+    dcn.dcnv4_set_option("layer_tile", tile)
+    dcn.dcnv4_set_option("layer_splits", splits)
+    P, K, N = size
+    rng = np.random.default_rng(sum(size))
+    t = {"x": rng.standard_normal((P, K)), "w": rng.standard_normal((N, K)) / np.sqrt(K), "gy": 0.1 * rng.standard_normal((P, N)), "b": rng.standard_normal(N)}
+    t = {k: v.astype(NP[dtype]) for k, v in t.items()}
+    x, w, gy, b = (gpu(t[k]) for k in ("x", "w", "gy", "b"))
+    got = dict(zip(("grad_x", "grad_w", "grad_b"), dcn.dcnv4_linear_backward(x, w, gy, b)))
+    for name, (want, slack) in ref.linear_backward(t["x"], t["w"], t["gy"], dtype == "f16").items():
+        close(name, got[name], want, slack, dtype)
+    gx, gw, gb = dcn.dcnv4_linear_backward(x, w, gy, need_x=False)
+    assert gx is None and gb is None and torch.equal(gw, got["grad_w"])
+
+
+def test_gradients_through_the_forward_layers_by_differences():
+    """A sum over the layers' own results in fp32, moved along a direction in each input: its slope is the gradients' product with that direction."""
+    t = draw(60, 24, 40, "f32", 7)
+    x, w, b, gh = (gpu(t[k]) for k in ("x", "w", "b", "gh"))
+    gx, gw, gb = dcn.dcnv4_gated_linear_backward(x, w, gh, b, activation="gelu")
+    value = lambda x, w, b: (dcn.dcnv4_gated_linear(x, w, b, activation="gelu").double() * gh.double()).sum().item()
+    step = 2.0 ** -9
+    for i, grad in enumerate((gx, gw, gb)):
+        way = torch.randn_like(grad)
+        moved = [[v + s * step * way if j == i else v for j, v in enumerate((x, w, b))] for s in (1, -1)]
+        slope = (value(*moved[0]) - value(*moved[1])) / (2 * step)
+        size = (grad.double() * way.double()).norm().item()
+        # the difference's own error: third derivatives times step^2 / 6, and roundings of the results over 2 * step
+        assert abs(slope - (grad.double() * way.double()).sum().item()) <= 1e-3 * size + 1e-3, i
+    x, w, b = (gpu(a) for a in (np.random.default_rng(1).standard_normal((33, 32)).astype(np.float32), t["w"][0, :32, :8].repeat(4, 1), t["b"][0, :32]))
+    gy = torch.randn((33, 32), device="cuda")
+    grads = dcn.dcnv4_linear_backward(x, w, gy, b)
+    value = lambda x, w, b: (dcn.dcnv4_linear(x, w, b).double() * gy.double()).sum().item()
+    for i, grad in enumerate(grads):
+        way = torch.randn_like(grad)
+        moved = [[v + s * way if j == i else v for j, v in enumerate((x, w, b))] for s in (1, -1)]
+        size = (grad.double() * way.double()).norm().item()
+        assert abs((value(*moved[0]) - value(*moved[1])) / 2 - (grad.double() * way.double()).sum().item()) <= 1e-4 * size + 1e-3, i
+
+
+def test_nothing_is_written_behind_the_results():
+    for P, K, F in ((37, 48, 40), (300, 272, 136)):
+        t = draw(P, K, F, "f16", 8)
+        x, w, b, gh = (gpu(t[k]) for k in ("x", "w", "b", "gh"))
+        shapes = {"h": (P, F), "gx": (P, K), "gw": (2, F, K), "gb": (2, F)}
+        room = {k: torch.full((int(np.prod(s)) + 4096,), 5.0, dtype=torch.float16, device="cuda") for k, s in shapes.items()}
+        part = {k: room[k][:int(np.prod(s))].view(s) for k, s in shapes.items()}
+        for tile in (1, 2, 3):
+            dcn.dcnv4_set_option("layer_tile", tile)
+            need = dcn.dcnv4_gated_linear_workspace_bytes(P, K, F, 1, True)
+            space = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+            dcn.dcnv4_gated_linear(x, w, b, out=part["h"])
+            dcn.dcnv4_gated_linear_backward(x, w, gh, b, out=[part["gx"], part["gw"], part["gb"]], workspace=space[:need])
+            assert bool((space[need:] == 77).all())
+            for k, s in shapes.items():
+                assert bool((room[k][int(np.prod(s)):] == 5.0).all()), k
+
+
+def test_streams_graphs_and_repeated_bits():
+    t = draw(500, 96, 136, "f16", 9)
+    x, w, b, gh = (gpu(t[k]) for k in ("x", "w", "b", "gh"))
+    down = gpu(np.random.default_rng(2).standard_normal((64, 136)).astype(np.float16))
+    gy = torch.randn((500, 64), device="cuda").half()
+
+    def step(**kw):
+        h = dcn.dcnv4_gated_linear(x, w, b, **kw)
+        g = dcn.dcnv4_linear_backward(h, down, gy, down[:, 0].contiguous(), **kw)
+        return (h, *g, *dcn.dcnv4_gated_linear_backward(x, w, g[0], b, **kw))
+
+    want = step()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(want, step()))
+    with torch.cuda.stream(s):
+        got = step(stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(want, got))
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            outs = step()
+    for k in range(3):
+        torch.cuda.synchronize()
+        x.normal_()
+        gy.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        assert all(torch.equal(a, c) for a, c in zip(got, step())), k
+
+
+def test_refusals():
+    x, w, b, gh = (gpu(v) for v in draw(6, 32, 16, "f16", 10).values())
+    for bad in (lambda: dcn.dcnv4_gated_linear(x, w[0]), lambda: dcn.dcnv4_gated_linear(x, w[:, :, :16]), lambda: dcn.dcnv4_gated_linear(x, w, b[0]),
+                lambda: dcn.dcnv4_gated_linear(x, w, b, activation="relu"), lambda: dcn.dcnv4_gated_linear(x, w.float(), b), lambda: dcn.dcnv4_gated_linear(x.t(), w),
+                lambda: dcn.dcnv4_gated_linear_backward(x, w, gh[:5], b), lambda: dcn.dcnv4_gated_linear_backward(x, w, gh[:, :8], b),
+                lambda: dcn.dcnv4_linear_backward(x, w[0], gh[:, :8]), lambda: dcn.dcnv4_linear_backward(x, w[0], gh, b[0][:8]),
+                lambda: dcn.dcnv4_linear_backward(x, w[0].cpu(), gh)):
+        with pytest.raises(ValueError):
+            bad()
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    for bad in (lambda: dcn.dcnv4_gated_linear(x[:, :20].contiguous(), w[:, :, :20].contiguous()), lambda: dcn.dcnv4_gated_linear(x, w[:, :12].contiguous()),
+                lambda: dcn.dcnv4_gated_linear_backward(x, w, gh, b, workspace=small), lambda: dcn.dcnv4_linear_backward(x, w[0], gh, workspace=small),
+                lambda: dcn.dcnv4_linear_backward(x, w[0, :12].contiguous(), gh[:, :12].contiguous()),
+                lambda: dcn.dcnv4_gated_linear(x.float(), w.float(), workspace=small)):
+        with pytest.raises(dcn.Dcnv4Error):
+            bad()
