@@ -58,6 +58,29 @@ template <int ACT, bool EXACT> __device__ __forceinline__ Act activation(float a
     }
 }
 
+// Sixteen numbers of each lane summed over the lane's half of the wave: lane i gets the sum of number i % 16.  Lanes whose numbers differ in a bit exchange
+// halves of what they still have: 15 additions and one, where each number's own sum would take five.
+__device__ __forceinline__ float sums_of_32(float (&v)[16])
+{
+    const int lane = (int)threadIdx.x & 63;
+    auto halve = [&](auto ctrl, int bit, int left) {
+        const bool up = (lane & bit) != 0;
+#pragma unroll
+        for (int i = 0; i < left; ++i) {
+            const float keep = up ? v[i + left] : v[i], give = up ? v[i] : v[i + left];
+            v[i] = keep + dpp<decltype(ctrl)::value>(give);
+        }
+    };
+    // (mirrors change more bits than one: the lane on the other side has the other half, and the same numbers of the halves before)
+    halve(std::integral_constant<int, 0x140>(), 8, 8);     // row_mirror: lane 15 - i
+    halve(std::integral_constant<int, 0x141>(), 4, 4);     // row_half_mirror: lane 7 - i of eight
+    halve(std::integral_constant<int, 0x4E>(), 2, 2);      // quad_perm [2,3,0,1]
+    halve(std::integral_constant<int, 0xB1>(), 1, 1);      // quad_perm [1,0,3,2]
+    float a = v[0], b = v[0];
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return a + b;
+}
+
 struct Pairs {
     const void *bias;                                      // [2][F] of the layer's type, or null
     int F, P;
@@ -144,6 +167,16 @@ struct Deltas {
     Scale *scale;                                          // fp16: what undoes d's factor
 };
 
+// Four numbers at a byte offset.
+template <typename T> __device__ __forceinline__ auto load_four(rsrc_t r, int at)
+{
+    typedef T four __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(T) == 2)
+        return __builtin_bit_cast(four, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0));
+    else
+        return __builtin_bit_cast(four, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+}
+
 struct Result {
     void *out;                                             // [b rows][a rows] of T; or float planes, one per split
     long long plane;                                       // floats
@@ -226,19 +259,21 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     f32x16 acc[WM][WN];
     start_with_bias<T, WM, WN>(l, first, kb, acc);
     G::multiply(smem, q.a, q.b, at * (G::BM / 2), bt * G::BN, 0, q.steps, acc);
+    // (all asked for at once; outside the tensor, which a wave's pixels may be altogether: zeros.  128 pixels of 2^19 numbers at most: 2^28 bytes)
+    four g[WN][WM][2];
+    const int pixels = max(min(l.P - px0, 32 * WN), 0);
+    const rsrc_t from = make_rsrc((const T *)d.grad_h + (long long)px0 * l.F, (unsigned)(pixels * l.F * (int)sizeof(T)));
 #pragma unroll
-    for (int n = 0; n < WN; ++n) {
-        const int px = px0 + n * 32 + row;
-        four g[WM][2];
+    for (int n = 0; n < WN; ++n)
 #pragma unroll
         for (int m = 0; m < WM; ++m)
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
                 const int f = first + pair_of(m, a, kb);
-                g[m][a] = four{};
-                if (px < l.P && f < l.F)
-                    g[m][a] = *reinterpret_cast<const four *>((const T *)d.grad_h + (long long)px * l.F + f);
+                g[n][m][a] = load_four<T>(from, f < l.F ? ((n * 32 + row) * l.F + f) * (int)sizeof(T) : kOutside);
             }
+#pragma unroll
+    for (int n = 0; n < WN; ++n)
 #pragma unroll
         for (int m = 0; m < WM; ++m)
 #pragma unroll
@@ -246,28 +281,25 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const Act v = activation<ACT, PL == 3>(acc[m][n][4 * a + c]);
-                    const float gh = (float)g[m][a][c];
+                    const float gh = (float)g[n][m][a][c];
                     acc[m][n][4 * a + c] = gh * acc[m][n][4 * (a + 2) + c] * v.slope;
                     acc[m][n][4 * (a + 2) + c] = gh * v.value;
                 }
-    }
     if (d.bias_sums != nullptr) {
-        // over the pixels of a lane, then of 32 lanes; lane i of them stores number i
 #pragma unroll
         for (int m = 0; m < WM; ++m) {
-            float mine = 0.f;
+            float v[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                float s = 0.f;
+                v[r] = acc[m][0][r];
 #pragma unroll
-                for (int n = 0; n < WN; ++n)
-                    s += acc[m][n][r];
-                s = sum_of_32(s);
-                mine = (row & 15) == r ? s : mine;
+                for (int n = 1; n < WN; ++n)
+                    v[r] += acc[m][n][r];
             }
+            const float sum = sums_of_32(v);               // lane i: of number i % 16
             const int r = row & 15, f = first + pair_of(m, r >> 2 & 1, kb) + (r & 3);
             if (row < 16 && f < l.F)
-                d.bias_sums[((long long)(bt * WC + wc) * 2 + (r >> 3)) * l.F + f] = mine;
+                d.bias_sums[((long long)(bt * WC + wc) * 2 + (r >> 3)) * l.F + f] = sum;
         }
     }
     // results in 16 bits, PL planes one after the other: 32 pixels at a time, each 16 * WM numbers of da and as many of du
@@ -454,9 +486,16 @@ bool fits(int pl, const Choice &c, long long m, long long n)
     return c.shape >= 0 && ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn) * c.splits < (1 << 22);     // (a grid has fewer than 2^32 lanes)
 }
 
+// A product over pixels in one launch, or in two: as many pixels as give whole rounds of large tiles, and the others in the tile that suits them.
+struct Parts {
+    int count, pixels[2];
+    Choice choice[2];
+};
+
 struct LayerPlan {
     int pl, es, P, K, N, kp, np;       // N: results of the layer (gated: 2F); padded in split operands
-    Choice forward, gx, gw;
+    Parts forward;
+    Choice gx, gw;
     int most_parts, columns_runs, columns_rows;
     // bytes from the start of the workspace
     long long x_split, w_split, g_split, d, scale, most, bias_sums, gx_at, gw_at, bytes;
@@ -481,6 +520,22 @@ struct Room {
         return here;
     }
 };
+
+// (12544 x 512, 2 x 2048, fp16: 784 large tiles for 256 units; forward 74 us in one launch, FWD2 in two)
+Parts parts_of(int pl, int m, int P, int length)
+{
+    Parts best = {1, {P, 0}, {choose_product(pl, m, P, length, false, g_layers.tile, 0), {0, 1}}};
+    const Shape &s = shape_of(pl, kLarge);
+    const long long across = (m + s.bm - 1) / s.bm, rounds = across * ((P + s.bn - 1) / s.bn) / kUnits;
+    const long long first = rounds * kUnits / across * s.bn;
+    if (g_layers.tile || first <= 0 || first >= P)
+        return best;
+    const Choice rest = choose_product(pl, m, P - first, length, false, 0, 0);
+    const Choice &one = best.choice[0];
+    if (estimate(s, m, first, length, 1) + estimate(shape_of(pl, rest.shape), m, P - first, length, 1) + 3.f < estimate(shape_of(pl, one.shape), m, P, length, 1))
+        best = {2, {(int)first, P - (int)first}, {{kLarge, 1}, rest}};
+    return best;
+}
 
 // The two products of a gradient, and room for their planes: [P][K] over N numbers, [N][K] over P.
 bool plan_gradients(LayerPlan &p, Room &room)
@@ -513,9 +568,10 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
     p.kp = p.pl == 1 ? K : (int)round_up(K, 32);
     if ((long long)p.N * p.pl * p.kp * 2 >= 0x7fffffffLL)
         return DCNV4_ERR_UNSUPPORTED;
-    p.forward = choose_product(p.pl, p.N, P, p.kp, false, g_layers.tile, 0);
-    if (!fits(p.pl, p.forward, p.N, P))
-        return DCNV4_ERR_UNSUPPORTED;
+    p.forward = parts_of(p.pl, p.N, p.P, p.kp);
+    for (int i = 0; i < p.forward.count; ++i)
+        if (!fits(p.pl, p.forward.choice[i], p.N, p.forward.pixels[i]))
+            return DCNV4_ERR_UNSUPPORTED;
     Room room;
     if (p.pl == 3) {
         p.x_split = room.take(P * 6 * p.kp);
@@ -648,52 +704,74 @@ Operand narrowed(Operand o, int K)
     return o;
 }
 
+// The rows of an operand from `first` on.
+Operand rows_from(Operand o, int first, int count)
+{
+    o.base += first * o.row_bytes;
+    o.count = count;
+    return o;
+}
+
 template <typename T, int PL>
-int gated_forward(const LayerPlan &p, const void *x, const void *w, const Pairs &l, int act, void *h, char *ws, hipStream_t s)
+int gated_forward(const LayerPlan &p, const void *x, const void *w, const void *bias, int F, int act, T *h, char *ws, hipStream_t s)
 {
     Operand xo, wo;
     operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
-    wo.count = l.F;
-    const Product q = product_of(wo, xo, PL, p.forward, true);
-    by_activation(act, [&](auto A) {
-        with_tile<PL>(p.forward.shape, [&](auto t) {
-            typedef decltype(t) G;
-            hipLaunchKernelGGL((dcnv4_gated_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
-                               dim3(G::WR * G::WC * 64), 0, s, q, l, (T *)h);
-            return 0;
+    wo.count = F;
+    int first = 0;
+    for (int i = 0; i < p.forward.count; ++i) {
+        const Choice &c = p.forward.choice[i];
+        const Pairs l = {bias, F, p.forward.pixels[i]};
+        const Product q = product_of(wo, rows_from(xo, first, l.P), PL, c, true);
+        by_activation(act, [&](auto A) {
+            with_tile<PL>(c.shape, [&](auto t) {
+                typedef decltype(t) G;
+                hipLaunchKernelGGL((dcnv4_gated_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
+                                   dim3(G::WR * G::WC * 64), 0, s, q, l, h + (long long)first * F);
+                return 0;
+            });
         });
-    });
+        first += l.P;
+    }
     return launched();
 }
 
 template <typename T, int PL>
-int gated_backward(const LayerPlan &p, const void *x, const void *w, const Pairs &l, int act, const void *grad_h, void *grad_x, void *grad_w, void *grad_b,
+int gated_backward(const LayerPlan &p, const void *x, const void *w, const void *bias, int F, int act, const T *grad_h, void *grad_x, void *grad_w, void *grad_b,
                    char *ws, hipStream_t s)
 {
     if (PL == 1)
-        hipLaunchKernelGGL(dcnv4_gated_most_kernel, dim3((unsigned)p.most_parts), dim3(256), 0, s, (const unsigned short *)grad_h, (long long)p.P * l.F,
+        hipLaunchKernelGGL(dcnv4_gated_most_kernel, dim3((unsigned)p.most_parts), dim3(256), 0, s, (const unsigned short *)grad_h, (long long)p.P * F,
                            (float *)(ws + p.most));
     Operand xo, wo;
     operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
     Operand pairs = wo;
-    pairs.count = l.F;
-    const Product q = product_of(pairs, xo, PL, p.forward, true);
+    pairs.count = F;
     Scale *scale = PL == 1 ? (Scale *)(ws + p.scale) : nullptr;
-    const Deltas d = {grad_h, (unsigned short *)(ws + p.d), grad_b ? (float *)(ws + p.bias_sums) : nullptr, (const float *)(ws + p.most), p.most_parts, scale};
-    int runs = 0;
-    by_activation(act, [&](auto A) {
-        with_tile<PL>(p.forward.shape, [&](auto t) {
-            typedef decltype(t) G;
-            runs = q.b_tiles * G::WC;
-            hipLaunchKernelGGL((dcnv4_gated_delta_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
-                               dim3(G::WR * G::WC * 64), 0, s, q, l, d);
-            return 0;
+    unsigned short *d = (unsigned short *)(ws + p.d);
+    float *bias_sums = (float *)(ws + p.bias_sums);
+    int first = 0, runs = 0;
+    for (int i = 0; i < p.forward.count; ++i) {
+        const Choice &c = p.forward.choice[i];
+        const Pairs l = {bias, F, p.forward.pixels[i]};
+        const Product q = product_of(pairs, rows_from(xo, first, l.P), PL, c, true);
+        const Deltas e = {grad_h + (long long)first * F, d + (long long)first * PL * p.N, grad_b ? bias_sums + (long long)runs * p.N : nullptr,
+                          (const float *)(ws + p.most), p.most_parts, scale};
+        by_activation(act, [&](auto A) {
+            with_tile<PL>(c.shape, [&](auto t) {
+                typedef decltype(t) G;
+                runs += q.b_tiles * G::WC;
+                hipLaunchKernelGGL((dcnv4_gated_delta_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
+                                   dim3(G::WR * G::WC * 64), 0, s, q, l, e);
+                return 0;
+            });
         });
-    });
+        first += l.P;
+    }
     Bias b = {};
     if (grad_b)
-        b = {d.bias_sums, runs, p.N, (p.N + 15) / 16, grad_b};
-    gradients<T, PL>(p, narrowed(xo, p.K), narrowed(wo, p.K), rows_of(d.d, p.P, p.N, PL, p.N), scale, b, grad_x, grad_w, ws, s);
+        b = {bias_sums, runs, p.N, (p.N + 15) / 16, grad_b};
+    gradients<T, PL>(p, narrowed(xo, p.K), narrowed(wo, p.K), rows_of(d, p.P, p.N, PL, p.N), scale, b, grad_x, grad_w, ws, s);
     return launched();
 }
 
@@ -760,10 +838,9 @@ int dcnv4_gated_linear(const void *x, const void *w, const void *b, void *h, voi
         return DCNV4_ERR_SHAPE;
     if (off16(x) || off16(w) || off16(b) || off16(h) || off16(workspace))
         return DCNV4_ERR_ALIGN;
-    const Pairs l = {b, F, p.P};
     hipStream_t s = (hipStream_t)stream;
-    return dtype == DCNV4_F16 ? gated_forward<_Float16, 1>(p, x, w, l, activation, h, (char *)workspace, s)
-                              : gated_forward<float, 3>(p, x, w, l, activation, h, (char *)workspace, s);
+    return dtype == DCNV4_F16 ? gated_forward<_Float16, 1>(p, x, w, b, F, activation, (_Float16 *)h, (char *)workspace, s)
+                              : gated_forward<float, 3>(p, x, w, b, F, activation, (float *)h, (char *)workspace, s);
 }
 
 int dcnv4_gated_linear_backward(const void *x, const void *w, const void *b, const void *grad_h, void *grad_x, void *grad_w, void *grad_b, void *workspace,
@@ -781,10 +858,9 @@ int dcnv4_gated_linear_backward(const void *x, const void *w, const void *b, con
         return DCNV4_ERR_SHAPE;
     if (off16(x) || off16(w) || off16(b) || off16(grad_h) || off16(grad_x) || off16(grad_w) || off16(grad_b) || off16(workspace))
         return DCNV4_ERR_ALIGN;
-    const Pairs l = {b, F, p.P};
     hipStream_t s = (hipStream_t)stream;
-    return dtype == DCNV4_F16 ? gated_backward<_Float16, 1>(p, x, w, l, activation, grad_h, grad_x, grad_w, grad_b, (char *)workspace, s)
-                              : gated_backward<float, 3>(p, x, w, l, activation, grad_h, grad_x, grad_w, grad_b, (char *)workspace, s);
+    return dtype == DCNV4_F16 ? gated_backward<_Float16, 1>(p, x, w, b, F, activation, (const _Float16 *)grad_h, grad_x, grad_w, grad_b, (char *)workspace, s)
+                              : gated_backward<float, 3>(p, x, w, b, F, activation, (const float *)grad_h, grad_x, grad_w, grad_b, (char *)workspace, s);
 }
 
 long long dcnv4_linear_backward_workspace_bytes(long long P, int K, int Nout, int dtype)

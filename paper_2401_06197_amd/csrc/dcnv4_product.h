@@ -336,8 +336,23 @@ struct Choice {
     int shape, splits;
 };
 
+// Estimated time (us) of m x n results over `length` numbers, each sum in `splits` parts.
+float estimate(const Shape &s, long long m, long long n, int length, int splits)
+{
+    const int steps = (length + s.r - 1) / s.r;
+    const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
+    const float x = (float)(tiles * splits) / (float)kUnits, full = ceilf(x), slots = (float)s.slots;
+    const float rounds = x > slots ? slots * ceilf(x / slots) : full, even = s.slots > 1 && x > 1.f ? .5f * (x + full) : full;
+    const float share = even + s.gen * (rounds - even);
+    const float step = s.step * share > s.alone ? s.step * share : s.alone;
+    float us = (float)((steps + splits - 1) / splits) * step + s.fixed * share;
+    if (splits > 1)                                        // planes written and read once more, by a launch of its own
+        us += 2.5f + .09f * (float)splits + (float)(m * n) * (float)splits * 1.2e-6f;
+    return us;
+}
+
 // The tile, and over how many workgroups a sum is split, with the lowest estimated time.
-// Test switches: only the tile `only` (1 + its number; 0: any); `splits` workgroups to a sum, where it may be split (0: any).
+// Test switches: only the tile `only` (1 + its number; 0: any); `asked` workgroups to a sum, where it may be split (0: any).
 Choice choose_product(int pl, long long m, long long n, int length, bool may_split, int only, int asked)
 {
     Choice best = {-1, 1};
@@ -346,20 +361,13 @@ Choice choose_product(int pl, long long m, long long n, int length, bool may_spl
         if (only && only != 1 + i)
             continue;
         const Shape &s = shape_of(pl, i);
-        const int steps = (length + s.r - 1) / s.r;
         const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
         // powers of two, and what fills the units once and twice
         const int fill = tiles < kUnits ? (int)(kUnits / tiles) : 1, tries[] = {1, 2, 4, 8, 16, 32, 64, fill, 2 * fill};
         for (const int splits : tries) {
             if (splits > 1 && (!may_split || splits > 64 || length / splits < 256))
                 continue;
-            const float x = (float)(tiles * splits) / (float)kUnits, full = ceilf(x), slots = (float)s.slots;
-            const float rounds = x > slots ? slots * ceilf(x / slots) : full, even = s.slots > 1 && x > 1.f ? .5f * (x + full) : full;
-            const float share = even + s.gen * (rounds - even);
-            const float step = s.step * share > s.alone ? s.step * share : s.alone;
-            float us = (float)((steps + splits - 1) / splits) * step + s.fixed * share;
-            if (splits > 1)                                // planes written and read once more, by a launch of its own
-                us += 2.5f + .09f * (float)splits + (float)(m * n) * (float)splits * 1.2e-6f;
+            const float us = estimate(s, m, n, length, splits);
             if (best.shape < 0 || us < best_us) {
                 best = {i, splits};
                 best_us = us;

@@ -72,6 +72,12 @@ def test_gated_layer(dtype, size, tile, act):
     check(draw(*size, dtype, sum(size)), dtype, act)
 
 
+@pytest.mark.parametrize("dtype,P", [("f16", 256 * 256 + 465), ("f32", 128 * 256 + 233)])
+def test_pixels_in_two_launches(dtype, P):
+    """One tile of pairs, and pixels for a whole round of large tiles and some more, which go by themselves."""
+    check(draw(P, 256, 128, dtype, 11), dtype, "silu")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("splits", [2, 3, 64])
 def test_sums_in_parts(dtype, splits):
