@@ -237,25 +237,10 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
     const int first = at * (G::BM / 2) + wr * 16 * WM, px0 = bt * G::BN + wc * 32 * WN;
-    float up = 1.f;
-    if constexpr (PL == 1) {
-        float top = 0.f;
+    float top = 0.f;                                       // (asked for here, joined after the products)
+    if constexpr (PL == 1)
         for (int i = (int)threadIdx.x; i < d.parts; i += G::kThreads)
             top = fmaxf(top, d.most[i]);
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2)
-            top = fmaxf(top, __shfl_xor(top, s));
-        if (lane == 0)
-            tops[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < G::kWaves; ++w)
-            top = fmaxf(top, tops[w]);
-        const int e = top > 0.f ? 2 - __builtin_amdgcn_frexp_expf(top) : 0;
-        up = ldexpf(1.f, e);
-        if (at == 0 && bt == 0 && threadIdx.x == 0)
-            d.scale->by = ldexpf(1.f, -e);
-    }
     f32x16 acc[WM][WN];
     start_with_bias<T, WM, WN>(l, first, kb, acc);
     G::multiply(smem, q.a, q.b, at * (G::BM / 2), bt * G::BN, 0, q.steps, acc);
@@ -272,6 +257,23 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
                 const int f = first + pair_of(m, a, kb);
                 g[n][m][a] = load_four<T>(from, f < l.F ? ((n * 32 + row) * l.F + f) * (int)sizeof(T) : kOutside);
             }
+    float up = 1.f, down = 1.f;
+    if constexpr (PL == 1) {
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2)
+            top = fmaxf(top, __shfl_xor(top, s));
+        if (lane == 0)
+            tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < G::kWaves; ++w)
+            top = fmaxf(top, tops[w]);
+        const int e = top > 0.f ? 2 - __builtin_amdgcn_frexp_expf(top) : 0;
+        up = ldexpf(1.f, e);
+        down = ldexpf(1.f, -e);
+        if (at == 0 && bt == 0 && threadIdx.x == 0)
+            d.scale->by = down;
+    }
 #pragma unroll
     for (int n = 0; n < WN; ++n)
 #pragma unroll
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const Act v = activation<ACT, PL == 3>(acc[m][n][4 * a + c]);
-                    const float gh = (float)g[n][m][a][c];
+                    const float gh = (float)g[n][m][a][c] * up;     // (exact: a power of two)
                     acc[m][n][4 * a + c] = gh * acc[m][n][4 * (a + 2) + c] * v.slope;
                     acc[m][n][4 * (a + 2) + c] = gh * v.value;
                 }
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
             const float sum = sums_of_32(v);               // lane i: of number i % 16
             const int r = row & 15, f = first + pair_of(m, r >> 2 & 1, kb) + (r & 3);
             if (row < 16 && f < l.F)
-                d.bias_sums[((long long)(bt * WC + wc) * 2 + (r >> 3)) * l.F + f] = sum;
+                d.bias_sums[((long long)(bt * WC + wc) * 2 + (r >> 3)) * l.F + f] = sum * down;
         }
     }
     // results in 16 bits, PL planes one after the other: 32 pixels at a time, each 16 * WM numbers of da and as many of du
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
                     for (int c = 0; c < 4; ++c) {
                         const float v = acc[m][n][4 * a + c];
                         if constexpr (PL == 1) {
-                            s[c] = __builtin_bit_cast(unsigned short, (_Float16)(v * up));
+                            s[c] = __builtin_bit_cast(unsigned short, (_Float16)v);
                         } else {
                             const __bf16 b = (__bf16)v;
                             acc[m][n][4 * a + c] = v - (float)b;
@@ -414,60 +416,82 @@ __global__ __launch_bounds__(256) void dcnv4_layer_sum_kernel(const float *plane
 }
 template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_bias_kernel(Bias b) { bias_of<T>(b, (int)blockIdx.x); }
 
-// fp32 rows as the products take them: in [rows][cols] -> out [rows][3 planes][pad] of bf16, zeros behind the columns.  Eight numbers a lane.
-__global__ __launch_bounds__(256) void dcnv4_layer_split_kernel(const float *in, long long rows, int cols, int pad, unsigned short *out)
-{
-    const int units = pad / 8;
-    const long long all = rows * units;
-    for (long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long row = i / units;
-        const int u = (int)(i - row * units);
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (u * 8 < cols)                                  // (columns come in eights)
-            __builtin_memcpy(v, __builtin_assume_aligned(in + row * cols + u * 8, 16), sizeof(v));
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            unsigned short s[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const __bf16 b = (__bf16)v[e];
-                v[e] -= (float)b;
-                s[e] = __builtin_bit_cast(unsigned short, b);
-            }
-            __builtin_memcpy(__builtin_assume_aligned(out + (row * 3 + p) * pad + u * 8, 16), s, sizeof(s));
-        }
-    }
-}
+namespace {
 
-// Sums over runs of rows of g [P][N] (N a multiple of eight): out [runs][N].  Eight columns a lane; `lanes` of them side by side, 256 / lanes rows.
-template <typename T>
-__global__ __launch_bounds__(256) void dcnv4_layer_columns_kernel(const T *g, int P, int N, int lanes_log, int rows, float *out)
+// What is made in front of the products, in one launch: sums over runs of rows of g, and fp32 tensors as the products take them.
+struct Ahead {
+    const void *g;                                         // [P][N], N a multiple of eight; sums [runs][N]
+    float *sums;
+    int P, N, lanes_log, run_rows, across, blocks;         // workgroups: `across` to a run, none for no sums
+    struct {
+        const float *in;                                   // [rows][cols] -> out [rows][3 planes][pad] of bf16, zeros behind the columns
+        unsigned short *out;
+        long long rows;
+        int cols, pad, blocks;
+    } split[3];
+};
+
+}  // namespace
+
+// Sums: eight columns a lane, 2^lanes_log of them side by side and 256 >> lanes_log rows.  Splits: eight numbers a lane.
+// (One launch where there were four: 2047 x 384 -> 1000 fp32 backward AHEAD1)
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_ahead_kernel(Ahead q)
 {
     typedef T eight __attribute__((ext_vector_type(8)));
     __shared__ float part[256][9];
-    const int lanes = 1 << lanes_log, side = 256 >> lanes_log, l = (int)threadIdx.x & (lanes - 1), s = (int)threadIdx.x >> lanes_log;
-    const int c = ((int)blockIdx.x * lanes + l) * 8, r0 = (int)blockIdx.y * rows, r1 = min(r0 + rows, P);
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c < N)
+    int block = (int)blockIdx.x;
+    if (block < q.blocks) {
+        const int run = block / q.across, lanes = 1 << q.lanes_log, side = 256 >> q.lanes_log, l = (int)threadIdx.x & (lanes - 1);
+        const int c0 = (block - run * q.across) * lanes * 8, c = c0 + l * 8, r0 = run * q.run_rows, r1 = min(r0 + q.run_rows, q.P);
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (c < q.N)
 #pragma unroll 4
-        for (int r = r0 + s; r < r1; r += side) {
-            const eight t = *reinterpret_cast<const eight *>(g + (long long)r * N + c);
+            for (int r = r0 + ((int)threadIdx.x >> q.lanes_log); r < r1; r += side) {
+                const eight t = *reinterpret_cast<const eight *>((const T *)q.g + (long long)r * q.N + c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] += (float)t[e];
+                for (int e = 0; e < 8; ++e)
+                    v[e] += (float)t[e];
+            }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            part[threadIdx.x][e] = v[e];
+        __syncthreads();
+        // eight lanes' numbers side by side: a lane a column, over the rows in order
+        for (int i = (int)threadIdx.x; i < lanes * 8; i += 256) {
+            float sum = 0.f;
+            for (int k = 0; k < side; ++k)
+                sum += part[k * lanes + (i >> 3)][i & 7];
+            if (c0 + i < q.N)
+                q.sums[(long long)run * q.N + c0 + i] = sum;
         }
+        return;
+    }
+    block -= q.blocks;
+    if constexpr (sizeof(T) == 4) {
+        int k = 0;
+        while (k < 2 && block >= q.split[k].blocks)
+            block -= q.split[k++].blocks;
+        const auto &t = q.split[k];
+        const int units = t.pad / 8;
+        const long long all = t.rows * units;
+        for (long long i = (long long)block * 256 + (int)threadIdx.x; i < all; i += (long long)t.blocks * 256) {
+            const long long row = i / units;
+            const int u = (int)(i - row * units);
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (u * 8 < t.cols)                            // (columns come in eights)
+                __builtin_memcpy(v, __builtin_assume_aligned(t.in + row * t.cols + u * 8, 16), sizeof(v));
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        part[threadIdx.x][e] = v[e];
-    __syncthreads();
-    // eight lanes' numbers side by side: a lane a column, over the rows in order
-    for (int i = (int)threadIdx.x; i < lanes * 8; i += 256) {
-        float sum = 0.f;
-        for (int k = 0; k < side; ++k)
-            sum += part[k * lanes + (i >> 3)][i & 7];
-        const int col = (int)blockIdx.x * lanes * 8 + i;
-        if (col < N)
-            out[(long long)blockIdx.y * N + col] = sum;
+            for (int p = 0; p < 3; ++p) {
+                unsigned short s[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const __bf16 b = (__bf16)v[e];
+                    v[e] -= (float)b;
+                    s[e] = __builtin_bit_cast(unsigned short, b);
+                }
+                __builtin_memcpy(__builtin_assume_aligned(t.out + (row * 3 + p) * t.pad + u * 8, 16), s, sizeof(s));
+            }
+        }
     }
 }
 
@@ -622,11 +646,20 @@ int plan_linear_backward(LayerPlan *out, long long P, int K, int N, int dtype)
     return DCNV4_OK;
 }
 
-void split_rows(const void *in, long long rows, int cols, int pad, void *out, hipStream_t s)
+void add_split(Ahead &q, const void *in, long long rows, int cols, int pad, void *out)
 {
+    int k = 0;
+    while (q.split[k].blocks > 0)
+        ++k;
     const long long groups = (rows * (pad / 8) + 255) / 256;
-    hipLaunchKernelGGL(dcnv4_layer_split_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, (const float *)in, rows, cols, pad,
-                       (unsigned short *)out);
+    q.split[k] = {(const float *)in, (unsigned short *)out, rows, cols, pad, (int)(groups < 4096 ? groups : 4096)};
+}
+
+template <typename T> void launch_ahead(const Ahead &q, hipStream_t s)
+{
+    const int blocks = q.blocks + q.split[0].blocks + q.split[1].blocks + q.split[2].blocks;
+    if (blocks > 0)
+        hipLaunchKernelGGL((dcnv4_layer_ahead_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, q);
 }
 
 template <typename T, int PL, bool PIXELS> void launch_product(const Product &q, const Choice &c, const Result &o, hipStream_t s)
@@ -685,13 +718,13 @@ template <typename F> void by_activation(int act, F &&f)
 }
 
 // x and w as the products take them
-template <int PL> void operands(const LayerPlan &p, const void *x, const void *w, char *ws, bool with_x, bool with_w, Operand *xo, Operand *wo, hipStream_t s)
+template <int PL> void operands(const LayerPlan &p, const void *x, const void *w, char *ws, bool with_x, bool with_w, Operand *xo, Operand *wo, Ahead &q)
 {
     if (PL == 3) {
         if (with_x)
-            split_rows(x, p.P, p.K, p.kp, ws + p.x_split, s);
+            add_split(q, x, p.P, p.K, p.kp, ws + p.x_split);
         if (with_w)
-            split_rows(w, p.N, p.K, p.kp, ws + p.w_split, s);
+            add_split(q, w, p.N, p.K, p.kp, ws + p.w_split);
     }
     *xo = rows_of(PL == 3 ? (const void *)(ws + p.x_split) : x, p.P, p.kp, PL, p.kp);
     *wo = rows_of(PL == 3 ? (const void *)(ws + p.w_split) : w, p.N, p.kp, PL, p.kp);
@@ -716,7 +749,9 @@ template <typename T, int PL>
 int gated_forward(const LayerPlan &p, const void *x, const void *w, const void *bias, int F, int act, T *h, char *ws, hipStream_t s)
 {
     Operand xo, wo;
-    operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
+    Ahead ahead = {};
+    operands<PL>(p, x, w, ws, true, true, &xo, &wo, ahead);
+    launch_ahead<T>(ahead, s);
     wo.count = F;
     int first = 0;
     for (int i = 0; i < p.forward.count; ++i) {
@@ -744,7 +779,9 @@ int gated_backward(const LayerPlan &p, const void *x, const void *w, const void 
         hipLaunchKernelGGL(dcnv4_gated_most_kernel, dim3((unsigned)p.most_parts), dim3(256), 0, s, (const unsigned short *)grad_h, (long long)p.P * F,
                            (float *)(ws + p.most));
     Operand xo, wo;
-    operands<PL>(p, x, w, ws, true, true, &xo, &wo, s);
+    Ahead ahead = {};
+    operands<PL>(p, x, w, ws, true, true, &xo, &wo, ahead);
+    launch_ahead<T>(ahead, s);
     Operand pairs = wo;
     pairs.count = F;
     Scale *scale = PL == 1 ? (Scale *)(ws + p.scale) : nullptr;
@@ -779,18 +816,27 @@ template <typename T, int PL>
 int linear_backward(const LayerPlan &p, const void *x, const void *w, const void *grad_y, void *grad_x, void *grad_w, void *grad_b, char *ws, hipStream_t s)
 {
     Operand xo, wo;
-    operands<PL>(p, x, w, ws, grad_w != nullptr, grad_x != nullptr, &xo, &wo, s);
+    Ahead ahead = {};
+    operands<PL>(p, x, w, ws, grad_w != nullptr, grad_x != nullptr, &xo, &wo, ahead);
     if (PL == 3 && (grad_x || grad_w))
-        split_rows(grad_y, p.P, p.N, p.np, ws + p.g_split, s);
+        add_split(ahead, grad_y, p.P, p.N, p.np, ws + p.g_split);
     Bias b = {};
     if (grad_b) {
         b = {(const float *)(ws + p.bias_sums), p.columns_runs, p.N, (p.N + 15) / 16, grad_b};
         int log = 0;
         while (log < 6 && (8 << log) < p.N)
             ++log;
-        hipLaunchKernelGGL((dcnv4_layer_columns_kernel<T>), dim3((unsigned)((p.N / 8 + (1 << log) - 1) >> log), (unsigned)p.columns_runs), dim3(256), 0, s,
-                           (const T *)grad_y, p.P, p.N, log, p.columns_rows, (float *)(ws + p.bias_sums));
+        const int across = (p.N / 8 + (1 << log) - 1) >> log;
+        ahead.g = grad_y;
+        ahead.sums = (float *)(ws + p.bias_sums);
+        ahead.P = p.P;
+        ahead.N = p.N;
+        ahead.lanes_log = log;
+        ahead.run_rows = p.columns_rows;
+        ahead.across = across;
+        ahead.blocks = across * p.columns_runs;
     }
+    launch_ahead<T>(ahead, s);
     gradients<T, PL>(p, narrowed(xo, p.K), narrowed(wo, p.K), rows_of(PL == 3 ? (const void *)(ws + p.g_split) : grad_y, p.P, p.N, PL, p.np), nullptr, b, grad_x,
                      grad_w, ws, s);
     return launched();
