@@ -18,7 +18,8 @@
 namespace {
 
 constexpr int kAdamBlock = 256;                            // elements that share a scale
-constexpr int kRuns = 4, kChunk = 256 * 8 * kRuns;         // runs of eight elements of a lane; elements of a workgroup
+constexpr int kRound = 256 * 8;                            // elements of a workgroup's round: a run of eight to a lane
+constexpr int kRounds = 4;                                 // of a workgroup, where there are many
 constexpr int kRecords = 56;                               // of a launch: its arguments are 4 KiB at most
 constexpr float kTop = 448.f, kNone = 0x1p-100f;           // e4m3's largest number; a block whose largest is less is stored as zeros
 
@@ -36,6 +37,7 @@ struct AdamArgs {
     AdamTensor t[kRecords];
     int first[kRecords];                                   // each tensor's first workgroup
     int count, number;                                     // tensors of this launch; number of the first one in the call
+    int rounds;                                            // of a workgroup
     double b1, b2, log_b1, log_b2;                         // logarithms: where the step's number is on the device
     double unbias1;                                        // 1 / (1 - b1^t)
     float unbias2, eps;                                    // 1 / sqrt(1 - b2^t)
@@ -130,7 +132,7 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
     const int before = lane < a.count ? a.first[lane] : 0x7fffffff;
     const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before <= (int)blockIdx.x)) - 1;
     const AdamTensor &t = a.t[at];
-    const long long n = t.n, chunk = (long long)((int)blockIdx.x - a.first[at]) * kChunk;
+    const long long n = t.n, begin = (long long)((int)blockIdx.x - a.first[at]) * a.rounds * kRound + (int)threadIdx.x * 8;
     double by = 1.0, lr = (double)t.lr, unbias1 = a.unbias1;
     float decay = t.decay, unbias2 = a.unbias2;
     long long step = a.step;
@@ -150,20 +152,37 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
     }
     const float rate = (float)(lr * unbias1);
     const double c1 = 1.0 - a.b1, c2 = 1.0 - a.b2;
+    // (the next round's numbers are asked for before the present ones are dealt with)
+    Raw8<float> p_next;
+    Raw8<T> g_next;
+    Raw8<S> m_next, v_next;
+    float2 s_next;
+    auto load = [&](long long i) {
+        const long long left = n - i;
+        p_next = take(t.p + i, left);
+        g_next = take((const T *)t.g + i, left);
+        m_next = take((const S *)t.m + i, left);
+        v_next = take((const S *)t.v + i, left);
+        if (EIGHT && i - (i & (kAdamBlock - 1)) < n)
+            s_next = t.scales[i / kAdamBlock];
+    };
+    load(begin);
 #pragma unroll 1
-    for (int run = 0; run < kRuns; ++run) {
-        const long long i = chunk + run * 2048 + (int)threadIdx.x * 8, left = n - i;
+    for (int round = 0; round < a.rounds; ++round) {
+        const long long i = begin + round * kRound, left = n - i;
         if (i - (i & (kAdamBlock - 1)) >= n)               // (all lanes of a block or none, for the exchanges between them)
             break;
-        const Raw8<float> p = take(t.p + i, left);
-        const Raw8<T> grad = take((const T *)t.g + i, left);
-        const Raw8<S> m0 = take((const S *)t.m + i, left), v0 = take((const S *)t.v + i, left);
+        const Raw8<float> p = p_next;
+        const Raw8<T> grad = g_next;
+        const Raw8<S> m0 = m_next, v0 = v_next;
+        const float2 s = s_next;
+        if (round + 1 < a.rounds)
+            load(i + kRound);
         float m[8], r[8], v[8];
         double sm = 1.0, sr = 1.0;
         if constexpr (EIGHT) {
             from_8_bits(m0, m);
             from_8_bits(v0, v);
-            const float2 s = t.scales[i / kAdamBlock];
             sm = (double)s.x;
             sr = (double)s.y;
         } else {
@@ -294,13 +313,17 @@ extern "C" int dcnv4_adamw(const dcnv4_adamw_tensor *tensors, int count, double 
     a.more = (const long long *)step_on_device;
     a.factors = (const float *)factors_on_device;
     for (int from = 0; from < count;) {
-        long long groups = 0;
+        long long groups = 0, elements = 0;
         a.count = 0;
         a.number = from;
+        // many rounds to a workgroup where that leaves every unit eight of them, else one after the other would only take longer
+        for (int i = from; i < count && i < from + kRecords; ++i)
+            elements += tensors[i].n;
+        a.rounds = elements >= 2048LL * kRounds * kRound ? kRounds : 1;
         for (; from < count && a.count < kRecords; ++from) {
             const dcnv4_adamw_tensor &t = tensors[from];
-            const long long more = (t.n + kChunk - 1) / kChunk;
-            if (groups + more >= 1 << 24)                  // (a tensor has 2^23 at most)
+            const long long more = (t.n + a.rounds * kRound - 1) / (a.rounds * kRound);
+            if (groups + more >= 1 << 24)                  // (a tensor has 2^23 at most: those past 2^24 elements have kRounds)
                 break;
             a.first[a.count] = (int)groups;
             a.t[a.count++] = {t.n, t.param, t.grad, t.m, t.v, (float2 *)t.scales, (_Float16 *)t.copy, (float)t.lr, (float)(t.lr * t.weight_decay)};

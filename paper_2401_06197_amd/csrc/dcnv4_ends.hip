@@ -334,7 +334,7 @@ __global__ __launch_bounds__(end_threads(L)) void dcnv4_end_backward_kernel(EndB
 
 struct EndJoin {
     const float *partial, *row_sums;                       // row_sums: null for no gradient of the gates
-    int groups, C, planes, k1;                             // k1: planes of the branch
+    int groups, C;
     const void *gamma1, *beta1, *scale;
     void *grad_scale, *grad_gamma1, *grad_beta1, *grad_gamma2, *grad_beta2;    // null: not asked for
     float *grad_gate;
@@ -343,18 +343,19 @@ struct EndJoin {
 };
 
 // Adds up the workgroups' sums (16 channels to a workgroup here, 64 of the rows side by side) and an image's row sums.
-template <typename T> __global__ __launch_bounds__(1024) void dcnv4_end_join_kernel(EndJoin j)
+template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024) void dcnv4_end_join_kernel(EndJoin j)
 {
-    __shared__ float part[4][16][16];
+    constexpr int K1 = FIRST ? 2 : 1, K = K1 + (SECOND ? 2 : 0);
+    __shared__ float part[K][16][16];
     const int in = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4;
     if ((int)blockIdx.x >= j.columns) {
-        const int image = (int)blockIdx.x - j.columns;
-        const float *from = j.row_sums + image * j.rows;
+        const int image = (int)blockIdx.x - j.columns;        // (rows are counted in 31 bits)
+        const float *from = j.row_sums + (long long)image * j.rows;
         // (in 64 bits: an image's rows may be millions of numbers that cancel)
         __shared__ double waves[16];
         double s = 0.;
-#pragma unroll 8
-        for (long long r = (int)threadIdx.x; r < j.rows; r += 1024)
+#pragma unroll 16
+        for (int r = (int)threadIdx.x; r < j.rows; r += 1024)
             s += (double)from[r];
 #pragma unroll
         for (int d = 1; d < 64; d *= 2)
@@ -372,16 +373,18 @@ template <typename T> __global__ __launch_bounds__(1024) void dcnv4_end_join_ker
         return;
     }
     const int col = (int)blockIdx.x * 16 + in;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float s[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        s[k] = 0.f;
     if (col < j.C)
-#pragma unroll 4
+#pragma unroll 8
         for (int r = slice; r < j.groups; r += 64)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k < j.planes)
-                    s[k] += j.partial[((long long)r * j.planes + k) * j.C + col];
+            for (int k = 0; k < K; ++k)
+                s[k] += j.partial[((long long)r * K + k) * j.C + col];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < K; ++k) {
         s[k] = add_halves(add_rows(s[k]));
         if ((threadIdx.x & 63) < 16)
             part[k][threadIdx.x >> 6][in] = s[k];
@@ -390,7 +393,7 @@ template <typename T> __global__ __launch_bounds__(1024) void dcnv4_end_join_ker
     if (threadIdx.x >= 16 || col >= j.C)
         return;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < K; ++k) {
         s[k] = 0.f;
 #pragma unroll
         for (int w = 0; w < 16; ++w)
@@ -401,17 +404,17 @@ template <typename T> __global__ __launch_bounds__(1024) void dcnv4_end_join_ker
         if (p != nullptr)
             ((T *)p)[col] = (T)v;
     };
-    if (j.k1 == 2) {
+    if constexpr (FIRST) {
         const float scale = vector(j.scale, 1.f);
         store(j.grad_scale, __builtin_fmaf(vector(j.gamma1, 1.f), s[0], vector(j.beta1, 0.f) * s[1]));
         store(j.grad_gamma1, scale * s[0]);
         store(j.grad_beta1, scale * s[1]);
-        store(j.grad_gamma2, s[2]);
-        store(j.grad_beta2, s[3]);
     } else {
         store(j.grad_scale, s[0]);
-        store(j.grad_gamma2, s[1]);
-        store(j.grad_beta2, s[2]);
+    }
+    if constexpr (SECOND) {
+        store(j.grad_gamma2, s[K1]);
+        store(j.grad_beta2, s[K1 + 1]);
     }
 }
 
@@ -468,7 +471,7 @@ template <typename T, bool FIRST, bool SECOND> int launch_end(const EndArgs &a, 
     });
 }
 
-template <typename T, bool FIRST, bool SECOND> int launch_end_backward(const EndBackArgs &a, int groups, EndJoin &j, hipStream_t s)
+template <typename T, bool FIRST, bool SECOND> int launch_end_backward(const EndBackArgs &a, int groups, const EndJoin &j, hipStream_t s)
 {
     const int rc = by_lanes(a.C, [&](auto L) {
         constexpr int threads = end_threads(L());
@@ -481,9 +484,7 @@ template <typename T, bool FIRST, bool SECOND> int launch_end_backward(const End
     const long long images = a.row_sums != nullptr ? a.P / j.rows : 0;
     if (rc || j.columns + images == 0)
         return rc;
-    j.k1 = FIRST ? 2 : 1;
-    j.planes = j.k1 + (SECOND ? 2 : 0);
-    hipLaunchKernelGGL((dcnv4_end_join_kernel<T>), dim3((unsigned)(j.columns + images)), dim3(1024), 0, s, j);
+    hipLaunchKernelGGL((dcnv4_end_join_kernel<T, FIRST, SECOND>), dim3((unsigned)(j.columns + images)), dim3(1024), 0, s, j);
     return hipGetLastError() == hipSuccess ? DCNV4_OK : DCNV4_ERR_LAUNCH;
 }
 
@@ -571,7 +572,7 @@ int dcnv4_norm_scale_add_norm_backward(const void *x, const void *z, const void 
                      sums ? partial : nullptr, grad_gate ? rows : nullptr, P, {}, C, 1.f / (float)C};
     if (gates > 0)
         a.rows = make_div((unsigned)(P / gates));
-    EndJoin j = {partial, rows, groups, C, 0, 0, gamma1, beta1, scale, grad_scale, grad_gamma1, grad_beta1, grad_gamma2, grad_beta2, grad_gate,
+    const EndJoin j = {partial, rows, groups, C, gamma1, beta1, scale, grad_scale, grad_gamma1, grad_beta1, grad_gamma2, grad_beta2, grad_gate,
                  sums ? (C + 15) / 16 : 0, gates > 0 ? P / gates : P};
     return by_form(norms, dtype, [&](auto t, auto one, auto two) {
         return launch_end_backward<decltype(t), decltype(one)::value, decltype(two)::value>(a, groups, j, (hipStream_t)stream);

@@ -246,3 +246,33 @@ def test_refusals_of_the_plan():
             dcn.dcnv4_adamw_step(plan, **kw)
     with pytest.raises(ValueError):
         dcn.dcnv4_adamw_step(plan, 1, factors_on_device=torch.ones(1, device="cuda"))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_large_tensors_take_several_rounds(bits):
+    """Past 2^24 elements a workgroup deals with several rounds of them; a part by itself, with one, gives the same bits."""
+    n, part = 2 ** 24 + 100003, 2 ** 20 + 256
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda size: torch.randn(n, device="cuda", generator=gen) * size
+    p, g, m, v = r(0.1), r(0.02).half(), r(0.01), r(0.01) ** 2
+    scales = None
+    if bits == 8:
+        m, v = (t.clamp(-1, 1).to(torch.float8_e4m3fn) for t in (m, v))
+        scales = [torch.rand((-(-n // 256), 2), device="cuda", generator=gen) * 0.1]
+        scales.append(scales[0].clone())
+    # of the beginning (whose elements have the same numbers in both), and without states of 8 bits of the end
+    cuts = [slice(0, part)] + ([slice(n - part - 3, n)] if bits == 32 else [])
+    alone = [[t[c].clone() for t in (p, g, m, v)] for c in cuts]
+    few = part // 256
+    small = dcn.dcnv4_adamw_plan(*map(list, zip(*alone)), 1e-2, 0.1, scales=None if bits == 32 else [scales[1][:few].clone()])
+    large = dcn.dcnv4_adamw_plan([p], [g], [m], [v], 1e-2, 0.1, scales=None if bits == 32 else [scales[0]])
+    for t in (1, 2):
+        dcn.dcnv4_adamw_step(large, t, seed=5)
+        dcn.dcnv4_adamw_step(small, t, seed=5)
+    torch.cuda.synchronize()
+    for c, (ap, _, am, av) in zip(cuts, alone):
+        for a, b in ((ap, p[c]), (am, m[c]), (av, v[c])):
+            assert torch.equal(a.view(torch.uint8), b.contiguous().view(torch.uint8))
+    if bits == 8:
+        assert torch.equal(small.held[4][0], scales[0][:few])
+    assert bool(torch.isfinite(p).all())
