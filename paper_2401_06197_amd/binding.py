@@ -812,9 +812,9 @@ def dcnv4_norm_scale_add_norm_workspace_bytes(P, C, gates):
     return int(load_library().dcnv4_norm_scale_add_norm_workspace_bytes(P, C, gates))
 
 
-def _end_args(x, scale, gate, first, second):
-    """(P, C, gates, norms, gamma1, beta1, gamma2, beta2) of a block's end, checked."""
-    import torch
+def _end_args(x, scale, gate, first, second, rows):
+    """(P, C, gates, norms, gamma1, beta1, gamma2, beta2) of a block's end, checked; rows: (name, tensor of x's shape or None)."""
+    shape = x.shape
     P, C = _rows(x)
     norms, gamma1, beta1, gamma2, beta2, gates = 0, None, None, None, None, 0
     if first is not None:
@@ -822,11 +822,13 @@ def _end_args(x, scale, gate, first, second):
     if second is not None:
         norms, (gamma2, beta2) = norms | SECOND_NORM, second
     vector = (C,)
-    _check_like(x, (("scale", scale, vector), ("gamma1", gamma1, vector), ("beta1", beta1, vector), ("gamma2", gamma2, vector), ("beta2", beta2, vector)))
+    _check_like(x, (("scale", scale, vector), ("gamma1", gamma1, vector), ("beta1", beta1, vector), ("gamma2", gamma2, vector), ("beta2", beta2, vector),
+                    *[(name, t, shape) for name, t in rows]))
     if gate is not None:
-        if len(x.shape) < 2:
+        import torch
+        if len(shape) < 2:
             raise ValueError("dcnv4: expected x [N, ..., C] with gate [N]")
-        gates = x.shape[0]
+        gates = shape[0]
         _check_plain("gate", gate, x.get_device(), (gates,), torch.float32)
     return P, C, gates, norms, gamma1, beta1, gamma2, beta2
 
@@ -841,16 +843,14 @@ def dcnv4_norm_scale_add_norm(x, residual, scale=None, gate=None, first=None, se
     layer norm's (gamma, beta), each of which may be None.  scale [C]; gate [N] float32, one for each image.  y and the statistics of
     norms that there are not are None; without `stats` all of these (and not in `out` either)."""
     import torch
-    P, C, gates, norms, gamma1, beta1, gamma2, beta2 = _end_args(x, scale, gate, first, second)
+    P, C, gates, norms, gamma1, beta1, gamma2, beta2 = _end_args(x, scale, gate, first, second, (("residual", residual),))
     shape, dt, f32 = x.shape, x.dtype, torch.float32
-    _check_like(x, (("residual", residual, shape),))
-    stat = shape[:-1]
+    stat = shape[:-1] if stats else None
     one, two = stats and first is not None, stats and second is not None
     z, y, mean1, rstd1, mean2, rstd2 = results = _outputs(x, out, (
         ("z", shape, dt), None if second is None else ("y", shape, dt), ("mean1", stat, f32) if one else None, ("rstd1", stat, f32) if one else None,
         ("mean2", stat, f32) if two else None, ("rstd2", stat, f32) if two else None), stream)
-    args = (x.data_ptr(), residual.data_ptr(), _ptr(gamma1), _ptr(beta1), _ptr(scale), _ptr(gate), _ptr(gamma2), _ptr(beta2), z.data_ptr(), _ptr(y),
-            _ptr(mean1), _ptr(rstd1), _ptr(mean2), _ptr(rstd2), P, C, gates, norms, float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
+    args = (*[None if t is None else t.data_ptr() for t in (x, residual, gamma1, beta1, scale, gate, gamma2, beta2, z, y, mean1, rstd1, mean2, rstd2)], P, C, gates, norms, float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return _prepared(args, out)
     _call(x.device, "dcnv4_norm_scale_add_norm", args)
@@ -863,22 +863,21 @@ def dcnv4_norm_scale_add_norm_backward(x, z, scale, gate, first, second, stats, 
     stats = (mean1, rstd1, mean2, rstd2).  grad_y is None without a second norm, where grad_residual is grad_z itself (in `out`: None).
     Gradients of what is None are None; so is the gates' with grad_gate=False."""
     import torch
-    P, C, gates, norms, gamma1, beta1, gamma2, beta2 = _end_args(x, scale, gate, first, second)
-    shape, dt, at, f32, vector = x.shape, x.dtype, x.get_device(), torch.float32, (C,)
-    mean1, rstd1, mean2, rstd2 = stats
     if second is None:
         if grad_y is not None or grad_z is None:
             raise ValueError("dcnv4: without a second norm there is grad_z, and no grad_y")
         z = None
-    else:
-        if grad_y is None or z is None:
-            raise ValueError("dcnv4: a second norm's backward pass takes z and grad_y")
+    elif grad_y is None or z is None:
+        raise ValueError("dcnv4: a second norm's backward pass takes z and grad_y")
+    P, C, gates, norms, gamma1, beta1, gamma2, beta2 = _end_args(x, scale, gate, first, second, (("z", z), ("grad_y", grad_y), ("grad_z", grad_z)))
+    shape, dt, at, f32, vector = x.shape, x.dtype, x.get_device(), torch.float32, (C,)
+    mean1, rstd1, mean2, rstd2 = stats
+    if second is not None:
         _check_plain("mean2", mean2, at, shape[:-1], f32)
         _check_plain("rstd2", rstd2, at, shape[:-1], f32)
     if first is not None:
         _check_plain("mean1", mean1, at, shape[:-1], f32)
         _check_plain("rstd1", rstd1, at, shape[:-1], f32)
-    _check_like(x, (("z", z, shape), ("grad_y", grad_y, shape), ("grad_z", grad_z, shape)))
     of = lambda name, t: None if t is None else (name, vector, dt)
     specs = (("grad_x", shape, dt), None if second is None else ("grad_residual", shape, dt), of("grad_scale", scale),
              ("grad_gate", (gates,), f32) if gate is not None and grad_gate else None, of("grad_gamma1", gamma1), of("grad_beta1", beta1),
@@ -887,8 +886,8 @@ def dcnv4_norm_scale_add_norm_backward(x, z, scale, gate, first, second, stats, 
     space, size = None, 0
     if any(s is not None for s in specs[2:]):
         space, size = _workspace(x, workspace, dcnv4_norm_scale_add_norm_workspace_bytes(P, C, gates) if workspace is None else 0, stream)
-    args = (x.data_ptr(), _ptr(z), _ptr(gamma1), _ptr(beta1), _ptr(scale), _ptr(gate), _ptr(gamma2), _ptr(mean1), _ptr(rstd1), _ptr(mean2), _ptr(rstd2),
-            _ptr(grad_y), _ptr(grad_z), *map(_ptr, results), _ptr(space), size, P, C, gates, norms, _dtype_code(x), _stream_ptr(stream, x.device))
+    args = (*[None if t is None else t.data_ptr() for t in (x, z, gamma1, beta1, scale, gate, gamma2, mean1, rstd1, mean2, rstd2, grad_y, grad_z,
+                                                            *results, space)], size, P, C, gates, norms, _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return _prepared(args, out, *(() if space is None else (workspace,)))
     _call(x.device, "dcnv4_norm_scale_add_norm_backward", args)

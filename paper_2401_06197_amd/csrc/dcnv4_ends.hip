@@ -342,14 +342,14 @@ struct EndJoin {
     long long rows;                                        // of an image
 };
 
-// Adds up the workgroups' sums (16 channels to a workgroup here, 64 of the rows side by side) and an image's row sums.
+// Adds up the workgroups' sums (16 channels to a workgroup here, of the branch or of the second norm; 64 of the rows side by side) and an image's row sums.
 template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024) void dcnv4_end_join_kernel(EndJoin j)
 {
     constexpr int K1 = FIRST ? 2 : 1, K = K1 + (SECOND ? 2 : 0);
-    __shared__ float part[K][16][16];
-    const int in = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4;
-    if ((int)blockIdx.x >= j.columns) {
-        const int image = (int)blockIdx.x - j.columns;        // (rows are counted in 31 bits)
+    __shared__ float part[2][16][16];
+    const int in = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4, all = SECOND ? 2 * j.columns : j.columns;
+    if ((int)blockIdx.x >= all) {
+        const int image = (int)blockIdx.x - all;        // (rows are counted in 31 bits)
         const float *from = j.row_sums + (long long)image * j.rows;
         // (in 64 bits: an image's rows may be millions of numbers that cancel)
         __shared__ double waves[16];
@@ -372,19 +372,17 @@ template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024
         }
         return;
     }
-    const int col = (int)blockIdx.x * 16 + in;
-    float s[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-        s[k] = 0.f;
+    const bool second = SECOND && (int)blockIdx.x >= j.columns;
+    const int col = ((int)blockIdx.x - (second ? j.columns : 0)) * 16 + in, k0 = second ? K1 : 0;
+    float s[2] = {0.f, 0.f};                               // (one sum of a branch without a norm, and whatever follows it, which nothing takes)
     if (col < j.C)
 #pragma unroll 8
         for (int r = slice; r < j.groups; r += 64)
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                s[k] += j.partial[((long long)r * K + k) * j.C + col];
+            for (int k = 0; k < (FIRST || SECOND ? 2 : 1); ++k)
+                s[k] += j.partial[((long long)r * K + k0 + k) * j.C + col];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < 2; ++k) {
         s[k] = add_halves(add_rows(s[k]));
         if ((threadIdx.x & 63) < 16)
             part[k][threadIdx.x >> 6][in] = s[k];
@@ -393,7 +391,7 @@ template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024
     if (threadIdx.x >= 16 || col >= j.C)
         return;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < 2; ++k) {
         s[k] = 0.f;
 #pragma unroll
         for (int w = 0; w < 16; ++w)
@@ -404,17 +402,16 @@ template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024
         if (p != nullptr)
             ((T *)p)[col] = (T)v;
     };
-    if constexpr (FIRST) {
+    if (second) {
+        store(j.grad_gamma2, s[0]);
+        store(j.grad_beta2, s[1]);
+    } else if constexpr (FIRST) {
         const float scale = vector(j.scale, 1.f);
         store(j.grad_scale, __builtin_fmaf(vector(j.gamma1, 1.f), s[0], vector(j.beta1, 0.f) * s[1]));
         store(j.grad_gamma1, scale * s[0]);
         store(j.grad_beta1, scale * s[1]);
     } else {
         store(j.grad_scale, s[0]);
-    }
-    if constexpr (SECOND) {
-        store(j.grad_gamma2, s[K1]);
-        store(j.grad_beta2, s[K1 + 1]);
     }
 }
 
@@ -484,7 +481,7 @@ template <typename T, bool FIRST, bool SECOND> int launch_end_backward(const End
     const long long images = a.row_sums != nullptr ? a.P / j.rows : 0;
     if (rc || j.columns + images == 0)
         return rc;
-    hipLaunchKernelGGL((dcnv4_end_join_kernel<T, FIRST, SECOND>), dim3((unsigned)(j.columns + images)), dim3(1024), 0, s, j);
+    hipLaunchKernelGGL((dcnv4_end_join_kernel<T, FIRST, SECOND>), dim3((unsigned)((SECOND ? 2 : 1) * j.columns + images)), dim3(1024), 0, s, j);
     return hipGetLastError() == hipSuccess ? DCNV4_OK : DCNV4_ERR_LAUNCH;
 }
 
