@@ -117,7 +117,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES, false, false, true> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt, split;
-    if (!tile_of(q, at, bt, split))
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
@@ -162,8 +162,8 @@ struct Deltas {
     const void *grad_h;
     unsigned short *d;                                     // [P][PL planes][2F]
     float *bias_sums;                                      // [pixel runs of 32 * WN][2F], or null
-    const float *most;                                     // fp16: largest |grad_h| of `parts` parts
-    int parts;
+    const float *most;                                     // fp16: largest |grad_h| of `parts` parts; no parts: grad_h has `few` numbers
+    int parts, few;
     Scale *scale;                                          // fp16: what undoes d's factor
 };
 
@@ -185,42 +185,55 @@ struct Result {
 
 }  // namespace
 
+namespace {
+
+// The largest finite magnitude of a lane's fp16 numbers.
+struct Most {
+    typedef unsigned short eight __attribute__((ext_vector_type(8)));
+    eight top = {};
+    __device__ __forceinline__ void add(eight v)
+    {
+        v &= (unsigned short)0x7fff;                       // (fp16's bits without the sign are in the numbers' order)
+        top = __builtin_elementwise_max(top, v < (unsigned short)0x7c00 ? v : eight{});
+    }
+    __device__ __forceinline__ float value() const
+    {
+        int v = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v = max(v, (int)top[e]);
+        return (float)__builtin_bit_cast(_Float16, (unsigned short)v);
+    }
+};
+
+}  // namespace
+
 // The largest finite |grad_h| of a workgroup's part of n numbers (a multiple of eight).
 __global__ __launch_bounds__(256) void dcnv4_gated_most_kernel(const unsigned short *g, long long n, float *most)
 {
-    typedef unsigned short us8 __attribute__((ext_vector_type(8)));
-    __shared__ unsigned short part[4];
-    us8 top = {};
-    auto add = [&](us8 v) {
-        v &= (unsigned short)0x7fff;                       // (fp16's bits without the sign are in the numbers' order)
-        top = __builtin_elementwise_max(top, v < (unsigned short)0x7c00 ? v : us8{});
-    };
+    __shared__ float part[4];
+    Most top;
     const long long units = n / 8, stride = (long long)gridDim.x * 256;
-    const us8 *p = reinterpret_cast<const us8 *>(g);
+    const Most::eight *p = reinterpret_cast<const Most::eight *>(g);
     long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x;
     for (; i + 3 * stride < units; i += 4 * stride) {
-        const us8 a = p[i], b = p[i + stride], c = p[i + 2 * stride], d = p[i + 3 * stride];
-        add(a);
-        add(b);
-        add(c);
-        add(d);
+        const Most::eight a = p[i], b = p[i + stride], c = p[i + 2 * stride], d = p[i + 3 * stride];
+        top.add(a);
+        top.add(b);
+        top.add(c);
+        top.add(d);
     }
     for (; i < units; i += stride)
-        add(p[i]);
-    int v = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        v = max(v, (int)top[e]);
+        top.add(p[i]);
+    float v = top.value();
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)
-        v = max(v, __shfl_xor(v, d));
+        v = fmaxf(v, __shfl_xor(v, d));
     if ((threadIdx.x & 63) == 0)
-        part[threadIdx.x >> 6] = (unsigned short)v;
+        part[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        v = max(max((int)part[0], (int)part[1]), max((int)part[2], (int)part[3]));
-        most[blockIdx.x] = (float)__builtin_bit_cast(_Float16, (unsigned short)v);
-    }
+    if (threadIdx.x == 0)
+        most[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
 // The tile again, and d out of it.
@@ -230,17 +243,23 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES, false, false, true> G;
     typedef T four __attribute__((ext_vector_type(4)));
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
-    __shared__ float tops[G::kWaves];
     int at, bt, split;
-    if (!tile_of(q, at, bt, split))
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
     const int first = at * (G::BM / 2) + wr * 16 * WM, px0 = bt * G::BN + wc * 32 * WN;
     float top = 0.f;                                       // (asked for here, joined after the products)
-    if constexpr (PL == 1)
+    if constexpr (PL == 1) {
         for (int i = (int)threadIdx.x; i < d.parts; i += G::kThreads)
             top = fmaxf(top, d.most[i]);
+        if (d.parts == 0) {                                // few numbers: all of them, a launch less
+            Most most;
+            for (int i = (int)threadIdx.x; i < d.few / 8; i += G::kThreads)
+                most.add(reinterpret_cast<const Most::eight *>(d.grad_h)[i]);
+            top = most.value();
+        }
+    }
     f32x16 acc[WM][WN];
     start_with_bias<T, WM, WN>(l, first, kb, acc);
     G::multiply(smem, q.a, q.b, at * (G::BM / 2), bt * G::BN, 0, q.steps, acc);
@@ -262,12 +281,15 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
 #pragma unroll
         for (int s = 1; s < 64; s *= 2)
             top = fmaxf(top, __shfl_xor(top, s));
+        // (the products are through with the LDS.  An object of its own: every LDS read of the loop would wait for all loads)
+        float *tops = reinterpret_cast<float *>(smem);
         if (lane == 0)
             tops[wave] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < G::kWaves; ++w)
             top = fmaxf(top, tops[w]);
+        __syncthreads();                                   // (results go there)
         const int e = top > 0.f ? 2 - __builtin_amdgcn_frexp_expf(top) : 0;
         up = ldexpf(1.f, e);
         down = ldexpf(1.f, -e);
@@ -343,33 +365,16 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     }
 }
 
-// out[j][i] = scale * sum_r A[i][r] * B[j][r], whole (T) or a split of the sum (float planes).  A turned; B turned in the product over pixels (grad_w).
-template <typename T, bool WHOLE, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_layer_product_kernel(Product q, Result o)
+// out[j][i] = scale * sum_r A[i][r] * B[j][r] of a tile, whole (T) or a split of the sum (float planes).  A turned; B turned in the product over
+// pixels (grad_w).
+template <typename G, typename S, int WR, int WC, int WM, int WN>
+__device__ __forceinline__ void store_tile(char *smem, const Product &q, S *to, float by, int at, int bt, f32x16 (&acc)[WM][WN])
 {
-    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
-    typedef std::conditional_t<WHOLE, T, float> S;
-    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
-    int at, bt, split;
-    if (!tile_of(q, at, bt, split))
-        return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
-    f32x16 acc[WM][WN];
-#pragma unroll
-    for (int m = 0; m < WM; ++m)
-#pragma unroll
-        for (int n = 0; n < WN; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                acc[m][n][r] = 0.f;
-    const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
-    G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
-    const float by = WHOLE && o.scale != nullptr ? o.scale->by : 1.f;
     char *out = smem + wave * (G::OUT / G::kWaves);
     const int i0 = at * G::BM + wr * 32 * WM, j0 = bt * G::BN + wc * 32 * WN;
     constexpr int ES = (int)sizeof(S), ROW = 32 * WM * ES + 16, UNITS = 32 * WM * ES / 16;
-    S *to = (S *)o.out + (WHOLE ? 0 : (long long)split * o.plane);
 #pragma unroll
     for (int n = 0; n < WN; ++n) {
 #pragma unroll
@@ -382,6 +387,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
                     s[c] = (S)(acc[m][n][4 * a + c] * by);
                 __builtin_memcpy(out + row * ROW + (32 * m + 8 * a + 4 * kb) * ES, s, sizeof(s));
             }
+        // (the same wave wrote and reads)
 #pragma unroll
         for (int it = 0; it < UNITS / 2; ++it) {
             const int e = it * 64 + lane, u = e % UNITS, r = e / UNITS, j = j0 + n * 32 + r, i = i0 + u * (16 / ES);
@@ -392,29 +398,76 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     }
 }
 
-// Adds up the splits' planes [splits][n] and rounds: four numbers a lane.  The first workgroups make grad_b, where that saves it a launch.
-template <typename T>
-__global__ __launch_bounds__(256) void dcnv4_layer_sum_kernel(const float *planes, int splits, long long n, Result o, Bias b)
+// grad_x, or grad_w (PIXELS); `b`: with the last product of a layer, grad_b, by workgroups of its own behind it.
+template <typename T, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_layer_product_kernel(Product q, Result o, Bias b)
 {
-    if ((int)blockIdx.x < b.blocks) {
-        bias_of<T>(b, (int)blockIdx.x);
+    typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
+    int at, bt, split;
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split)) {
+        if ((int)blockIdx.x >= q.per_xcd * kXcds)
+            bias_of<T>(b, (int)blockIdx.x - q.per_xcd * kXcds, reinterpret_cast<float(*)[17]>(smem));
         return;
     }
-    const int block = (int)blockIdx.x - b.blocks, blocks = (int)gridDim.x - b.blocks;
-    const float by = o.scale != nullptr ? o.scale->by : 1.f;
-    for (long long i = (long long)block * 256 + (int)threadIdx.x; i < n / 4; i += (long long)blocks * 256) {
-        f32x4 v = *reinterpret_cast<const f32x4 *>(planes + i * 4);
+    f32x16 acc[WM][WN];
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+        for (int n = 0; n < WN; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[m][n][r] = 0.f;
+    const int t0 = split * q.steps_per_split, t1 = min(t0 + q.steps_per_split, q.steps);
+    G::multiply(smem, q.a, q.b, at * G::BM, bt * G::BN, t0, t1, acc);
+    if (o.plane > 0)
+        store_tile<G, float, WR, WC, WM, WN>(smem, q, (float *)o.out + (long long)split * o.plane, 1.f, at, bt, acc);
+    else
+        store_tile<G, T, WR, WC, WM, WN>(smem, q, (T *)o.out, o.scale != nullptr ? o.scale->by : 1.f, at, bt, acc);
+}
+
+namespace {
+
+struct Sum {
+    const float *planes;                                   // [splits][n]
+    int splits, blocks;                                    // blocks: workgroups, none for no sum
+    long long n;
+    Result o;
+};
+
+}  // namespace
+
+// Adds up the splits' planes of both gradients and rounds: four numbers a lane.  The last workgroups make grad_b.
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_sum_kernel(Sum x, Sum w, Bias b)
+{
+    __shared__ float part[16][17];
+    int block = (int)blockIdx.x;
+    if (block >= x.blocks + w.blocks) {
+        bias_of<T>(b, block - x.blocks - w.blocks, part);
+        return;
+    }
+    const bool second = block >= x.blocks;
+    const Sum &q = second ? w : x;
+    block -= second ? x.blocks : 0;
+    const float by = q.o.scale != nullptr ? q.o.scale->by : 1.f;
+    const long long n = q.n;
+    for (long long i = (long long)block * 256 + (int)threadIdx.x; i < n / 4; i += (long long)q.blocks * 256) {
+        f32x4 v = *reinterpret_cast<const f32x4 *>(q.planes + i * 4);
 #pragma unroll 8
-        for (int s = 1; s < splits; ++s)
-            v += *reinterpret_cast<const f32x4 *>(planes + s * n + i * 4);
+        for (int s = 1; s < q.splits; ++s)
+            v += *reinterpret_cast<const f32x4 *>(q.planes + s * n + i * 4);
         T t[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             t[e] = (T)(v[e] * by);
-        __builtin_memcpy(__builtin_assume_aligned((T *)o.out + i * 4, 4 * sizeof(T)), t, sizeof(t));
+        __builtin_memcpy(__builtin_assume_aligned((T *)q.o.out + i * 4, 4 * sizeof(T)), t, sizeof(t));
     }
 }
-template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_bias_kernel(Bias b) { bias_of<T>(b, (int)blockIdx.x); }
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_bias_kernel(Bias b)
+{
+    __shared__ float part[16][17];
+    bias_of<T>(b, (int)blockIdx.x, part);
+}
 
 namespace {
 
@@ -502,6 +555,7 @@ struct LayerOptions {
 } g_layers;
 
 // One more limit than the products': byte offsets inside a gated layer's weights are 32 bits (fp32: of three planes of 16 bits).
+constexpr int kFewNumbers = 1 << 15;                       // of grad_h, which every workgroup looks through by itself
 constexpr int kLayerMaxRows = 1 << 24, kLayerMaxWidth = 1 << 20;
 
 bool fits(int pl, const Choice &c, long long m, long long n)
@@ -602,9 +656,9 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
         p.w_split = room.take((long long)p.N * 6 * p.kp);
     }
     if (backward) {
-        p.most_parts = (int)(P * F / 8 / 1024 < 512 ? P * F / 8 / 1024 + 1 : 512);
+        p.most_parts = P * F <= kFewNumbers ? 0 : (int)(P * F / 8 / 1024 < 512 ? P * F / 8 / 1024 + 1 : 512);
         p.scale = room.take(sizeof(Scale));
-        p.most = room.take(p.most_parts * 4);
+        p.most = room.take((p.most_parts + 1) * 4);
         p.d = room.take(P * p.pl * p.N * 2);
         p.bias_sums = room.take(round_up(P, 256) / 32 * p.N * 4);
         if (!plan_gradients(p, room))
@@ -662,50 +716,39 @@ template <typename T> void launch_ahead(const Ahead &q, hipStream_t s)
         hipLaunchKernelGGL((dcnv4_layer_ahead_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, q);
 }
 
-template <typename T, int PL, bool PIXELS> void launch_product(const Product &q, const Choice &c, const Result &o, hipStream_t s)
-{
-    with_tile<PL>(c.shape, [&](auto t) {
-        typedef decltype(t) G;
-        const dim3 grid((unsigned)(q.per_xcd * kXcds)), block(G::WR * G::WC * 64);
-        if (c.splits > 1)
-            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, false, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
-        else
-            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, true, PIXELS, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), grid, block, 0, s, q, o);
-        return 0;
-    });
-}
-
-template <typename T> void sum_planes(const void *planes, int splits, long long n, const Result &o, const Bias &b, hipStream_t s)
-{
-    const long long groups = (n / 4 + 255) / 256;
-    hipLaunchKernelGGL((dcnv4_layer_sum_kernel<T>), dim3((unsigned)((groups < 8192 ? groups : 8192) + b.blocks)), dim3(256), 0, s, (const float *)planes,
-                       splits, n, o, b);
-}
-
 // grad_x, grad_w and, out of the runs' sums, grad_b (each may be null) of a layer with rows w [N][K], x [P][K], d [P][N] as operands.
 template <typename T, int PL>
 void gradients(const LayerPlan &p, const Operand &x, const Operand &w, const Operand &d, const Scale *scale, Bias b, void *grad_x, void *grad_w, char *ws,
                hipStream_t s)
 {
-    if (grad_x) {
-        const Result o = {grad_x, 0, scale};
-        const Product q = product_of(turned(w), d, PL, p.gx);
-        const Result planes = {ws + p.gx_at, (long long)p.P * p.K, nullptr};
-        launch_product<T, PL, false>(q, p.gx, p.gx.splits > 1 ? planes : o, s);
-        if (p.gx.splits > 1)
-            sum_planes<T>(ws + p.gx_at, p.gx.splits, planes.plane, o, Bias{}, s);
-    }
-    if (grad_w) {
-        const Result o = {grad_w, 0, scale};
-        const Product q = product_of(turned(x), turned(d), PL, p.gw);
-        const Result planes = {ws + p.gw_at, (long long)p.N * p.K, nullptr};
-        launch_product<T, PL, true>(q, p.gw, p.gw.splits > 1 ? planes : o, s);
-        if (p.gw.splits > 1) {
-            sum_planes<T>(ws + p.gw_at, p.gw.splits, planes.plane, o, b, s);
-            b.blocks = 0;
-        }
-    }
-    if (b.blocks > 0)
+    const bool x_planes = grad_x && p.gx.splits > 1, w_planes = grad_w && p.gw.splits > 1;
+    const Result ox = {grad_x, 0, scale}, ow = {grad_w, 0, scale};
+    Sum sx = {}, sw = {};
+    const Bias none = {};
+    auto sum_of = [&](Sum &q, const Choice &c, long long at, long long n, const Result &o) {
+        const long long groups = (n / 4 + 255) / 256;
+        q = {(const float *)(ws + at), c.splits, (int)(groups < 8192 ? groups : 8192), n, o};
+        return Result{ws + at, n, nullptr};
+    };
+    const Result to_x = x_planes ? sum_of(sx, p.gx, p.gx_at, (long long)p.P * p.K, ox) : ox;
+    const Result to_w = w_planes ? sum_of(sw, p.gw, p.gw_at, (long long)p.N * p.K, ow) : ow;
+    // (grad_b goes with a launch that is there anyway)
+    const bool sums = x_planes || w_planes, with_products = b.blocks > 0 && !sums && (grad_x || grad_w);
+    auto launch = [&](auto pixels, const Choice &c, const Product &q, const Result &to, const Bias &bias) {
+        with_tile<PL>(c.shape, [&](auto t) {
+            typedef decltype(t) G;
+            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, decltype(pixels)::value, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>),
+                               dim3((unsigned)(q.per_xcd * kXcds + bias.blocks)), dim3(G::WR * G::WC * 64), 0, s, q, to, bias);
+            return 0;
+        });
+    };
+    if (grad_x)
+        launch(std::false_type(), p.gx, product_of(turned(w), d, PL, p.gx), to_x, with_products && !grad_w ? b : none);
+    if (grad_w)
+        launch(std::true_type(), p.gw, product_of(turned(x), turned(d), PL, p.gw), to_w, with_products ? b : none);
+    if (sums)
+        hipLaunchKernelGGL((dcnv4_layer_sum_kernel<T>), dim3((unsigned)(sx.blocks + sw.blocks + b.blocks)), dim3(256), 0, s, sx, sw, b);
+    else if (b.blocks > 0 && !with_products)
         hipLaunchKernelGGL((dcnv4_layer_bias_kernel<T>), dim3((unsigned)b.blocks), dim3(256), 0, s, b);
 }
 
@@ -775,7 +818,7 @@ template <typename T, int PL>
 int gated_backward(const LayerPlan &p, const void *x, const void *w, const void *bias, int F, int act, const T *grad_h, void *grad_x, void *grad_w, void *grad_b,
                    char *ws, hipStream_t s)
 {
-    if (PL == 1)
+    if (PL == 1 && p.most_parts > 0)
         hipLaunchKernelGGL(dcnv4_gated_most_kernel, dim3((unsigned)p.most_parts), dim3(256), 0, s, (const unsigned short *)grad_h, (long long)p.P * F,
                            (float *)(ws + p.most));
     Operand xo, wo;
@@ -793,7 +836,7 @@ int gated_backward(const LayerPlan &p, const void *x, const void *w, const void 
         const Pairs l = {bias, F, p.forward.pixels[i]};
         const Product q = product_of(pairs, rows_from(xo, first, l.P), PL, c, true);
         const Deltas e = {grad_h + (long long)first * F, d + (long long)first * PL * p.N, grad_b ? bias_sums + (long long)runs * p.N : nullptr,
-                          (const float *)(ws + p.most), p.most_parts, scale};
+                          (const float *)(ws + p.most), p.most_parts, p.most_parts > 0 ? 0 : p.P * F, scale};
         by_activation(act, [&](auto A) {
             with_tile<PL>(c.shape, [&](auto t) {
                 typedef decltype(t) G;

@@ -109,7 +109,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt, split;
-    if (!tile_of(q, at, bt, split))
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, kb = lane >> 5;
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt, split;
-    if (!tile_of(q, at, bt, split))
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     typedef std::conditional_t<WHOLE, T, float> S;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt, split;
-    if (!tile_of(q, at, bt, split))
+    if (!tile_of(q, (int)blockIdx.x, at, bt, split))
         return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / WC, wc = wave % WC, row = lane & 31, kb = lane >> 5;
@@ -561,7 +561,11 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
     }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void dcnv4_loss_bias_kernel(Bias b) { bias_of<T>(b, (int)blockIdx.x); }
+template <typename T> __global__ __launch_bounds__(256) void dcnv4_loss_bias_kernel(Bias b)
+{
+    __shared__ float part[16][17];
+    bias_of<T>(b, (int)blockIdx.x, part);
+}
 
 // Adds up the splits' planes [splits][rows][cols] and rounds: four numbers a lane.  The first workgroups make grad_b, where that saves it a
 // launch of its own (51200 x 256, 150 classes backward 70.6 -> 68.1 us).
@@ -569,8 +573,9 @@ template <typename T>
 __global__ __launch_bounds__(256) void dcnv4_loss_sum_kernel(const float *planes, long long plane, int splits, long long n, int cols,
                                                              Result o, Bias b)
 {
+    __shared__ float part[16][17];
     if ((int)blockIdx.x < b.blocks) {
-        bias_of<T>(b, (int)blockIdx.x);
+        bias_of<T>(b, (int)blockIdx.x, part);
         return;
     }
     const int units = cols / 4, block = (int)blockIdx.x - b.blocks, blocks = (int)gridDim.x - b.blocks;

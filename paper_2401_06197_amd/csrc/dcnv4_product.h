@@ -244,13 +244,13 @@ template <int PL, int WR, int WC, int WM, int WN, int R, int STAGES, bool TA = f
     }
 };
 
-// The tile and split of this workgroup: consecutive ones to one XCD, split after split (the tiles of a split read the same part of both
+// The tile and split of workgroup `block`: consecutive ones to one XCD, split after split (the tiles of a split read the same part of both
 // operands), in the order of bands of four tiles of B and along A within a band, so that the 32 tiles that an XCD has at once
 // read eight tiles of A and four of B into its L2, not 32 and one.  False: none.
-__device__ __forceinline__ bool tile_of(const Product &q, int &a_tile, int &b_tile, int &split)
+__device__ __forceinline__ bool tile_of(const Product &q, int block, int &a_tile, int &b_tile, int &split)
 {
-    const int at = ((int)blockIdx.x & (kXcds - 1)) * q.per_xcd + ((int)blockIdx.x >> 3);
-    if (((int)blockIdx.x >> 3) >= q.per_xcd || at >= q.all)
+    const int at = (block & (kXcds - 1)) * q.per_xcd + (block >> 3);
+    if ((block >> 3) >= q.per_xcd || at >= q.all)
         return false;
     split = fdiv(at, q.div_tiles);
     const int tile = at - split * q.a_tiles * q.b_tiles;
@@ -291,10 +291,11 @@ struct Bias {
 };
 
 // 16 classes to a workgroup of 256, 16 runs side by side.
-template <typename T> __device__ __forceinline__ void bias_of(const Bias &b, int block)
+// (Of more threads the others do the same.  `part` is the caller's: with a second LDS object in a kernel this compiler lets the LDS reads of Tile::multiply
+// wait for all loads.)
+template <typename T> __device__ __forceinline__ void bias_of(const Bias &b, int block, float (*part)[17])
 {
-    __shared__ float part[16][17];
-    const int i = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4, c = block * 16 + i;
+    const int i = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4 & 15, c = block * 16 + i;
     float s = 0.f;
     if (c < b.count)
 #pragma unroll 8
