@@ -435,7 +435,7 @@ long long dcnv4_backward_merged_algorithmic_bytes(int N, int H, int W, int G, in
  *   "loss_splits" workgroups that share a sum of its gradients (1..64)
  *   "loss_piece"  classes of a piece (rounded up to a multiple of 256); these three change the size of its workspace
  *   "layer_tile"  tile of the gated layer's and the layers' gradients' products, as "loss_tile"
- *   "layer_splits" workgroups that share a sum of those gradients (1..64); both change the size of their workspaces
+ *   "layer_splits" workgroups that share a sum of those gradients (1, 2, 3, 8 or 64); both change the size of their workspaces
  *   "gom_coop"    1 = the fp32 grad_offset/grad_mask pass moves its values through per-wave LDS slices
  *                 even for whole groups (default: each lane reads and writes its own pixel's values)
  *   "gx_threads"  workgroup size of the staged grad_x kernel (256, 512 or 768)

@@ -398,18 +398,14 @@ __device__ __forceinline__ void store_tile(char *smem, const Product &q, S *to, 
     }
 }
 
-// grad_x, or grad_w (PIXELS); `b`: with the last product of a layer, grad_b, by workgroups of its own behind it.
+// grad_x, or grad_w (PIXELS).
 template <typename T, bool PIXELS, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
-__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_layer_product_kernel(Product q, Result o, Bias b)
+__device__ __forceinline__ void product_tile(char *smem, const Product &q, const Result &o, int block)
 {
     typedef Tile<PL, WR, WC, WM, WN, R, STAGES, true, PIXELS> G;
-    __shared__ __attribute__((aligned(16))) char smem[G::LDS];
     int at, bt, split;
-    if (!tile_of(q, (int)blockIdx.x, at, bt, split)) {
-        if ((int)blockIdx.x >= q.per_xcd * kXcds)
-            bias_of<T>(b, (int)blockIdx.x - q.per_xcd * kXcds, reinterpret_cast<float(*)[17]>(smem));
+    if (!tile_of(q, block, at, bt, split))
         return;
-    }
     f32x16 acc[WM][WN];
 #pragma unroll
     for (int m = 0; m < WM; ++m)
@@ -424,6 +420,33 @@ __global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>:
         store_tile<G, float, WR, WC, WM, WN>(smem, q, (float *)o.out + (long long)split * o.plane, 1.f, at, bt, acc);
     else
         store_tile<G, T, WR, WC, WM, WN>(smem, q, (T *)o.out, o.scale != nullptr ? o.scale->by : 1.f, at, bt, acc);
+}
+
+// Both gradients of a layer, and grad_b: workgroups of grad_x, of grad_w (in front of the others where they take longer, so that what is left in the end is
+// short), then of grad_b.  One launch, so that the two fill the units together (5883 x 352 -> 1872 fp16: 39 us one after the other, 30 so).
+namespace {
+
+struct Gradients {
+    Product x, w;
+    Result to_x, to_w;
+    int x_blocks, w_blocks, w_first;
+    Bias bias;
+};
+
+}  // namespace
+
+template <typename T, int PL, int WR, int WC, int WM, int WN, int R, int STAGES>
+__global__ __launch_bounds__(WR * WC * 64, (Tile<PL, WR, WC, WM, WN, R, STAGES>::kWavesPerSimd)) void dcnv4_layer_gradients_kernel(Gradients q)
+{
+    // (the only LDS object: see bias_of)
+    __shared__ __attribute__((aligned(16))) char smem[Tile<PL, WR, WC, WM, WN, R, STAGES>::LDS];
+    const int block = (int)blockIdx.x, both = q.x_blocks + q.w_blocks;
+    if (block >= both)
+        bias_of<T>(q.bias, block - both, reinterpret_cast<float(*)[17]>(smem));
+    else if (q.w_first ? block >= q.w_blocks : block < q.x_blocks)
+        product_tile<T, false, PL, WR, WC, WM, WN, R, STAGES>(smem, q.x, q.to_x, q.w_first ? block - q.w_blocks : block);
+    else
+        product_tile<T, true, PL, WR, WC, WM, WN, R, STAGES>(smem, q.w, q.to_w, q.w_first ? block : block - q.x_blocks);
 }
 
 namespace {
@@ -573,7 +596,8 @@ struct Parts {
 struct LayerPlan {
     int pl, es, P, K, N, kp, np;       // N: results of the layer (gated: 2F); padded in split operands
     Parts forward;
-    Choice gx, gw;
+    Choice gx, gw;                     // (of one shape)
+    int w_first;
     int most_parts, columns_runs, columns_rows;
     // bytes from the start of the workspace
     long long x_split, w_split, g_split, d, scale, most, bias_sums, gx_at, gw_at, bytes;
@@ -615,11 +639,50 @@ Parts parts_of(int pl, int m, int P, int length)
     return best;
 }
 
-// The two products of a gradient, and room for their planes: [P][K] over N numbers, [N][K] over P.
+// The two products of a gradient, [P][K] over N numbers and [N][K] over P, in one launch: the tile and over how many workgroups each sum is split, with the
+// lowest estimated time.  The units share what all tiles take (as in `estimate`), feel half a tile of the shorter kind in the end, and are not through before
+// the longest is.
+void choose_gradients(LayerPlan &p)
+{
+    static const int tries[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    float best = -1.f;
+    auto may = [&](int splits, int length) { return g_layers.splits ? splits == g_layers.splits : splits == 1 || length / splits >= 256; };
+    auto planes = [&](int splits, long long n) { return splits > 1 ? .09f * (float)splits + (float)n * (float)splits * 1.2e-6f : 0.f; };
+    for (int i = kSmall; i <= kLarge; ++i) {
+        if (g_layers.tile && g_layers.tile != 1 + i)
+            continue;
+        const Shape &s = shape_of(p.pl, i);
+        const long long across = (p.K + s.bm - 1) / s.bm, x_tiles = across * ((p.P + s.bn - 1) / s.bn), w_tiles = across * ((p.N + s.bn - 1) / s.bn);
+        const int x_steps = (p.np + s.r - 1) / s.r, w_steps = (p.P + s.r - 1) / s.r;
+        const float alone = s.step > s.alone ? s.step : s.alone;
+        for (const int sx : tries) {
+            if (!may(sx, p.np))
+                continue;
+            const int nx = (x_steps + sx - 1) / sx;
+            const float x = (float)nx * s.step + s.fixed;
+            for (const int sw : tries) {
+                if (!may(sw, p.P))
+                    continue;
+                const int nw = (w_steps + sw - 1) / sw;
+                const float w = (float)nw * s.step + s.fixed;
+                const float shared = ((float)(x_tiles * sx) * x + (float)(w_tiles * sw) * w) / (float)kUnits + .5f * (x < w ? x : w);
+                const float longest = (float)(nx > nw ? nx : nw) * alone + s.fixed;
+                const float us = (shared > longest ? shared : longest) + planes(sx, (long long)p.P * p.K) + planes(sw, (long long)p.N * p.K) +
+                                 (sx > 1 || sw > 1 ? 2.5f : 0.f);
+                if (best < 0.f || us < best) {
+                    best = us;
+                    p.gx = {i, sx};
+                    p.gw = {i, sw};
+                    p.w_first = w > x;
+                }
+            }
+        }
+    }
+}
+
 bool plan_gradients(LayerPlan &p, Room &room)
 {
-    p.gx = choose_product(p.pl, p.K, p.P, p.np, true, g_layers.tile, g_layers.splits);
-    p.gw = choose_product(p.pl, p.K, p.N, p.P, true, g_layers.tile, g_layers.splits);
+    choose_gradients(p);
     if (!fits(p.pl, p.gx, p.K, p.P) || !fits(p.pl, p.gw, p.K, p.N))
         return false;
     if (p.gx.splits > 1)
@@ -724,7 +787,6 @@ void gradients(const LayerPlan &p, const Operand &x, const Operand &w, const Ope
     const bool x_planes = grad_x && p.gx.splits > 1, w_planes = grad_w && p.gw.splits > 1;
     const Result ox = {grad_x, 0, scale}, ow = {grad_w, 0, scale};
     Sum sx = {}, sw = {};
-    const Bias none = {};
     auto sum_of = [&](Sum &q, const Choice &c, long long at, long long n, const Result &o) {
         const long long groups = (n / 4 + 255) / 256;
         q = {(const float *)(ws + at), c.splits, (int)(groups < 8192 ? groups : 8192), n, o};
@@ -734,18 +796,17 @@ void gradients(const LayerPlan &p, const Operand &x, const Operand &w, const Ope
     const Result to_w = w_planes ? sum_of(sw, p.gw, p.gw_at, (long long)p.N * p.K, ow) : ow;
     // (grad_b goes with a launch that is there anyway)
     const bool sums = x_planes || w_planes, with_products = b.blocks > 0 && !sums && (grad_x || grad_w);
-    auto launch = [&](auto pixels, const Choice &c, const Product &q, const Result &to, const Bias &bias) {
-        with_tile<PL>(c.shape, [&](auto t) {
+    if (grad_x || grad_w) {
+        Gradients q = {product_of(turned(w), d, PL, p.gx), product_of(turned(x), turned(d), PL, p.gw), to_x, to_w, 0, 0, p.w_first, with_products ? b : Bias{}};
+        q.x_blocks = grad_x ? q.x.per_xcd * kXcds : 0;
+        q.w_blocks = grad_w ? q.w.per_xcd * kXcds : 0;
+        with_tile<PL>(p.gx.shape, [&](auto t) {
             typedef decltype(t) G;
-            hipLaunchKernelGGL((dcnv4_layer_product_kernel<T, decltype(pixels)::value, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>),
-                               dim3((unsigned)(q.per_xcd * kXcds + bias.blocks)), dim3(G::WR * G::WC * 64), 0, s, q, to, bias);
+            hipLaunchKernelGGL((dcnv4_layer_gradients_kernel<T, PL, G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>),
+                               dim3((unsigned)(q.x_blocks + q.w_blocks + q.bias.blocks)), dim3(G::WR * G::WC * 64), 0, s, q);
             return 0;
         });
-    };
-    if (grad_x)
-        launch(std::false_type(), p.gx, product_of(turned(w), d, PL, p.gx), to_x, with_products && !grad_w ? b : none);
-    if (grad_w)
-        launch(std::true_type(), p.gw, product_of(turned(x), turned(d), PL, p.gw), to_w, with_products ? b : none);
+    }
     if (sums)
         hipLaunchKernelGGL((dcnv4_layer_sum_kernel<T>), dim3((unsigned)(sx.blocks + sw.blocks + b.blocks)), dim3(256), 0, s, sx, sw, b);
     else if (b.blocks > 0 && !with_products)
@@ -895,7 +956,7 @@ int layers_set_option(const char *key, int value)
         g_layers = LayerOptions();
     else if (!strcmp(key, "layer_tile") && value >= 0 && value <= 3)
         g_layers.tile = value;
-    else if (!strcmp(key, "layer_splits") && value >= 0 && value <= 64)
+    else if (!strcmp(key, "layer_splits") && (value == 0 || value == 1 || value == 2 || value == 3 || value == 8 || value == 64))
         g_layers.splits = value;
     else
         return DCNV4_ERR_UNSUPPORTED;

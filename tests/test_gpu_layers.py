@@ -138,7 +138,7 @@ LINEAR = {"f16": [(1, 16, 8), (3, 32, 40), (65, 48, 1000), (300, 272, 72), (2000
           "f32": [(1, 8, 8), (3, 24, 40), (65, 40, 520), (300, 88, 72), (1200, 96, 136), (130, 520, 264)]}
 
 
-@pytest.mark.parametrize("tile,splits", [(0, 0), (1, 0), (2, 0), (3, 0), (0, 5)])
+@pytest.mark.parametrize("tile,splits", [(0, 0), (1, 0), (2, 0), (3, 0), (0, 3), (2, 8)])
 @pytest.mark.parametrize("dtype,size", [(d, s) for d in LINEAR for s in LINEAR[d]])
 def test_linear_backward(dtype, size, tile, splits):
     dcn.dcnv4_set_option("layer_tile", tile)
