@@ -510,7 +510,7 @@ struct Ahead {
 }  // namespace
 
 // Sums: eight columns a lane, 2^lanes_log of them side by side and 256 >> lanes_log rows.  Splits: eight numbers a lane.
-// (One launch where there were four: 2047 x 384 -> 1000 fp32 backward AHEAD1)
+// (One launch where there were four: 2047 x 384 -> 1000 fp32 backward 45 -> 38 us)
 template <typename T> __global__ __launch_bounds__(256) void dcnv4_layer_ahead_kernel(Ahead q)
 {
     typedef T eight __attribute__((ext_vector_type(8)));
@@ -623,7 +623,7 @@ struct Room {
     }
 };
 
-// (12544 x 512, 2 x 2048, fp16: 784 large tiles for 256 units; forward 74 us in one launch, FWD2 in two)
+// (12544 x 512, 2 x 2048, fp16: 784 large tiles for 256 units; forward 74 us in one launch, 68 in two)
 Parts parts_of(int pl, int m, int P, int length)
 {
     Parts best = {1, {P, 0}, {choose_product(pl, m, P, length, false, g_layers.tile, 0), {0, 1}}};
@@ -640,35 +640,49 @@ Parts parts_of(int pl, int m, int P, int length)
 }
 
 // The two products of a gradient, [P][K] over N numbers and [N][K] over P, in one launch: the tile and over how many workgroups each sum is split, with the
-// lowest estimated time.  The units share what all tiles take (as in `estimate`), feel half a tile of the shorter kind in the end, and are not through before
-// the longest is.
+// lowest estimated time (us).  Workgroups that are all there at once take as long as the longest, `share` to a unit; more of them share the units, which feel a
+// part (`tail`) of one of the shorter kind in the end.  A tile takes `step` for a step (alone on its unit `alone`) and `fixed`.  Planes are written and read once
+// more, by a launch of its own.  Fitted to 34 layers (23 to 50176 rows, K 32 to 2048, 40 to 4096 results; every tile, 1 to 64 splits of either sum, 1950
+// measurements) so that the choice costs least: 1.8 % (fp16) and 1.4 % (fp32) on average, 8 % at most.  12544, 512 -> 4096: 107 us with large tiles and 4 parts of
+// grad_w, 143 with middle ones and no parts; 3001, 256 -> 1360 fp32: 42 with middle ones, 2 and 6 parts, 51 with small ones and no parts.
 void choose_gradients(LayerPlan &p)
 {
+    struct Times {
+        float step, fixed, alone;
+    };
+    static const Times f16[] = {{.171f, 1.08f, .336f}, {.176f, 2.24f, .275f}, {.387f, 5.46f, .592f}};
+    static const Times f32[] = {{.551f, 2.33f, .652f}, {.835f, 4.81f, .835f}, {1.585f, 6.41f, 1.585f}};
     static const int tries[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const bool half = p.pl == 1;
+    const float tail = half ? 1.38f : .59f, per_split = half ? .144f : .09f, per_number = half ? .77e-6f : .48e-6f, sum = half ? 3.1f : 0.f;
     float best = -1.f;
     auto may = [&](int splits, int length) { return g_layers.splits ? splits == g_layers.splits : splits == 1 || length / splits >= 256; };
-    auto planes = [&](int splits, long long n) { return splits > 1 ? .09f * (float)splits + (float)n * (float)splits * 1.2e-6f : 0.f; };
+    auto planes = [&](int splits, long long n) { return splits > 1 ? per_split * (float)splits + (float)n * (float)splits * per_number : 0.f; };
     for (int i = kSmall; i <= kLarge; ++i) {
         if (g_layers.tile && g_layers.tile != 1 + i)
             continue;
         const Shape &s = shape_of(p.pl, i);
+        const Times &t = (half ? f16 : f32)[i];
         const long long across = (p.K + s.bm - 1) / s.bm, x_tiles = across * ((p.P + s.bn - 1) / s.bn), w_tiles = across * ((p.N + s.bn - 1) / s.bn);
         const int x_steps = (p.np + s.r - 1) / s.r, w_steps = (p.P + s.r - 1) / s.r;
-        const float alone = s.step > s.alone ? s.step : s.alone;
         for (const int sx : tries) {
             if (!may(sx, p.np))
                 continue;
             const int nx = (x_steps + sx - 1) / sx;
-            const float x = (float)nx * s.step + s.fixed;
+            const float x = (float)nx * t.step + t.fixed;
             for (const int sw : tries) {
                 if (!may(sw, p.P))
                     continue;
                 const int nw = (w_steps + sw - 1) / sw;
-                const float w = (float)nw * s.step + s.fixed;
-                const float shared = ((float)(x_tiles * sx) * x + (float)(w_tiles * sw) * w) / (float)kUnits + .5f * (x < w ? x : w);
-                const float longest = (float)(nx > nw ? nx : nw) * alone + s.fixed;
-                const float us = (shared > longest ? shared : longest) + planes(sx, (long long)p.P * p.K) + planes(sw, (long long)p.N * p.K) +
-                                 (sx > 1 || sw > 1 ? 2.5f : 0.f);
+                const float w = (float)nw * t.step + t.fixed;
+                const long long all = x_tiles * sx + w_tiles * sw;
+                const float full = (float)((all + kUnits - 1) / kUnits), share = full < (float)s.slots ? full : (float)s.slots;
+                float us = (float)(nx > nw ? nx : nw) * (t.step * share > t.alone ? t.step * share : t.alone) + t.fixed * share;
+                if (all > (long long)kUnits * s.slots) {
+                    const float shared = ((float)(x_tiles * sx) * x + (float)(w_tiles * sw) * w) / (float)kUnits + tail * (x < w ? x : w);
+                    us = shared > us ? shared : us;
+                }
+                us += planes(sx, (long long)p.P * p.K) + planes(sw, (long long)p.N * p.K) + (sx > 1 || sw > 1 ? sum : 0.f);
                 if (best < 0.f || us < best) {
                     best = us;
                     p.gx = {i, sx};
