@@ -434,7 +434,8 @@ long long dcnv4_backward_merged_algorithmic_bytes(int N, int H, int W, int G, in
  *   "loss_tile"   tile of the cross entropy's products, classes x pixels: 1 = 64x64, 2 = 128x128, 3 = 256x256 (fp32: 256x128)
  *   "loss_splits" workgroups that share a sum of its gradients (1..64)
  *   "loss_piece"  classes of a piece (rounded up to a multiple of 256); these three change the size of its workspace
- *   "layer_tile"  tile of the gated layer's and the layers' gradients' products, as "loss_tile"
+ *   "layer_tile"  tile of the gated layer's and the layers' gradients' products, as "loss_tile"; 4 = 256x128 by half the waves (the gated
+ *                 layer in fp16; elsewhere no preference)
  *   "layer_splits" workgroups that share a sum of those gradients (1, 2, 3, 8 or 64); both change the size of their workspaces
  *   "gom_coop"    1 = the fp32 grad_offset/grad_mask pass moves its values through per-wave LDS slices
  *                 even for whole groups (default: each lane reads and writes its own pixel's values)

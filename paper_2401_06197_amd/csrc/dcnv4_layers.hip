@@ -581,10 +581,9 @@ struct LayerOptions {
 constexpr int kFewNumbers = 1 << 15;                       // of grad_h, which every workgroup looks through by itself
 constexpr int kLayerMaxRows = 1 << 24, kLayerMaxWidth = 1 << 20;
 
-bool fits(int pl, const Choice &c, long long m, long long n)
+bool fits(const Shape &s, const Choice &c, long long m, long long n)
 {
-    const Shape &s = shape_of(pl, c.shape);
-    return c.shape >= 0 && ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn) * c.splits < (1 << 22);     // (a grid has fewer than 2^32 lanes)
+    return ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn) * c.splits < (1 << 22);     // (a grid has fewer than 2^32 lanes)
 }
 
 // A product over pixels in one launch, or in two: as many pixels as give whole rounds of large tiles, and the others in the tile that suits them.
@@ -623,18 +622,55 @@ struct Room {
     }
 };
 
-// (12544 x 512, 2 x 2048, fp16: 784 large tiles for 256 units; forward 74 us in one launch, 68 in two)
+// Tiles of pairs and pixels: the products', and in fp16 one more, half a large one by four waves, two workgroups to a unit, where one's products go on while the other
+// makes its results: with few features that is most of a tile's time.  Times as in `estimate`, of the forward kernel and the one that makes d together,
+// fitted to 31 layers (49 to 134400 pixels, K 32 to 2048, F 128 to 4096) in every tile so that the choice costs least: 0.4 % (fp16) and 0 on average.
+// Forward and d, 50176 x 256, 2 x 1024: 400, 238, 259 and 225 us by the four tiles; 8192 x 1024, 2 x 2816: 390, 268, 229, 250; 1000 x 1024, 2 x 1024: 25, 28, 53, 39.
+enum { kTall = kLarge + 1, kGatedTiles };
+const Shape &gated_shape(int pl, int i)
+{
+    static const Shape f16[] = {{64, 64, 64, 2, .347f, 1.77f, .476f, .067f}, {128, 128, 32, 2, .552f, 1.65f, .552f, 0.f},
+                                {256, 256, 32, 1, 1.105f, 11.7f, 1.105f, 0.f}, {256, 128, 32, 2, .901f, 2.01f, .901f, 0.f}};
+    static const Shape f32[] = {{64, 64, 64, 1, 1.68f, 2.46f, 1.68f, 0.f}, {128, 128, 32, 1, 2.38f, 4.83f, 2.38f, 0.f}, {256, 128, 32, 1, 3.85f, 1.54f, 3.85f, 0.f}};
+    return (pl == 1 ? f16 : f32)[i];
+}
+int gated_tiles(int pl) { return pl == 1 ? kGatedTiles : kLarge + 1; }
+template <int PL, typename F> int with_gated_tile(int shape, F &&f)
+{
+    if constexpr (PL == 1)
+        if (shape == kTall) return f(TileOf<4, 1, 2, 4, 32, 3>());
+    return with_tile<PL>(shape, f);
+}
+
+Choice choose_gated(int pl, int m, long long pixels, int length, int only)
+{
+    Choice best = {-1, 1};
+    float least = 0.f;
+    for (int i = 0; i < gated_tiles(pl); ++i) {
+        if (only && only <= gated_tiles(pl) && only != 1 + i)
+            continue;
+        const float us = estimate(gated_shape(pl, i), m, pixels, length, 1);
+        if (best.shape < 0 || us < least) {
+            best.shape = i;
+            least = us;
+        }
+    }
+    return best;
+}
+
+// (12544 x 512, 2 x 2048, fp16: 784 large tiles for 256 units; forward and d 190 us in one launch each, 174 in two)
 Parts parts_of(int pl, int m, int P, int length)
 {
-    Parts best = {1, {P, 0}, {choose_product(pl, m, P, length, false, g_layers.tile, 0), {0, 1}}};
-    const Shape &s = shape_of(pl, kLarge);
+    Parts best = {1, {P, 0}, {choose_gated(pl, m, P, length, g_layers.tile), {0, 1}}};
+    const Shape &s = gated_shape(pl, kLarge);
     const long long across = (m + s.bm - 1) / s.bm, rounds = across * ((P + s.bn - 1) / s.bn) / kUnits;
     const long long first = rounds * kUnits / across * s.bn;
     if (g_layers.tile || first <= 0 || first >= P)
         return best;
-    const Choice rest = choose_product(pl, m, P - first, length, false, 0, 0);
-    const Choice &one = best.choice[0];
-    if (estimate(s, m, first, length, 1) + estimate(shape_of(pl, rest.shape), m, P - first, length, 1) + 3.f < estimate(shape_of(pl, one.shape), m, P, length, 1))
+    const Choice rest = choose_gated(pl, m, P - first, length, 0);
+    // (6: two launches more)
+    if (estimate(s, m, first, length, 1) + estimate(gated_shape(pl, rest.shape), m, P - first, length, 1) + 6.f <
+        estimate(gated_shape(pl, best.choice[0].shape), m, P, length, 1))
         best = {2, {(int)first, P - (int)first}, {{kLarge, 1}, rest}};
     return best;
 }
@@ -659,7 +695,7 @@ void choose_gradients(LayerPlan &p)
     auto may = [&](int splits, int length) { return g_layers.splits ? splits == g_layers.splits : splits == 1 || length / splits >= 256; };
     auto planes = [&](int splits, long long n) { return splits > 1 ? per_split * (float)splits + (float)n * (float)splits * per_number : 0.f; };
     for (int i = kSmall; i <= kLarge; ++i) {
-        if (g_layers.tile && g_layers.tile != 1 + i)
+        if (g_layers.tile && g_layers.tile <= kLarge + 1 && g_layers.tile != 1 + i)
             continue;
         const Shape &s = shape_of(p.pl, i);
         const Times &t = (half ? f16 : f32)[i];
@@ -697,7 +733,7 @@ void choose_gradients(LayerPlan &p)
 bool plan_gradients(LayerPlan &p, Room &room)
 {
     choose_gradients(p);
-    if (!fits(p.pl, p.gx, p.K, p.P) || !fits(p.pl, p.gw, p.K, p.N))
+    if (!fits(shape_of(p.pl, p.gx.shape), p.gx, p.K, p.P) || !fits(shape_of(p.pl, p.gw.shape), p.gw, p.K, p.N))
         return false;
     if (p.gx.splits > 1)
         p.gx_at = room.take((long long)p.gx.splits * p.P * p.K * 4);
@@ -725,7 +761,7 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
         return DCNV4_ERR_UNSUPPORTED;
     p.forward = parts_of(p.pl, p.N, p.P, p.kp);
     for (int i = 0; i < p.forward.count; ++i)
-        if (!fits(p.pl, p.forward.choice[i], p.N, p.forward.pixels[i]))
+        if (!fits(gated_shape(p.pl, p.forward.choice[i].shape), p.forward.choice[i], p.N, p.forward.pixels[i]))
             return DCNV4_ERR_UNSUPPORTED;
     Room room;
     if (p.pl == 3) {
@@ -811,7 +847,7 @@ void gradients(const LayerPlan &p, const Operand &x, const Operand &w, const Ope
     // (grad_b goes with a launch that is there anyway)
     const bool sums = x_planes || w_planes, with_products = b.blocks > 0 && !sums && (grad_x || grad_w);
     if (grad_x || grad_w) {
-        Gradients q = {product_of(turned(w), d, PL, p.gx), product_of(turned(x), turned(d), PL, p.gw), to_x, to_w, 0, 0, p.w_first, with_products ? b : Bias{}};
+        Gradients q = {product_of(turned(w), d, shape_of(PL, p.gx.shape), p.gx), product_of(turned(x), turned(d), shape_of(PL, p.gw.shape), p.gw), to_x, to_w, 0, 0, p.w_first, with_products ? b : Bias{}};
         q.x_blocks = grad_x ? q.x.per_xcd * kXcds : 0;
         q.w_blocks = grad_w ? q.w.per_xcd * kXcds : 0;
         with_tile<PL>(p.gx.shape, [&](auto t) {
@@ -875,9 +911,9 @@ int gated_forward(const LayerPlan &p, const void *x, const void *w, const void *
     for (int i = 0; i < p.forward.count; ++i) {
         const Choice &c = p.forward.choice[i];
         const Pairs l = {bias, F, p.forward.pixels[i]};
-        const Product q = product_of(wo, rows_from(xo, first, l.P), PL, c, true);
+        const Product q = product_of(wo, rows_from(xo, first, l.P), gated_shape(PL, c.shape), c, true);
         by_activation(act, [&](auto A) {
-            with_tile<PL>(c.shape, [&](auto t) {
+            with_gated_tile<PL>(c.shape, [&](auto t) {
                 typedef decltype(t) G;
                 hipLaunchKernelGGL((dcnv4_gated_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
                                    dim3(G::WR * G::WC * 64), 0, s, q, l, h + (long long)first * F);
@@ -909,11 +945,11 @@ int gated_backward(const LayerPlan &p, const void *x, const void *w, const void 
     for (int i = 0; i < p.forward.count; ++i) {
         const Choice &c = p.forward.choice[i];
         const Pairs l = {bias, F, p.forward.pixels[i]};
-        const Product q = product_of(pairs, rows_from(xo, first, l.P), PL, c, true);
+        const Product q = product_of(pairs, rows_from(xo, first, l.P), gated_shape(PL, c.shape), c, true);
         const Deltas e = {grad_h + (long long)first * F, d + (long long)first * PL * p.N, grad_b ? bias_sums + (long long)runs * p.N : nullptr,
                           (const float *)(ws + p.most), p.most_parts, p.most_parts > 0 ? 0 : p.P * F, scale};
         by_activation(act, [&](auto A) {
-            with_tile<PL>(c.shape, [&](auto t) {
+            with_gated_tile<PL>(c.shape, [&](auto t) {
                 typedef decltype(t) G;
                 runs += q.b_tiles * G::WC;
                 hipLaunchKernelGGL((dcnv4_gated_delta_kernel<T, PL, A(), G::WR, G::WC, G::WM, G::WN, G::R, G::STAGES>), dim3((unsigned)(q.per_xcd * kXcds)),
@@ -968,7 +1004,7 @@ int layers_set_option(const char *key, int value)
 {
     if (!strcmp(key, "reset"))
         g_layers = LayerOptions();
-    else if (!strcmp(key, "layer_tile") && value >= 0 && value <= 3)
+    else if (!strcmp(key, "layer_tile") && value >= 0 && value <= kGatedTiles)
         g_layers.tile = value;
     else if (!strcmp(key, "layer_splits") && (value == 0 || value == 1 || value == 2 || value == 3 || value == 8 || value == 64))
         g_layers.splits = value;

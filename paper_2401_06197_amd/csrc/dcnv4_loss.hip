@@ -712,7 +712,7 @@ template <typename T, int PL> int loss_forward(const Plan &p, const void *x, con
         const char *rows = (const char *)w + (long long)l.v0 * p.K * p.es;
         if (PL == 3)
             split_rows(rows, l.count, p.K, p.kp, ws + p.w_split, s);
-        const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, PL, p.logits);
+        const Product q = product_of(rows_of(PL == 3 ? ws + p.w_split : rows, l.count, p.kp, PL, p.kp), b, shape_of(PL, p.logits.shape), p.logits);
         const bool one = p.pieces == 1 && q.a_tiles == 1;
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
@@ -776,7 +776,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         const void *wrows = PL == 3 ? (const void *)(ws + p.w_split) : rows;
         // d
         const Deltas d = {lse, g, (unsigned short *)(ws + p.d), grad_b != nullptr ? (float *)(ws + p.bias_sums) : nullptr, vp};
-        const Product q = product_of(rows_of(wrows, l.count, p.kp, PL, p.kp), xo, PL, p.logits);
+        const Product q = product_of(rows_of(wrows, l.count, p.kp, PL, p.kp), xo, shape_of(PL, p.logits.shape), p.logits);
         int runs = 0;
         with_tile<PL>(p.logits.shape, [&](auto t) {
             typedef decltype(t) G;
@@ -792,7 +792,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
             hipLaunchKernelGGL((dcnv4_loss_bias_kernel<T>), dim3((unsigned)bias.blocks), dim3(256), 0, s, bias);
         // grad_x, over the pieces
         const Result ox = {grad_x, 0, g, nullptr, 0};
-        const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), PL, p.gx);
+        const Product qx = product_of(turned(rows_of(wrows, l.count, p.K, PL, p.kp)), rows_of(d.d, p.P, vp, PL, vp), shape_of(PL, p.gx.shape), p.gx);
         if (p.gx_planes) {
             const Result o = {ws + p.gx_at, (long long)p.P * p.K, nullptr, nullptr, piece > 0};
             launch_product<T, PL, false>(qx, p.gx, true, o, s);
@@ -803,7 +803,7 @@ int loss_backward(const Plan &p, const void *x, const void *w, const Labels &lab
         }
         // grad_w of the piece
         const Result ow = {(char *)grad_w + (long long)l.v0 * p.K * p.es, 0, nullptr, scale, 0};
-        const Product qw = product_of(xg, turned(rows_of(d.d, p.P, l.count, PL, vp)), PL, p.gw);
+        const Product qw = product_of(xg, turned(rows_of(d.d, p.P, l.count, PL, vp)), shape_of(PL, p.gw.shape), p.gw);
         if (p.gw_planes) {
             const Result o = {ws + p.gw_at, (long long)l.count * p.K, nullptr, scale, 0};
             launch_product<T, PL, true>(qw, p.gw, true, o, s);

@@ -390,9 +390,8 @@ Operand rows_of(const void *base, int rows, int cols, int pl, int pad)
 Operand turned(const Operand &o) { return {o.base, o.row_bytes, o.length, o.count, o.plane_bytes}; }
 
 // `pairs`: A has 2 * count rows, which the tiles take in pairs.
-Product product_of(const Operand &a, const Operand &b, int pl, const Choice &c, bool pairs = false)
+Product product_of(const Operand &a, const Operand &b, const Shape &s, const Choice &c, bool pairs = false)
 {
-    const Shape &s = shape_of(pl, c.shape);
     Product q;
     q.a = a;
     q.b = b;

@@ -164,7 +164,7 @@ def test_layers_validate_on_the_host():
         assert gated_back(size=bytes_of(5, 32, 16, dtype, True) - 1, dtype=dtype) == 2
         assert linear_back(size=dcn.dcnv4_linear_backward_workspace_bytes(5, 32, 16, dtype) - 1, dtype=dtype) == 2
     assert gated(size=bytes_of(5, 32, 16, 0, False) - 1) == 2
-    for key, bad in (("layer_tile", 4), ("layer_splits", 65), ("layer_tile", -1)):
+    for key, bad in (("layer_tile", 5), ("layer_splits", 65), ("layer_tile", -1)):
         with pytest.raises(dcn.Dcnv4Error):
             dcn.dcnv4_set_option(key, bad)
 

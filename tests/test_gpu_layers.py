@@ -65,17 +65,17 @@ SIZES = {"f16": [(1, 16, 8), (3, 32, 8), (2, 48, 264), (65, 48, 72), (257, 80, 1
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
-@pytest.mark.parametrize("tile", [0, 1, 2, 3])
+@pytest.mark.parametrize("tile", [0, 1, 2, 3, 4])
 @pytest.mark.parametrize("dtype,size", [(d, s) for d in SIZES for s in SIZES[d]])
 def test_gated_layer(dtype, size, tile, act):
     dcn.dcnv4_set_option("layer_tile", tile)
     check(draw(*size, dtype, sum(size)), dtype, act)
 
 
-@pytest.mark.parametrize("dtype,P", [("f16", 256 * 256 + 465), ("f32", 128 * 256 + 233)])
-def test_pixels_in_two_launches(dtype, P):
-    """One tile of pairs, and pixels for a whole round of large tiles and some more, which go by themselves."""
-    check(draw(P, 256, 128, dtype, 11), dtype, "silu")
+@pytest.mark.parametrize("dtype,P,K", [("f16", 8192 + 200, 1024), ("f32", 4096 + 100, 256)])
+def test_pixels_in_two_launches(dtype, P, K):
+    """Eight tiles of pairs, and pixels for a whole round of large tiles and some more, which go by themselves."""
+    check(draw(P, K, 1024, dtype, 11), dtype, "silu")
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
@@ -187,7 +187,7 @@ def test_nothing_is_written_behind_the_results():
         shapes = {"h": (P, F), "gx": (P, K), "gw": (2, F, K), "gb": (2, F)}
         room = {k: torch.full((int(np.prod(s)) + 4096,), 5.0, dtype=torch.float16, device="cuda") for k, s in shapes.items()}
         part = {k: room[k][:int(np.prod(s))].view(s) for k, s in shapes.items()}
-        for tile in (1, 2, 3):
+        for tile in (1, 2, 3, 4):
             dcn.dcnv4_set_option("layer_tile", tile)
             need = dcn.dcnv4_gated_linear_workspace_bytes(P, K, F, 1, True)
             space = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
