@@ -376,7 +376,7 @@ typedef struct {
 /* A step of AdamW (decoupled weight decay) over `count` tensors, t = step + the number at step_on_device:
  *     g = grad * f0,   m = beta1 * m + (1 - beta1) * g,   v = beta2 * v + (1 - beta2) * g^2
  *     param = param * (1 - lr * f1 * weight_decay) - lr * f1 / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
- * tensors: host memory, read during the call only.  Each n from 1 to 2^36; no two buffers may share memory.  `dtype`: that of the gradients (and copies).
+ * tensors: host memory, read during the call only.  Each n from 1 to 2^34; no two buffers may share memory.  `dtype`: that of the gradients (and copies).
  * step_on_device: NULL, or the device address of one 64-bit number (8-byte aligned; t is 1 where the sum is less).  factors_on_device:
  * NULL (f0 = f1 = 1), or the device address of two fp32 numbers f0, f1 (8-byte aligned): a loss scale's inverse times what clips gradients, and a schedule's
  * factor.  Where f0 is infinite or NaN the step changes nothing (a loss scale that was too large).  Both are for captured graphs, whose

@@ -8,6 +8,9 @@
 // Memory bounds it: an element is read and written once.  The moments are made in 64 bits (their rate leaves room for it), so that what is rounded to 8 bits
 // does not hang on the order of operations.  A launch takes up to kRecords tensors, whose addresses travel with its
 // arguments: nothing has to be copied to the device first, so a captured step needs no memory of its own.
+// A lane takes one run of eight and ends: two or four of them one after the other, the next asked for early, take longer wherever it was
+// measured (55 million parameters in 54 tensors, fp16 gradients and copies, states of 32 bits: 285 us, 292 by two, 299 by four; 78 million in 314,
+// states of 8 bits: 264, 282, 296; 4096 * 16: 5.6, 5.6, 7.1).
 #include <float.h>
 #include <math.h>
 
@@ -18,8 +21,7 @@
 namespace {
 
 constexpr int kAdamBlock = 256;                            // elements that share a scale
-constexpr int kRound = 256 * 8;                            // elements of a workgroup's round: a run of eight to a lane
-constexpr int kRounds = 4;                                 // of a workgroup, where there are many
+constexpr int kPart = 256 * 8;                             // elements of a workgroup: a run of eight to a lane
 constexpr int kRecords = 56;                               // of a launch: its arguments are 4 KiB at most
 constexpr float kTop = 448.f, kNone = 0x1p-100f;           // e4m3's largest number; a block whose largest is less is stored as zeros
 
@@ -37,7 +39,6 @@ struct AdamArgs {
     AdamTensor t[kRecords];
     int first[kRecords];                                   // each tensor's first workgroup
     int count, number;                                     // tensors of this launch; number of the first one in the call
-    int rounds;                                            // of a workgroup
     double b1, b2, log_b1, log_b2;                         // logarithms: where the step's number is on the device
     double unbias1;                                        // 1 / (1 - b1^t)
     float unbias2, eps;                                    // 1 / sqrt(1 - b2^t)
@@ -132,7 +133,13 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
     const int before = lane < a.count ? a.first[lane] : 0x7fffffff;
     const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before <= (int)blockIdx.x)) - 1;
     const AdamTensor &t = a.t[at];
-    const long long n = t.n, begin = (long long)((int)blockIdx.x - a.first[at]) * a.rounds * kRound + (int)threadIdx.x * 8;
+    const long long i = (long long)((int)blockIdx.x - a.first[at]) * kPart + (int)threadIdx.x * 8, left = t.n - i;
+    if (i - (i & (kAdamBlock - 1)) >= t.n)                 // (all lanes of a block or none, for the exchanges between them)
+        return;
+    const Raw8<float> p = take(t.p + i, left);
+    const Raw8<T> grad = take((const T *)t.g + i, left);
+    const Raw8<S> m0 = take((const S *)t.m + i, left), v0 = take((const S *)t.v + i, left);
+    const float2 s = EIGHT ? t.scales[i / kAdamBlock] : float2{};
     double by = 1.0, lr = (double)t.lr, unbias1 = a.unbias1;
     float decay = t.decay, unbias2 = a.unbias2;
     long long step = a.step;
@@ -152,104 +159,77 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
     }
     const float rate = (float)(lr * unbias1);
     const double c1 = 1.0 - a.b1, c2 = 1.0 - a.b2;
-    // (the next round's numbers are asked for before the present ones are dealt with)
-    Raw8<float> p_next;
-    Raw8<T> g_next;
-    Raw8<S> m_next, v_next;
-    float2 s_next;
-    auto load = [&](long long i) {
-        const long long left = n - i;
-        p_next = take(t.p + i, left);
-        g_next = take((const T *)t.g + i, left);
-        m_next = take((const S *)t.m + i, left);
-        v_next = take((const S *)t.v + i, left);
-        if (EIGHT && i - (i & (kAdamBlock - 1)) < n)
-            s_next = t.scales[i / kAdamBlock];
-    };
-    load(begin);
-#pragma unroll 1
-    for (int round = 0; round < a.rounds; ++round) {
-        const long long i = begin + round * kRound, left = n - i;
-        if (i - (i & (kAdamBlock - 1)) >= n)               // (all lanes of a block or none, for the exchanges between them)
-            break;
-        const Raw8<float> p = p_next;
-        const Raw8<T> grad = g_next;
-        const Raw8<S> m0 = m_next, v0 = v_next;
-        const float2 s = s_next;
-        if (round + 1 < a.rounds)
-            load(i + kRound);
-        float m[8], r[8], v[8];
-        double sm = 1.0, sr = 1.0;
-        if constexpr (EIGHT) {
-            from_8_bits(m0, m);
-            from_8_bits(v0, v);
-            sm = (double)s.x;
-            sr = (double)s.y;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m[e] = m0[e];
-                v[e] = v0[e];
-            }
-        }
+    float m[8], r[8], v[8];
+    double sm = 1.0, sr = 1.0;
+    if constexpr (EIGHT) {
+        from_8_bits(m0, m);
+        from_8_bits(v0, v);
+        sm = (double)s.x;
+        sr = (double)s.y;
+    } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const double g = (double)(float)grad[e] * by;
-            double mm = (double)m[e], vv = (double)v[e];
-            if constexpr (EIGHT) {
-                mm *= sm;
-                vv *= sr;
-                vv *= vv;
-            }
-            m[e] = (float)__builtin_fma(a.b1, mm, c1 * g);
-            v[e] = (float)__builtin_fma(a.b2, vv, c2 * (g * g));
-            r[e] = __builtin_sqrtf(v[e]);
+            m[e] = m0[e];
+            v[e] = v0[e];
         }
-        Raw8<float> out;
-        Raw8<_Float16> half;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double g = (double)(float)grad[e] * by;
+        double mm = (double)m[e], vv = (double)v[e];
+        if constexpr (EIGHT) {
+            mm *= sm;
+            vv *= sr;
+            vv *= vv;
+        }
+        m[e] = (float)__builtin_fma(a.b1, mm, c1 * g);
+        v[e] = (float)__builtin_fma(a.b2, vv, c2 * (g * g));
+        r[e] = __builtin_sqrtf(v[e]);
+    }
+    Raw8<float> out;
+    Raw8<_Float16> half;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float move = rate * m[e] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[e], unbias2, a.eps));
+        out[e] = __builtin_fmaf(-decay, p[e], p[e]) - move;
+        half[e] = (_Float16)out[e];
+    }
+    put(t.p + i, left, out);
+    if (t.copy != nullptr)
+        put(t.copy + i, left, half);
+    if constexpr (EIGHT) {
+        float tm = 0.f, tr = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {                  // (behind the last element: zeros)
+            tm = fmaxf(tm, fabsf(m[e]));
+            tr = fmaxf(tr, r[e]);
+        }
+        tm = block_max(tm);
+        tr = block_max(tr);
+        tm = tm >= kNone ? tm : 0.f;
+        tr = tr >= kNone ? tr : 0.f;
+        const float im = tm > 0.f ? kTop / tm : 0.f, ir = tr > 0.f ? kTop / tr : 0.f;
+        const Bits8 bits = philox((unsigned long long)(i >> 3) + ((unsigned long long)(a.number + at) << 40), (unsigned long long)step, a.seed);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float move = rate * m[e] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[e], unbias2, a.eps));
-            out[e] = __builtin_fmaf(-decay, p[e], p[e]) - move;
-            half[e] = (_Float16)out[e];
+            m[e] *= im;
+            m[e] = m[e] > kTop ? kTop : m[e] < -kTop ? -kTop : m[e];
+            r[e] *= ir;
+            r[e] = round_by(r[e] > kTop ? kTop : r[e], (bits.w[e / 2] >> (16 * (e & 1))) & 0xffffu);
         }
-        put(t.p + i, left, out);
-        if (t.copy != nullptr)
-            put(t.copy + i, left, half);
-        if constexpr (EIGHT) {
-            float tm = 0.f, tr = 0.f;
+        put((Byte *)t.m + i, left, to_8_bits(m));
+        put((Byte *)t.v + i, left, to_8_bits(r));
+        if ((lane & 31) == 0 && left > 0)
+            t.scales[i / kAdamBlock] = make_float2(tm * (1.f / kTop), tr * (1.f / kTop));
+    } else {
+        Raw8<float> mo, vo;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {                  // (behind the last element: zeros)
-                tm = fmaxf(tm, fabsf(m[e]));
-                tr = fmaxf(tr, r[e]);
-            }
-            tm = block_max(tm);
-            tr = block_max(tr);
-            tm = tm >= kNone ? tm : 0.f;
-            tr = tr >= kNone ? tr : 0.f;
-            const float im = tm > 0.f ? kTop / tm : 0.f, ir = tr > 0.f ? kTop / tr : 0.f;
-            const Bits8 bits = philox((unsigned long long)(i >> 3) + ((unsigned long long)(a.number + at) << 40), (unsigned long long)step, a.seed);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m[e] *= im;
-                m[e] = m[e] > kTop ? kTop : m[e] < -kTop ? -kTop : m[e];
-                r[e] *= ir;
-                r[e] = round_by(r[e] > kTop ? kTop : r[e], (bits.w[e / 2] >> (16 * (e & 1))) & 0xffffu);
-            }
-            put((Byte *)t.m + i, left, to_8_bits(m));
-            put((Byte *)t.v + i, left, to_8_bits(r));
-            if ((lane & 31) == 0 && left > 0)
-                t.scales[i / kAdamBlock] = make_float2(tm * (1.f / kTop), tr * (1.f / kTop));
-        } else {
-            Raw8<float> mo, vo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mo[e] = m[e];
-                vo[e] = v[e];
-            }
-            put((float *)t.m + i, left, mo);
-            put((float *)t.v + i, left, vo);
+        for (int e = 0; e < 8; ++e) {
+            mo[e] = m[e];
+            vo[e] = v[e];
         }
+        put((float *)t.m + i, left, mo);
+        put((float *)t.v + i, left, vo);
     }
 }
 
@@ -264,7 +244,7 @@ int check_tensor(const dcnv4_adamw_tensor &t, bool eight, bool f16)
     if (t.n < 1)
         return DCNV4_ERR_SHAPE;
     // (a launch has fewer than 2^32 lanes; learning rates and decays of any sign are a caller's choice)
-    if (t.n > (1LL << 36) || (t.copy && !f16) || !(fabs(t.lr) <= 3e38) || !(fabs(t.lr * t.weight_decay) <= 3e38))
+    if (t.n > (1LL << 34) || (t.copy && !f16) || !(fabs(t.lr) <= 3e38) || !(fabs(t.lr * t.weight_decay) <= 3e38))
         return DCNV4_ERR_UNSUPPORTED;
     if (!aligned_to(t.param, 16) || !aligned_to(t.grad, 16) || !aligned_to(t.m, 16) || !aligned_to(t.v, 16) || !aligned_to(t.copy, 16) ||
         (eight && !aligned_to(t.scales, 8)))
@@ -313,17 +293,13 @@ extern "C" int dcnv4_adamw(const dcnv4_adamw_tensor *tensors, int count, double 
     a.more = (const long long *)step_on_device;
     a.factors = (const float *)factors_on_device;
     for (int from = 0; from < count;) {
-        long long groups = 0, elements = 0;
+        long long groups = 0;
         a.count = 0;
         a.number = from;
-        // many rounds to a workgroup where that leaves every unit eight of them, else one after the other would only take longer
-        for (int i = from; i < count && i < from + kRecords; ++i)
-            elements += tensors[i].n;
-        a.rounds = elements >= 2048LL * kRounds * kRound ? kRounds : 1;
         for (; from < count && a.count < kRecords; ++from) {
             const dcnv4_adamw_tensor &t = tensors[from];
-            const long long more = (t.n + a.rounds * kRound - 1) / (a.rounds * kRound);
-            if (groups + more >= 1 << 24)                  // (a tensor has 2^23 at most: those past 2^24 elements have kRounds)
+            const long long more = (t.n + kPart - 1) / kPart;
+            if (groups + more >= 1 << 24)                  // (a tensor has 2^23 at most)
                 break;
             a.first[a.count] = (int)groups;
             a.t[a.count++] = {t.n, t.param, t.grad, t.m, t.v, (float2 *)t.scales, (_Float16 *)t.copy, (float)t.lr, (float)(t.lr * t.weight_decay)};

@@ -419,8 +419,6 @@ namespace {
 
 // Rows wider than this are refused: sixteen waves with a run of eight each.
 constexpr int kEndMaxChannels = 8192;
-// Workgroups of the backward pass, each of which leaves partial sums of up to 4 * C.
-int end_back_most(int C) { return C <= 512 ? 1024 : C <= 2048 ? 512 : 256; }
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
@@ -441,13 +439,15 @@ template <typename F> int by_lanes(int C, F &&f)
     return f(std::integral_constant<int, 1024>());
 }
 
+// Workgroups of the backward pass, each of which leaves partial sums of up to 4 * C: two to a unit, more only write more sums; one where rows are so wide that
+// the sums are much of the traffic.  With both norms, us by 256, 512 and 1024 workgroups: fp16 134400 x 256 88, 87, 98; 50176 x 512 66, 59, 69; 12544 x 1024
+// 43, 37, 47; 50176 x 1536 178, 186, 203; 12544 x 2048 64, 72, 90; 4096 x 4096 52, 67, 99; fp32 50176 x 512 117, 122, 125.
 int end_back_groups(long long P, int C)
 {
     return by_lanes(C, [&](auto L) {
         const long long rows = end_threads(L()) / L(), n = (P + rows - 1) / rows;
-        // (four rows a lane at least, where that leaves every unit two workgroups)
-        const long long enough = n / 4 > 512 ? n / 4 : 512, most = end_back_most(C);
-        return (int)(n < enough ? n < most ? n : most : enough < most ? enough : most);
+        const int most = C <= 1024 ? 512 : 256;
+        return n < most ? (int)n : most;
     });
 }
 

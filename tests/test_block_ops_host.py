@@ -25,7 +25,7 @@ def test_adamw_validates_on_the_host():
         assert adam(**{name: None}) == 1 and adam(**{name: A + 8}) == 4
     assert adam(bits=8) == 1 and adam(bits=8, scales=A + 4) == 4 and adam(dtype=1, copy=A + 8) == 4
     assert adam(count=0) == 2 and adam(count=-1) == 2 and adam(n=0) == 2 and adam(n=-5) == 2
-    assert adam(n=(1 << 36) + 1) == 3 and adam(bits=16) == 3 and adam(dtype=2) == 3 and adam(copy=A) == 3
+    assert adam(n=(1 << 34) + 1) == 3 and adam(bits=16) == 3 and adam(dtype=2) == 3 and adam(copy=A) == 3
     for bad in (-0.1, 1.0, nan):
         assert adam(beta1=bad) == 3 and adam(beta2=bad) == 3
     for bad in (0.0, -1e-8, nan, inf, 1e-40):
