@@ -965,8 +965,8 @@ def dcnv4_gated_linear_backward(x, w, grad_h, b=None, activation="silu", need_x=
 
 
 class AdamwPlan:
-    """The tensors of a dcnv4_adamw_step, checked and listed once (dcnv4_adamw_plan makes it).  It holds the tensors themselves: their
-    gradients are read where they are at each step."""
+    """The tensors of a dcnv4_adamw_step, checked and listed once (dcnv4_adamw_plan makes it).  It holds their memory and works there at each
+    step: a tensor that is given other memory (a gradient that is made anew) needs a new plan."""
 
     def __init__(self, records, held, device, state_bits, dtype):
         self.records, self.held, self.device, self.state_bits, self.dtype = records, held, device, state_bits, dtype
@@ -1038,7 +1038,9 @@ def dcnv4_adamw_plan(params, grads, exp_avgs, exp_avg_sqs, lr, weight_decay=0.0,
     ptr = lambda t: None if t is None else t.data_ptr()
     for r, p, g, m, v, s, c in zip(records, params, grads, ms, vs, scales, copies):
         r.n, r.param, r.grad, r.m, r.v, r.scales, r.copy = p.numel(), ptr(p), ptr(g), ptr(m), ptr(v), ptr(s), ptr(c)
-    plan = AdamwPlan(records, (params, grads, ms, vs, scales, copies), device, 8 if eight else 32, dtype)
+    # (the memory that is listed, whatever the caller's tensors are made to hold later)
+    held = tuple([None if t is None else t.detach() for t in l] for l in (params, grads, ms, vs, scales, copies))
+    plan = AdamwPlan(records, held, device, 8 if eight else 32, dtype)
     plan.set(lr=lr, weight_decay=weight_decay)
     return plan
 

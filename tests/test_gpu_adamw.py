@@ -249,8 +249,8 @@ def test_refusals_of_the_plan():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
-def test_large_tensors_take_several_rounds(bits):
-    """Past 2^24 elements a workgroup deals with several rounds of them; a part by itself, with one, gives the same bits."""
+def test_large_tensors_and_their_parts(bits):
+    """A part of a large tensor by itself gets the same bits."""
     n, part = 2 ** 24 + 100003, 2 ** 20 + 256
     gen = torch.Generator(device="cuda").manual_seed(1)
     r = lambda size: torch.randn(n, device="cuda", generator=gen) * size
