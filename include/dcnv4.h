@@ -383,7 +383,8 @@ typedef struct {
  * arguments stay what they were.  state_bits: 32, or 8: m and r = sqrt(v) are stored as e4m3 (fp8, largest number 448, zeros to start with), times a scale
  * of its own for each 256 elements of the tensor: their largest magnitude / 448 (zeros for blocks below 2^-100).  m * 448 / that magnitude is rounded to nearest; r so
  * scaled to one of its two neighbours, up with the probability that keeps its mean (random bits of dcnv4_dropout's generator with key `seed` and
- * counter (i / 8 + number of the tensor * 2^40, t), 16 for element i as there), and never from above zero to zero.  With 8 bits g must be finite where f0 is, and less than 2^63: a block shares what is not.
+ * counter (i / 8 + number of the tensor * 2^40, t), 16 for element i as there), and never from above zero to zero.  With 8 bits g must be finite where f0
+ * is, and less than 2^63: a block of elements shares what is not.
  * 0 <= beta < 1, eps > 0 (a normal fp32 number), step >= 1 (0 with step_on_device). */
 int dcnv4_adamw(const dcnv4_adamw_tensor *tensors, int count, double beta1, double beta2, double eps, long long step,
                 const void *step_on_device, const void *factors_on_device, unsigned long long seed, int state_bits, int dtype, void *stream);

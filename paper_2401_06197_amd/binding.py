@@ -850,7 +850,8 @@ def dcnv4_norm_scale_add_norm(x, residual, scale=None, gate=None, first=None, se
     z, y, mean1, rstd1, mean2, rstd2 = results = _outputs(x, out, (
         ("z", shape, dt), None if second is None else ("y", shape, dt), ("mean1", stat, f32) if one else None, ("rstd1", stat, f32) if one else None,
         ("mean2", stat, f32) if two else None, ("rstd2", stat, f32) if two else None), stream)
-    args = (*[None if t is None else t.data_ptr() for t in (x, residual, gamma1, beta1, scale, gate, gamma2, beta2, z, y, mean1, rstd1, mean2, rstd2)], P, C, gates, norms, float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
+    args = (*[None if t is None else t.data_ptr() for t in (x, residual, gamma1, beta1, scale, gate, gamma2, beta2, z, y, mean1, rstd1, mean2, rstd2)],
+            P, C, gates, norms, float(eps), _dtype_code(x), _stream_ptr(stream, x.device))
     if prepare_only:
         return _prepared(args, out)
     _call(x.device, "dcnv4_norm_scale_add_norm", args)
