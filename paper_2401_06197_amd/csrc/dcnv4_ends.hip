@@ -350,13 +350,13 @@ template <typename T, bool FIRST, bool SECOND> __global__ __launch_bounds__(1024
     __shared__ float part[2][16][16];
     const int in = (int)threadIdx.x & 15, slice = (int)threadIdx.x >> 4, all = SECOND ? 2 * j.columns : j.columns;
     if ((int)blockIdx.x >= all) {
-        const int image = (int)blockIdx.x - all;        // (rows are counted in 31 bits)
+        const int image = (int)blockIdx.x - all;
         const float *from = j.row_sums + (long long)image * j.rows;
         // (in 64 bits: an image's rows may be millions of numbers that cancel)
         __shared__ double waves[16];
         double s = 0.;
 #pragma unroll 16
-        for (int r = (int)threadIdx.x; r < j.rows; r += 1024)
+        for (long long r = (int)threadIdx.x; r < j.rows; r += 1024)
             s += (double)from[r];
 #pragma unroll
         for (int d = 1; d < 64; d *= 2)

@@ -92,6 +92,23 @@ def test_block_end_past_32_bit_offsets():
         assert bool(((back[k].double() - totals[k]).abs() <= 1.1 * U16 * (sizes[k] + back[k].double().abs()) + 2.0 ** -20).all()), k
 
 
+def test_gate_of_an_image_of_nearly_2_to_31_rows():
+    P = 2 ** 31 - 1
+    x, gz = normal(1, P, 1, seed=1), normal(1, P, 1, seed=2, size=0.5)
+    gate = torch.tensor([0.75], device="cuda")
+    z = dcn.dcnv4_norm_scale_add_norm(x, gz, None, gate)[0]
+    for c in pieces(P, 2 ** 27):
+        assert torch.equal(z[0, c], gz[0, c].float().add_(x[0, c].float(), alpha=0.75).half())   # (0.75 x is exact)
+    del z
+    grad_x, _, _, grad_gate, *_ = dcn.dcnv4_norm_scale_add_norm_backward(x, None, None, gate, None, None, (None,) * 4, None, gz)
+    want = 0.0
+    for c in pieces(P, 2 ** 27):
+        want += float((x[0, c].double() * gz[0, c].double()).sum())
+        assert torch.equal(grad_x[0, c], (gz[0, c].float() * 0.75).half())
+    # (products are exact in fp32; sums in 64 bits, one rounding to fp32)
+    assert abs(float(grad_gate[0]) - want) <= 2.0 ** -24 * abs(want) + 1e-3
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_past_32_bit_offsets(bits):
     n, part = 2 ** 31 + 256 * 3 + 77, 2 ** 20
