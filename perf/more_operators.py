@@ -3,8 +3,8 @@ backward pass of the linear layer, the two ends of a residual block with norms, 
 over a network's tensors.
 
 Feature maps enter as rows: P pixels of K (or C) channels.  `run` computes a case either through the framework's entry
-points (`own`) or in plain torch operations in 32 bits, rounded once at the end (in 64 where 32 lose what matters:
-moments that are rounded to 8 bits, an image's sum of millions of numbers that cancel).
+points (`own`) or in plain torch operations in 32 bits, rounded once at the end (moments in 64, where they are rounded
+to 8 bits).
 
 Gated layer: h = act(x Wg^T + bg) * (x Wu^T + bu), w = (Wg, Wu), b = (bg, bu); act: silu or gelu (with erf).
 
@@ -221,7 +221,7 @@ def _run_own(s):
     if op in ("end", "end_train"):
         first = (s["gamma1"], s["beta1"]) if "gamma1" in s else None
         second = (s["gamma2"], s["beta2"]) if "gamma2" in s else None
-        z, y, *stats = dcn.dcnv4_norm_scale_add_norm(s["x"], s["residual"], s["scale"], s["gate"], first, second, eps=NORM_EPS, stats=op != "end")
+        z, y, *stats = dcn.dcnv4_norm_scale_add_norm(s["x"], s["residual"], s["scale"], s["gate"], first, second, eps=NORM_EPS)
         if op == "end":
             return z, y
         return (z, y, *dcn.dcnv4_norm_scale_add_norm_backward(s["x"], z, s["scale"], s["gate"], first, second, stats, s["grad_y"], s["grad_z"],
@@ -349,7 +349,7 @@ def run(s):
     if "gamma1" in f:
         grad_x = _norm_backward(unit1, rstd1, gb * f["gamma1"])
         gamma1, beta1 = (gb * unit1).sum(pixels).to(dt), gb.sum(pixels).to(dt)
-    return (z, y, grad_x.to(dt), grad.to(dt), (grad * gate * b).sum(pixels).to(dt), (grad * f["scale"] * b).double().sum((1, 2)).float(), gamma1, beta1, gamma2, beta2)
+    return (z, y, grad_x.to(dt), grad.to(dt), (grad * gate * b).sum(pixels).to(dt), (grad * f["scale"] * b).sum((1, 2)), gamma1, beta1, gamma2, beta2)
 
 
 def work(case):
