@@ -381,9 +381,10 @@ typedef struct {
  * NULL (f0 = f1 = 1), or the device address of two fp32 numbers f0, f1 (8-byte aligned): a loss scale's inverse times what clips gradients, and a schedule's
  * factor.  Where f0 is infinite or NaN the step changes nothing (a loss scale that was too large).  Both are for captured graphs, whose
  * arguments stay what they were.  state_bits: 32, or 8: m and r = sqrt(v) are stored as e4m3 (fp8, largest number 448, zeros to start with), times a scale
- * of its own for each 256 elements of the tensor: their largest magnitude / 448 (zeros for blocks below 2^-100).  m * 448 / that magnitude is rounded to nearest; r so
- * scaled to one of its two neighbours, up with the probability that keeps its mean (random bits of dcnv4_dropout's generator with key `seed` and
- * counter (i / 8 + number of the tensor * 2^40, t), 16 for element i as there), and never from above zero to zero.  With 8 bits g must be finite where f0
+ * of its own for each 256 elements of the tensor: their largest magnitude / 448 (zeros for blocks of m below 2^-100, and for blocks of r below 2^-75, as v in fp32 is
+ * zero below 2^-150).  m * 448 / that magnitude is rounded to nearest; r so scaled to one of its two neighbours, up with the probability that keeps its mean
+ * (random bits of dcnv4_dropout's generator with key `seed` and counter (i / 8 + number of the tensor * 2^40, t), 16 for element i as there), and in
+ * other blocks never from above zero to zero.  With 8 bits g must be finite where f0
  * is, and less than 2^63: a block of elements shares what is not.
  * 0 <= beta < 1, eps > 0 (a normal fp32 number), step >= 1 (0 with step_on_device). */
 int dcnv4_adamw(const dcnv4_adamw_tensor *tensors, int count, double beta1, double beta2, double eps, long long step,

@@ -3,7 +3,8 @@
 // with m and v in fp32, or m and r = sqrt(v) in 8 bits (e4m3: 3 bits behind the point) times an fp32 scale per block of 256 elements.  The root is
 // kept, and not v, since e4m3 reaches from 448 down to 2^-9: 18 powers of two of r are 36 of v.  m is rounded to nearest.  r is rounded
 // to either neighbour, with the probability that keeps its mean: with b2 = 0.999 a step moves r by less than a thousandth, and rounding to the nearest (up
-// to 1/16 away) would take it back to where it was, for good.  r above zero never becomes zero, which would leave eps alone to divide by.
+// to 1/16 away) would take it back to where it was, for good.  r above zero does not become zero, which would leave eps alone to divide by, but in blocks
+// whose largest is below 2^-75 (as v in fp32 is zero below 2^-150): r is the root of v in 64 bits, not of v in fp32, which a small r beside larger ones has not.
 //
 // Memory bounds it: an element is read and written once.  The moments are made in 64 bits (their rate leaves room for it), so that what is rounded to 8 bits
 // does not hang on the order of operations.  A launch takes up to kRecords tensors, whose addresses travel with its
@@ -23,7 +24,8 @@ namespace {
 constexpr int kAdamBlock = 256;                            // elements that share a scale
 constexpr int kPart = 256 * 8;                             // elements of a workgroup: a run of eight to a lane
 constexpr int kRecords = 56;                               // of a launch: its arguments are 4 KiB at most
-constexpr float kTop = 448.f, kNone = 0x1p-100f;           // e4m3's largest number; a block whose largest is less is stored as zeros
+constexpr float kTop = 448.f;                              // e4m3's largest number
+constexpr float kNoM = 0x1p-100f, kNoR = 0x1p-75f;         // a block whose largest is less is stored as zeros
 
 struct AdamTensor {
     long long n;
@@ -113,14 +115,21 @@ __device__ __forceinline__ float block_max(float v)
     return fmaxf(a, b);
 }
 
-// A number t from 0 to 448 to one of its neighbours in e4m3, up with probability (missing part) by 16 bits, and not from above zero to zero.
-__device__ __forceinline__ float round_by(float t, unsigned bits)
+// The root of a number of 64 bits in fp32, below fp32's range too: its bits, where v has a square there, are those of (float)v's root.
+__device__ __forceinline__ float root_of(double v)
+{
+    const bool small = v < 0x1p-100;
+    return __builtin_sqrtf((float)(small ? v * 0x1p200 : v)) * (small ? 0x1p-100f : 1.f);
+}
+
+// A number t from 0 to 448 to one of its neighbours in e4m3, up with probability (missing part) by 16 bits; what is above zero, whatever t is, not to zero.
+__device__ __forceinline__ float round_by(float t, bool above_zero, unsigned bits)
 {
     const float fine = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, t) + (bits << 4)) & ~0xFFFFFu);
     const float coarse = (float)(((int)(t * 0x1p25f) + (int)bits) >> 16) * 0x1p-9f;      // numbers below 2^-6 are 2^-9 apart
     float q = t < 0x1p-6f ? coarse : fine;
     q = q < 0x1p-9f ? 0x1p-9f : q;
-    return t == 0.f ? 0.f : q;
+    return above_zero ? q : 0.f;
 }
 
 }  // namespace
@@ -160,6 +169,7 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
     const float rate = (float)(lr * unbias1);
     const double c1 = 1.0 - a.b1, c2 = 1.0 - a.b2;
     float m[8], r[8], v[8];
+    bool some[8];                                          // of v
     double sm = 1.0, sr = 1.0;
     if constexpr (EIGHT) {
         from_8_bits(m0, m);
@@ -183,8 +193,10 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
             vv *= vv;
         }
         m[e] = (float)__builtin_fma(a.b1, mm, c1 * g);
-        v[e] = (float)__builtin_fma(a.b2, vv, c2 * (g * g));
-        r[e] = __builtin_sqrtf(v[e]);
+        vv = __builtin_fma(a.b2, vv, c2 * (g * g));
+        v[e] = (float)vv;
+        r[e] = EIGHT ? root_of(vv) : __builtin_sqrtf(v[e]);
+        some[e] = vv > 0.;
     }
     Raw8<float> out;
     Raw8<_Float16> half;
@@ -206,8 +218,8 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
         }
         tm = block_max(tm);
         tr = block_max(tr);
-        tm = tm >= kNone ? tm : 0.f;
-        tr = tr >= kNone ? tr : 0.f;
+        tm = tm >= kNoM ? tm : 0.f;
+        tr = tr >= kNoR ? tr : 0.f;
         const float im = tm > 0.f ? kTop / tm : 0.f, ir = tr > 0.f ? kTop / tr : 0.f;
         const Bits8 bits = philox((unsigned long long)(i >> 3) + ((unsigned long long)(a.number + at) << 40), (unsigned long long)step, a.seed);
 #pragma unroll
@@ -215,7 +227,7 @@ template <typename T, bool EIGHT> __global__ __launch_bounds__(256) void dcnv4_a
             m[e] *= im;
             m[e] = m[e] > kTop ? kTop : m[e] < -kTop ? -kTop : m[e];
             r[e] *= ir;
-            r[e] = round_by(r[e] > kTop ? kTop : r[e], (bits.w[e / 2] >> (16 * (e & 1))) & 0xffffu);
+            r[e] = round_by(r[e] > kTop ? kTop : r[e], some[e] && tr > 0.f, (bits.w[e / 2] >> (16 * (e & 1))) & 0xffffu);
         }
         put((Byte *)t.m + i, left, to_8_bits(m));
         put((Byte *)t.v + i, left, to_8_bits(r));
