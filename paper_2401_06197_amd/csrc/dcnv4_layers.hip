@@ -787,6 +787,16 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
     return DCNV4_OK;
 }
 
+// Lanes side by side over N columns, eight each, in the sums over runs of rows.
+constexpr int kChain = 256;
+int lanes_log_of(int N)
+{
+    int log = 0;
+    while (log < 6 && (8 << log) < N)
+        ++log;
+    return log;
+}
+
 int plan_linear_backward(LayerPlan *out, long long P, int K, int N, int dtype)
 {
     if (const int rc = check_layer(P, K, N, dtype))
@@ -805,10 +815,11 @@ int plan_linear_backward(LayerPlan *out, long long P, int K, int N, int dtype)
         p.w_split = room.take((long long)N * 6 * p.kp);
         p.g_split = room.take(P * 6 * p.np);
     }
-    // runs of rows: two workgroups to a unit, 32 rows at least
-    const long long across = (N / 8 + 63) / 64;
-    long long runs = across < 512 ? 512 / across : 1;
-    p.columns_rows = (int)round_up((P + runs - 1) / runs, 32);
+    // runs of rows: two workgroups to a unit, 32 rows at least, and no more than give a lane kChain numbers to add up one after the other (fp32 sums of one sign
+    // lose as many halves of a step: 131080 outputs and 8192 rows, in one run until then, were 2^-15 off)
+    const long long across = (N / 8 + 63) / 64, chain = (long long)kChain * (256 >> lanes_log_of(N));
+    const long long runs = across < 512 ? 512 / across : 1, rows = round_up((P + runs - 1) / runs, 32);
+    p.columns_rows = (int)(rows < chain ? rows : chain);
     p.columns_runs = (int)((P + p.columns_rows - 1) / p.columns_rows);
     p.bias_sums = room.take((long long)p.columns_runs * N * 4);
     if (!plan_gradients(p, room))
@@ -983,9 +994,7 @@ int linear_backward(const LayerPlan &p, const void *x, const void *w, const void
     Bias b = {};
     if (grad_b) {
         b = {(const float *)(ws + p.bias_sums), p.columns_runs, p.N, (p.N + 15) / 16, grad_b};
-        int log = 0;
-        while (log < 6 && (8 << log) < p.N)
-            ++log;
+        const int log = lanes_log_of(p.N);
         const int across = (p.N / 8 + (1 << log) - 1) >> log;
         ahead.g = grad_y;
         ahead.sums = (float *)(ws + p.bias_sums);
