@@ -977,10 +977,11 @@ class AdamwPlan:
 
     def set(self, lr=None, weight_decay=None):
         """Other learning rates or weight decays from the next step on: a number, or one for each tensor."""
-        for name, values in (("lr", lr), ("weight_decay", weight_decay)):
-            if values is not None:
-                for record, value in zip(self.records, _each(values, len(self), name)):
-                    setattr(record, name, value)
+        # (both are looked at before the first is set)
+        new = [(name, _each(values, len(self), name)) for name, values in (("lr", lr), ("weight_decay", weight_decay)) if values is not None]
+        for name, values in new:
+            for record, value in zip(self.records, values):
+                setattr(record, name, value)
 
 
 def _each(values, count, name):
