@@ -543,7 +543,7 @@ def _check_like(x, named):
 
 
 def _check_plain(name, t, at, shape, dtype):
-    if t.get_device() != at or t.dtype is not dtype or not t.is_contiguous() or t.shape != shape:
+    if t is None or t.get_device() != at or t.dtype is not dtype or not t.is_contiguous() or t.shape != shape:
         raise ValueError(f"dcnv4: {name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on x's device")
 
 
@@ -861,7 +861,7 @@ def dcnv4_norm_scale_add_norm(x, residual, scale=None, gate=None, first=None, se
 def dcnv4_norm_scale_add_norm_backward(x, z, scale, gate, first, second, stats, grad_y, grad_z=None, grad_gate=True, workspace=None, out=None,
                                        stream=None, prepare_only=False):
     """(grad_x, grad_residual, grad_scale, grad_gate, grad_gamma1, grad_beta1, grad_gamma2, grad_beta2) of dcnv4_norm_scale_add_norm, from its z and
-    stats = (mean1, rstd1, mean2, rstd2).  grad_y is None without a second norm, where grad_residual is grad_z itself (in `out`: None).
+    stats = (mean1, rstd1, mean2, rstd2), None where there is no such norm.  grad_y is None without a second norm, where grad_residual is grad_z itself (in `out`: None).
     Gradients of what is None are None; so is the gates' with grad_gate=False."""
     import torch
     if second is None:
@@ -872,6 +872,8 @@ def dcnv4_norm_scale_add_norm_backward(x, z, scale, gate, first, second, stats, 
         raise ValueError("dcnv4: a second norm's backward pass takes z and grad_y")
     P, C, gates, norms, gamma1, beta1, gamma2, beta2 = _end_args(x, scale, gate, first, second, (("z", z), ("grad_y", grad_y), ("grad_z", grad_z)))
     shape, dt, at, f32, vector = x.shape, x.dtype, x.get_device(), torch.float32, (C,)
+    if stats is None or len(stats) != 4:
+        raise ValueError("dcnv4: stats must be (mean1, rstd1, mean2, rstd2)")
     mean1, rstd1, mean2, rstd2 = stats
     if second is not None:
         _check_plain("mean2", mean2, at, shape[:-1], f32)
