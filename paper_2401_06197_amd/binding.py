@@ -901,16 +901,18 @@ def dcnv4_linear_backward_workspace_bytes(P, K, Nout, dtype):
     return int(load_library().dcnv4_linear_backward_workspace_bytes(P, K, Nout, dtype))
 
 
-def dcnv4_linear_backward(x, w, grad_y, b=None, need_x=True, workspace=None, out=None, stream=None, prepare_only=False):
-    """(grad_x, grad_w, grad_b) of dcnv4_linear for grad_y [..., Nout]; grad_b is None where b is, grad_x with need_x=False (a first layer)."""
+def dcnv4_linear_backward(x, w, grad_y, b=None, need_x=True, workspace=None, out=None, stream=None, prepare_only=False, need_w=True):
+    """(grad_x, grad_w, grad_b) of dcnv4_linear for grad_y [..., Nout]; grad_b is None where b is, grad_x with need_x=False (a first layer), grad_w with
+    need_w=False (a layer that is not trained).  Sizes as in include/dcnv4.h, which are more than dcnv4_linear takes."""
     P, K = _rows(x)
     if w.dim() != 2 or w.shape[1] != K:
         raise ValueError("dcnv4: expected x [..., K], w [Nout, K]")
     N, shape, dt = w.shape[0], x.shape, x.dtype
     _check_like(x, (("w", w, w.shape), ("b", b, (N,)), ("grad_y", grad_y, (*shape[:-1], N))))
-    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt), None if b is None else ("grad_b", (N,), dt)), stream)
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt) if need_w else None,
+                                   None if b is None else ("grad_b", (N,), dt)), stream)
     space, size = _workspace(x, workspace, dcnv4_linear_backward_workspace_bytes(P, K, N, _dtype_code(x)) if workspace is None else 0, stream)
-    args = (x.data_ptr(), w.data_ptr(), grad_y.data_ptr(), _ptr(gx), gw.data_ptr(), _ptr(gb), space.data_ptr(), size, P, K, N, _dtype_code(x),
+    args = (x.data_ptr(), w.data_ptr(), grad_y.data_ptr(), _ptr(gx), _ptr(gw), _ptr(gb), space.data_ptr(), size, P, K, N, _dtype_code(x),
             _stream_ptr(stream, x.device))
     if prepare_only:
         return _prepared(args, out, workspace)
@@ -951,15 +953,18 @@ def dcnv4_gated_linear(x, w, b=None, activation="silu", workspace=None, out=None
     return h
 
 
-def dcnv4_gated_linear_backward(x, w, grad_h, b=None, activation="silu", need_x=True, workspace=None, out=None, stream=None, prepare_only=False):
-    """(grad_x, grad_w, grad_b) of dcnv4_gated_linear for grad_h [..., F]; grad_b is None where b is, grad_x with need_x=False (a first layer)."""
+def dcnv4_gated_linear_backward(x, w, grad_h, b=None, activation="silu", need_x=True, workspace=None, out=None, stream=None, prepare_only=False, need_w=True,
+                                need_b=True):
+    """(grad_x, grad_w, grad_b) of dcnv4_gated_linear for grad_h [..., F]; grad_b is None where b is, grad_x with need_x=False (a first layer), grad_w and
+    grad_b with need_w=False and need_b=False (a layer that is not trained)."""
     P, K, F, act = _gated_args(x, w, b, activation)
     shape, dt = x.shape, x.dtype
     _check_like(x, (("grad_h", grad_h, (*shape[:-1], F)),))
-    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt), None if b is None else ("grad_b", (2, F), dt)), stream)
+    gx, gw, gb = _outputs(x, out, (("grad_x", shape, dt) if need_x else None, ("grad_w", w.shape, dt) if need_w else None,
+                                   ("grad_b", (2, F), dt) if need_b and b is not None else None), stream)
     code = _dtype_code(x)
     space, size = _workspace(x, workspace, dcnv4_gated_linear_workspace_bytes(P, K, F, code, True) if workspace is None else 0, stream)
-    args = (x.data_ptr(), w.data_ptr(), _ptr(b), grad_h.data_ptr(), _ptr(gx), gw.data_ptr(), _ptr(gb), space.data_ptr(), size, P, K, F, act, code,
+    args = (x.data_ptr(), w.data_ptr(), _ptr(b), grad_h.data_ptr(), _ptr(gx), _ptr(gw), _ptr(gb), space.data_ptr(), size, P, K, F, act, code,
             _stream_ptr(stream, x.device))
     if prepare_only:
         return _prepared(args, out, workspace)
