@@ -167,7 +167,7 @@ struct Deltas {
     const void *grad_h;
     unsigned short *d;                                     // [P][PL planes][2F]
     float *bias_sums;                                      // [pixel runs of 32 * WN][2F], or null
-    const float *most;                                     // fp16: largest |grad_h| of `parts` parts; no parts: grad_h has `few` numbers
+    const float *most;                                     // fp16: largest |grad_h| of `parts` parts; no parts: grad_h (of the one launch) has `few` numbers
     int parts, few;
     Scale *scale;                                          // fp16: what undoes d's factor
 };
@@ -582,7 +582,6 @@ struct LayerOptions {
     int tile = 0, splits = 0;          // as loss_tile and loss_splits
 } g_layers;
 
-// One more limit than the products': byte offsets inside a gated layer's weights are 32 bits (fp32: of three planes of 16 bits).
 constexpr int kFewNumbers = 1 << 15;                       // of grad_h, which every workgroup looks through by itself
 constexpr int kLayerMaxRows = 1 << 24, kLayerMaxWidth = 1 << 20;
 
@@ -762,6 +761,7 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
     p.K = K;
     p.N = p.np = 2 * F;
     p.kp = p.pl == 1 ? K : (int)round_up(K, 32);
+    // one more limit than the products': byte offsets inside the weights are 32 bits (fp32: of three planes of 16 bits)
     if ((long long)p.N * p.pl * p.kp * 2 >= 0x7fffffffLL)
         return DCNV4_ERR_UNSUPPORTED;
     p.forward = parts_of(p.pl, p.N, p.P, p.kp);
@@ -774,7 +774,8 @@ int plan_gated(LayerPlan *out, long long P, int K, int F, int dtype, bool backwa
         p.w_split = room.take((long long)p.N * 6 * p.kp);
     }
     if (backward) {
-        p.most_parts = P * F <= kFewNumbers ? 0 : (int)(P * F / 8 / 1024 < 512 ? P * F / 8 / 1024 + 1 : 512);
+        // (0: workgroups look through all of grad_h, from where their launch's rows begin, so there may be one launch only)
+        p.most_parts = P * F <= kFewNumbers && p.forward.count == 1 ? 0 : (int)(P * F / 8 / 1024 < 512 ? P * F / 8 / 1024 + 1 : 512);
         p.scale = room.take(sizeof(Scale));
         p.most = room.take((p.most_parts + 1) * 4);
         p.d = room.take(P * p.pl * p.N * 2);
