@@ -157,7 +157,8 @@ int dcnv4_linear(const void *x, const void *w, const void *b, void *y,
  *     grad_x[p] = sum_o grad_y[p][o] * w[o],   grad_w[o] = sum_p grad_y[p][o] * x[p],   grad_b[o] = sum_p grad_y[p][o]
  * Each of the three may be NULL where not wanted (not all); x is read for grad_w alone, w for grad_x alone.  Sums are fp32 in a fixed order, rounded once in
  * F16.  F32: operands as three bf16 numbers, fp32's accuracy for numbers above 2^-100; finite and below 3.3e38.
- * Needs K and Nout multiples of 8, at most 2^24 rows, K and Nout at most 2^20 (else DCNV4_ERR_UNSUPPORTED).
+ * Needs K and Nout multiples of 8, at most 2^24 rows, K and Nout at most 2^20 (else DCNV4_ERR_UNSUPPORTED): more layers than dcnv4_linear takes, which needs
+ * Nout a multiple of 32 and whole 32 bytes of K (fp16 2728 -> 1024 or 936 -> 352 and fp32 384 -> 1000 have this gradient here and no forward layer).
  * `workspace`: at least dcnv4_linear_backward_workspace_bytes() bytes. */
 int dcnv4_linear_backward(const void *x, const void *w, const void *grad_y, void *grad_x, void *grad_w, void *grad_b, void *workspace,
                           long long workspace_bytes, long long P, int K, int Nout, int dtype, void *stream);
@@ -177,9 +178,10 @@ int dcnv4_gated_linear(const void *x, const void *w, const void *b, void *h, voi
 
 /* Its backward pass, from grad_h [P][F]; a and u are made again.  With da = grad_h * u * act'(a) and du = grad_h * act(a):
  *     grad_x[p] = sum_f da[p][f] * w[0][f] + du[p][f] * w[1][f],   grad_w = (sum_p da[p][f] * x[p], sum_p du[p][f] * x[p]),   grad_b = sums over the rows
- * Each of the three may be NULL where not wanted (not all).  In F16 da and du are rounded to fp16, times a power of two that puts the largest finite
- * |grad_h| into [2, 4), for grad_x and grad_w: they keep all of fp16's bits down to 2^-16 of it, and u * act'(a) and act(a) have to be less than 16000.
- * grad_b is made from fp32 numbers alone.  Sums are fp32 in a fixed order.
+ * Each of the three may be NULL where not wanted (not all).  In F16 da and du are rounded to fp16, times one power of two that puts the largest finite
+ * |grad_h| of the tensor into [2, 4), for grad_x and grad_w: they keep all of fp16's bits down to 2^-15 of that, lose them one by one below and are zero from
+ * 2^-27 on (2^-26 where that lies at 2), so a row whose grad_h is that much smaller than another's gets no more of grad_x; and u * act'(a) and act(a) have to be less than 16000
+ * (else infinities).  F32 has neither limit.  grad_b is made from fp32 numbers alone.  Sums are fp32 in a fixed order.
  * `workspace`: at least dcnv4_gated_linear_workspace_bytes(..., backward = 1) bytes. */
 int dcnv4_gated_linear_backward(const void *x, const void *w, const void *b, const void *grad_h, void *grad_x, void *grad_w, void *grad_b, void *workspace,
                                 long long workspace_bytes, long long P, int K, int F, int activation, int dtype, void *stream);

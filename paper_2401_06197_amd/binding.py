@@ -974,7 +974,8 @@ def dcnv4_gated_linear_backward(x, w, grad_h, b=None, activation="silu", need_x=
 
 class AdamwPlan:
     """The tensors of a dcnv4_adamw_step, checked and listed once (dcnv4_adamw_plan makes it).  It holds their memory and works there at each
-    step: a tensor that is given other memory (a gradient that is made anew) needs a new plan."""
+    step: a tensor that is given other memory needs a new plan.  Gradients among them: where autograd makes them anew (torch's zero_grad() drops them unless
+    it is called with set_to_none=False), an old plan's step reads the old ones."""
 
     def __init__(self, records, held, device, state_bits, dtype):
         self.records, self.held, self.device, self.state_bits, self.dtype = records, held, device, state_bits, dtype

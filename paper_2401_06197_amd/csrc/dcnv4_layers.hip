@@ -6,11 +6,13 @@
 // stored in 16 bits as d [P][2F], and the two products
 //     grad_x[p] = sum_j d[p][j] * w[j],    grad_w[j] = sum_p d[p][j] * x[p]
 // whose operands lie as they are and are turned on the way from LDS to registers where the product wants them turned.  grad_b's sums are of d before it
-// is rounded.  a and u are not kept from the forward pass: they would be 2F numbers a row, twice what h takes, written and read; making them again costs
-// a third of the whole step's products.
+// is rounded.  a and u are not kept from the forward pass: that would hold 2F numbers a row from there to here, twice h's memory, and in fp16 round both once
+// more before anything is made of them.  It would not be slower: making them again is a third of the step's products, for 12544 x 512, 2 x 2048, fp16
+// 53 GFLOP, 75 us at the rate below, where 205 MB written and read are 41 us of a copy.
 //
 // fp16: d is rounded to fp16 once, for both products, times a power of two that puts the largest |grad_h| into [2, 4): u * act'(a) and act(a) may be as
-// large as 16000 before d is infinite, and d of down to 2^-16 of the largest grad_h keeps all bits.  fp32: operands as three bf16 numbers, six products.
+// large as 16000 before d is infinite, and d of down to 2^-15 of the largest grad_h keeps all bits (2^-14, fp16's least normal number, is 2^-15 of what
+// lies at 2); from 2^-27 on it is zero.  fp32: operands as three bf16 numbers, six products.
 //
 // What bounds it: large layers the matrix units, under the card's power limit, and the results of tiles; small ones the steps of a tile one after the
 // other.  fp16, 12544 x 512, 2 x 2048: h 68 + 7 us (700 TFLOP/s; a library's product with K = 512 reaches 680), d 92 + 8 (with 102 MB written), both
@@ -627,8 +629,10 @@ struct Room {
 };
 
 // Tiles of pairs and pixels: the products', and in fp16 one more, half a large one by four waves, two workgroups to a unit, where one's products go on while the other
-// makes its results: with few features that is most of a tile's time.  Times as in `estimate`, of the forward kernel and the one that makes d together,
-// fitted to 31 layers (49 to 134400 pixels, K 32 to 2048, F 128 to 4096) in every tile so that the choice costs least: 0.4 % (fp16) and 0 on average.
+// makes its results: with few features that is most of a tile's time.  What `estimate` makes of these figures ranks the tiles: they were
+// fitted to the forward kernel and the one that makes d together, of 31 layers (49 to 134400 pixels, K 32 to 2048, F 128 to 4096) in every tile, so that the
+// choice costs least (0.4 % in fp16, 0 in fp32, on average), not so that it is the time, of which it is 0.5 (three rounds of large tiles: 88 for 160 us) to 0.9 (half a
+// round: 47 for 53).
 // Forward and d, 50176 x 256, 2 x 1024: 400, 238, 259 and 225 us by the four tiles; 8192 x 1024, 2 x 2816: 390, 268, 229, 250; 1000 x 1024, 2 x 1024: 25, 28, 53, 39.
 enum { kTall = kLarge + 1, kGatedTiles };
 const Shape &gated_shape(int pl, int i)
@@ -672,7 +676,7 @@ Parts parts_of(int pl, int m, int P, int length)
     if (g_layers.tile || first <= 0 || first >= P)
         return best;
     const Choice rest = choose_gated(pl, m, P - first, length, 0);
-    // (6: two launches more)
+    // (6: two launches more, in units of the estimate, which are up to two us)
     if (estimate(s, m, first, length, 1) + estimate(gated_shape(pl, rest.shape), m, P - first, length, 1) + 6.f <
         estimate(gated_shape(pl, best.choice[0].shape), m, P, length, 1))
         best = {2, {(int)first, P - (int)first}, {{kLarge, 1}, rest}};
@@ -680,7 +684,7 @@ Parts parts_of(int pl, int m, int P, int length)
 }
 
 // The two products of a gradient, [P][K] over N numbers and [N][K] over P, in one launch: the tile and over how many workgroups each sum is split, with the
-// lowest estimated time (us).  Workgroups that are all there at once take as long as the longest, `share` to a unit; more of them share the units, which feel a
+// lowest estimate (which is 0.7 to 0.9 of the time in us: 91 for 129, 54 for 75, 30 for 34; it is made to rank).  Workgroups that are all there at once take as long as the longest, `share` to a unit; more of them share the units, which feel a
 // part (`tail`) of one of the shorter kind in the end.  A tile takes `step` for a step (alone on its unit `alone`) and `fixed`.  Planes are written and read once
 // more, by a launch of its own.  Fitted to 34 layers (23 to 50176 rows, K 32 to 2048, 40 to 4096 results; every tile, 1 to 64 splits of either sum, 1950
 // measurements) so that the choice costs least: 1.8 % (fp16) and 1.4 % (fp32) on average, 8 % at most.  12544, 512 -> 4096: 107 us with large tiles and 4 parts of
